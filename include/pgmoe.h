@@ -63,7 +63,10 @@ typedef enum {
     PGMOE_ESTATE = -7      /* call order violated (e.g. FFN of a block that was never fetched) */
 } pgmoe_status;
 
-typedef enum { PGMOE_F32 = 0, PGMOE_BF16 = 1 } pgmoe_dtype;
+/* A context's dtype is one of the first two.  The routing and 8-bit expert operators below also take
+ * the others: e4m3 has 3 fraction bits, a largest value of 448 and no infinities, e5m2 has 2, 57344
+ * and infinities. */
+typedef enum { PGMOE_F32 = 0, PGMOE_BF16 = 1, PGMOE_F16 = 2, PGMOE_E4M3 = 3, PGMOE_E5M2 = 4 } pgmoe_dtype;
 
 /* Bits of pgmoe_config.flags */
 #define PGMOE_FLAG_HOST_ONLY 1u /* create no device resources: argument checks and host logic
@@ -383,6 +386,101 @@ typedef struct {
  * whatever max_tokens the context was created with. */
 int pgmoe_stack_step(pgmoe_ctx *ctx, const pgmoe_step_buffers *io, int T, void *compute_stream,
                      void *copy_stream);
+
+/* ---- routing from logits, with its gradient ------------------------------------------------
+ * pgmoe_pregate_topk() is the paper's gate: softmax, the k largest, probabilities as weights.  The calls
+ * below route from logits the caller has, in the other ways mixture-of-experts models do, and train the
+ * router.  They and the 8-bit calls further down need no context (sizes are the call's own, the text of an
+ * error is pgmoe_last_error(NULL)'s, a process without a GPU gets PGMOE_ENODEVICE once the arguments have
+ * passed), allocate nothing and may be captured into a HIP graph.
+ *
+ * For every token: an expert whose logit z is NaN or -infinity is unavailable.
+ *   scores     s = softmax(z) over the available experts, or 1 / (1 + exp(-z)); 0 for the others.
+ *   selection  by v = s + bias (a balancing bias moves the selection, never a weight; a NaN bias counts
+ *              as -infinity); without a bias by z itself.  With n_groups > 1 the experts are n_groups runs
+ *              of n_experts / n_groups; a group is worth the sum of the two largest s + bias above
+ *              -infinity of its available experts (of the one it has, or nothing: then it ranks last), the
+ *              topk_groups worthiest are kept (equal: the lowest) and only their experts are selected.
+ *              The top_k largest v in descending order, equal values to the lowest index, unavailable
+ *              experts last.  Values that 32 bits do not tell apart are compared in 64.
+ *   weights    scale * s, or with renormalize scale * s / (sum of the selected s); 0 for an unavailable
+ *              expert, so all 0 for a token that has no available one. */
+#define PGMOE_SCORE_SOFTMAX 0
+#define PGMOE_SCORE_SIGMOID 1
+#define PGMOE_MAX_GROUPS 16
+typedef struct {
+    int32_t n_experts;    /* 1 .. PGMOE_MAX_EXPERTS */
+    int32_t top_k;        /* 1 .. experts of topk_groups groups */
+    int32_t n_groups;     /* 1 .. PGMOE_MAX_GROUPS, divides n_experts; 0 counts as 1 */
+    int32_t topk_groups;  /* 1 .. n_groups; 0 counts as n_groups */
+    int32_t score;        /* PGMOE_SCORE_* */
+    int32_t renormalize;  /* 0 or 1 */
+    float scale;          /* finite */
+    int32_t logits_dtype; /* PGMOE_F32, PGMOE_BF16 or PGMOE_F16: logits and d_logits */
+} pgmoe_router;
+/*   logits dev [T, E], rows logits_stride >= E elements apart    bias dev [E] f32 | NULL
+ *   topk_idx dev [T,k] int32 out    topk_weight dev [T,k] f32 out    scores_out dev [T,E] f32 out | NULL */
+int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_stride, const float *bias, int T,
+                int32_t *topk_idx, float *topk_weight, float *scores_out, void *stream);
+/* Gradient of the logits: d_weight dev [T,k] f32 is that of topk_weight, d_scores dev [T,E] f32 | NULL that of
+ * scores_out (a balancing loss on the scores); the selection topk_idx (distinct experts a token, as pgmoe_route
+ * wrote them) and the bias are constants.  With total = sum of the selected s and c = scale
+ *   d_s[e] = d_scores[e] + (e selected: c * d_weight, renormalised c * (d_weight - sum d_weight s / total) / total)
+ *   softmax: d_z = s * (d_s - sum d_s s)      sigmoid: d_z = s * (1 - s) * d_s       unavailable experts: 0.
+ * An index outside [0, E) contributes nothing.
+ *   d_logits dev [T, E] in logits_dtype, rows d_logits_stride apart, out; d_logits may not overlap logits. */
+int pgmoe_route_backward(const pgmoe_router *router, const void *logits, int64_t logits_stride, const int32_t *topk_idx,
+                         const float *d_weight, const float *d_scores, int T, void *d_logits, int64_t d_logits_stride,
+                         void *stream);
+/* The integer half of pgmoe_permute(), for callers whose rows are dealt out by pgmoe_quantize_rows(): row_of and
+ * expert_offsets as there. */
+int pgmoe_group_rows(pgmoe_ctx *ctx, const int32_t *topk_idx, int T, int32_t *row_of, int32_t *expert_offsets, void *stream);
+
+/* ---- experts in 8-bit floating point, one scale for each block of 128 -----------------------
+ * A value is its code times the scale of its block.  Quantising a block: scale = largest magnitude of its
+ * finite values / largest value of the type (448 or 57344), at least 2^-126; code = value / scale, a 32-bit
+ * quotient rounded to the nearest, ties to even.  NaN stays NaN; an infinity becomes NaN in e4m3 and stays one in
+ * e5m2.  All divisions are correctly rounded: the codes are a function of the input alone.
+ *
+ * Rows: codes [rows] of 128 * ceil(cols/128) bytes, row r at q + r * q_stride, zero past the last column; the scale
+ * of (row r, block b of 128 columns) at scale[b * scale_stride + r]. */
+typedef struct {
+    void *q;              /* dev, 16-byte aligned */
+    int64_t q_stride;     /* bytes, multiple of 16, >= 128 * ceil(cols/128) */
+    float *scale;         /* dev [ceil(cols/128), scale_stride] */
+    int64_t scale_stride; /* >= rows */
+    int32_t rows, cols;
+    int32_t dtype;        /* PGMOE_E4M3 or PGMOE_E5M2 */
+} pgmoe_fp8_rows;
+/* Weights, e4m3: the matrices of n_experts experts, y = x . W with W [n_in, n_out] as everywhere in this header, one
+ * scale for each 128 x 128 block: scale[(e * ceil(n_out/128) + o/128) * ceil(n_in/128) + i/128].  The code of input i
+ * and output o of expert e is byte
+ *   ((e * 8*ceil(n_out/128) + o/16) * ceil(n_in/128) + i/128) * 2048 + (i%128/64)*1024 + (i%64/16)*256 + (o%16)*16 + i%16
+ * of q: operand tiles of 16 outputs x 128 inputs, whole blocks of 128 in both directions, padded with zeros. */
+typedef struct {
+    void *q;       /* dev, 16-byte aligned, n_experts * 16384 * ceil(n_in/128) * ceil(n_out/128) bytes */
+    float *scale;  /* dev */
+    int32_t n_experts, n_in, n_out;  /* n_experts 1 .. PGMOE_MAX_EXPERTS */
+} pgmoe_fp8_weights;
+/* Quantise x dev [T, out->cols] (PGMOE_F32, BF16 or F16, rows x_stride elements apart).  row_of NULL: token t becomes
+ * row t (copies = 1, T <= out->rows).  row_of dev [T * copies]: token t becomes the rows row_of[t*copies + j] (what
+ * pgmoe_permute and pgmoe_group_rows give: the dispatch to experts, quantised once and written `copies` times); an
+ * entry outside [0, out->rows) is skipped. */
+int pgmoe_quantize_rows(const void *x, int64_t x_stride, int x_dtype, int T, const int32_t *row_of, int copies,
+                        const pgmoe_fp8_rows *out, void *stream);
+/* Quantise w dev [E, n_in, n_out] (PGMOE_F32, BF16 or F16; contiguous) into `forward` (y = x . W) and, if given, into
+ * `backward`, the same codes and scales laid out for d_x = d_y . W^T: its n_in is forward's n_out and the other way
+ * round.  Either may be NULL, not both. */
+int pgmoe_quantize_weights(const void *w, int w_dtype, const pgmoe_fp8_weights *forward, const pgmoe_fp8_weights *backward,
+                           void *stream);
+/* For every expert e and its rows [expert_offsets[e], expert_offsets[e+1]) of x: y[rows] = act(x[rows] . W_e), products on
+ * the matrix cores and sums in float32, each block of 128 inputs scaled by its row's and its weights' scale.
+ *   x->cols == w->n_in; expert_offsets dev [E+1], rows past x->rows are not touched; relu 0 or 1.
+ * Exactly one output: y dev [x->rows, n_out] (PGMOE_F32, BF16 or F16, rows y_stride >= n_out elements apart), or y_q
+ * (rows = x->rows, cols = n_out): the float32 results quantised as by pgmoe_quantize_rows, the next product's operand.
+ * Backward: the gradient of x is this call on d_y's codes with the `backward` weights. */
+int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, const int32_t *expert_offsets, int relu, void *y,
+                        int64_t y_stride, int y_dtype, const pgmoe_fp8_rows *y_q, void *stream);
 
 /* ---- observability: duration of the expert-FFN kernel ------------------------------------
  * pgmoe_ffn_timing_begin() makes every following pgmoe_expert_ffn() bracket its main kernel

@@ -14,7 +14,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpgmoe.so")
 
 OK, EINVAL, ENOTPINNED, ENOSLOT, EBADINDEX, EHIP, ENODEVICE, ESTATE = 0, -1, -2, -3, -4, -5, -6, -7
-F32, BF16 = 0, 1
+F32, BF16, F16, E4M3, E5M2 = 0, 1, 2, 3, 4
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+MAX_GROUPS = 16
+FP8_BLOCK = 128
 STREAMS_COMPUTE_COPY, STREAMS_COMPUTE_OWN, STREAMS_COPY_OWN = 1, 2, 4
 FLAG_HOST_ONLY = 1
 FLAG_FETCH_MEMCPY = 2
@@ -34,6 +37,7 @@ EXPORTS = [
     "pgmoe_permute", "pgmoe_expert_ffn", "pgmoe_combine", "pgmoe_stack_step", "pgmoe_device_flags",
     "pgmoe_ffn_timing_begin", "pgmoe_ffn_timing_end", "pgmoe_slot_address", "pgmoe_fetch_timing", "pgmoe_trace", "pgmoe_get_block_trace", "pgmoe_fetch_all_experts", "pgmoe_set_schedule",
     "pgmoe_ffn_kernel_name", "pgmoe_set_nonmoe_standin", "pgmoe_check_streams", "pgmoe_expert_ffn_static", "pgmoe_migration_engine", "pgmoe_fetch_experts_as_turn",
+    "pgmoe_route", "pgmoe_route_backward", "pgmoe_group_rows", "pgmoe_quantize_rows", "pgmoe_quantize_weights", "pgmoe_expert_matmul",
 ]
 
 
@@ -58,6 +62,20 @@ class StepBuffers(Structure):
     _fields_ = [("gate_w", POINTER(c_void_p)), ("gate_b", POINTER(c_void_p)), ("x_states", c_void_p),
                 ("y_blocks", c_void_p), ("topk_idx", c_void_p), ("topk_prob", c_void_p), ("row_of", c_void_p),
                 ("expert_offsets", c_void_p), ("x_perm", c_void_p), ("y_perm", c_void_p), ("workspace", c_void_p)]
+
+
+class RouterConfig(Structure):
+    _fields_ = [("n_experts", c_int32), ("top_k", c_int32), ("n_groups", c_int32), ("topk_groups", c_int32), ("score", c_int32),
+                ("renormalize", c_int32), ("scale", c_float), ("logits_dtype", c_int32)]
+
+
+class FP8Rows(Structure):
+    _fields_ = [("q", c_void_p), ("q_stride", c_int64), ("scale", c_void_p), ("scale_stride", c_int64), ("rows", c_int32), ("cols", c_int32),
+                ("dtype", c_int32)]
+
+
+class FP8Weights(Structure):
+    _fields_ = [("q", c_void_p), ("scale", c_void_p), ("n_experts", c_int32), ("n_in", c_int32), ("n_out", c_int32)]
 
 
 class PgmoeError(RuntimeError):
@@ -114,6 +132,12 @@ def _load():
     L.pgmoe_check_streams.argtypes = [vp, vp, vp, POINTER(c_int)]
     L.pgmoe_get_block_trace.argtypes = [vp, i, POINTER(BlockTrace)]
     L.pgmoe_slot_address.argtypes = [vp, i, i, POINTER(vp)]
+    L.pgmoe_route.argtypes = [POINTER(RouterConfig), vp, c_int64, vp, i, vp, vp, vp, vp]
+    L.pgmoe_route_backward.argtypes = [POINTER(RouterConfig), vp, c_int64, vp, vp, vp, i, vp, c_int64, vp]
+    L.pgmoe_group_rows.argtypes = [vp, vp, i, vp, vp, vp]
+    L.pgmoe_quantize_rows.argtypes = [vp, c_int64, i, i, vp, i, POINTER(FP8Rows), vp]
+    L.pgmoe_quantize_weights.argtypes = [vp, i, POINTER(FP8Weights), POINTER(FP8Weights), vp]
+    L.pgmoe_expert_matmul.argtypes = [POINTER(FP8Rows), POINTER(FP8Weights), vp, i, vp, c_int64, i, POINTER(FP8Rows), vp]
     L.pgmoe_ffn_timing_end.argtypes = [vp, POINTER(c_int), POINTER(c_float), POINTER(c_float)]
     for name in EXPORTS:
         if name not in ("pgmoe_last_error", "pgmoe_expert_bytes", "pgmoe_workspace_bytes", "pgmoe_ffn_kernel_name"):
@@ -181,6 +205,146 @@ def unique_experts(idx, n_experts: int):
     return out[:rc].copy()
 
 
+# ---- routing and 8-bit experts: no context; tensors carry their sizes, types and strides
+_DTYPES = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16, "torch.float8_e4m3fn": E4M3, "torch.float8_e5m2": E5M2}
+
+
+def _dtype(t) -> int:
+    code = _DTYPES.get(str(t.dtype))
+    if code is None:
+        raise TypeError(f"no operator of the library takes {t.dtype}")
+    return code
+
+
+def _expect(t, name, shape, dtype, strides=True):
+    """The checks only the tensor allows: the library sees addresses."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if str(t.dtype) not in ((dtype,) if isinstance(dtype, str) else dtype):
+        raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
+    if strides and not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+
+
+def _row_stride(t, name) -> int:
+    """Elements from one row of a matrix to the next; within a row they lie side by side."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} has {t.dim()} dimensions, not 2")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"the elements of a row of {name} do not lie side by side")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+_FLOATS = ("torch.float32", "torch.bfloat16", "torch.float16")
+_FP8 = ("torch.float8_e4m3fn", "torch.float8_e5m2")
+
+
+def fp8_blocks(n: int) -> int:
+    return (n + FP8_BLOCK - 1) // FP8_BLOCK
+
+
+def _fp8_rows(q, scale, cols, name) -> FP8Rows:
+    """q [rows, >= 128 * blocks] codes, scale [blocks, >= rows] float32."""
+    rows = q.shape[0]
+    if str(q.dtype) not in _FP8:
+        raise TypeError(f"{name} has dtype {q.dtype}, not one of {_FP8}")
+    if q.shape[1] < FP8_BLOCK * fp8_blocks(cols):
+        raise ValueError(f"{name} has {q.shape[1]} columns, fewer than the {FP8_BLOCK * fp8_blocks(cols)} of whole blocks")
+    _expect(scale, name + "'s scale", (fp8_blocks(cols), rows), "torch.float32", strides=False)
+    return FP8Rows(q.data_ptr(), _row_stride(q, name), scale.data_ptr(), _row_stride(scale, name + "'s scale"), rows, cols, _dtype(q))
+
+
+def fp8_weight_shapes(n_experts: int, n_in: int, n_out: int):
+    """Shapes of the codes and the scales of n_experts matrices [n_in, n_out]."""
+    return ((n_experts, 8 * fp8_blocks(n_out), fp8_blocks(n_in), 2, 4, 16, 16), (n_experts, fp8_blocks(n_out), fp8_blocks(n_in)))
+
+
+def _fp8_weights(q, scale, n_in, n_out, name) -> FP8Weights:
+    shape, scale_shape = fp8_weight_shapes(q.shape[0], n_in, n_out)
+    _expect(q, name, shape, "torch.float8_e4m3fn")
+    _expect(scale, name + "'s scale", scale_shape, "torch.float32")
+    return FP8Weights(q.data_ptr(), scale.data_ptr(), q.shape[0], n_in, n_out)
+
+
+class Router:
+    """A pgmoe_router: how experts are selected and weighed from logits."""
+
+    def __init__(self, n_experts, top_k, score=SCORE_SOFTMAX, n_groups=1, topk_groups=0, renormalize=False, scale=1.0):
+        self.cfg = RouterConfig(n_experts, top_k, n_groups, topk_groups, score, 1 if renormalize else 0, scale, F32)
+
+    def _outer(self, logits):
+        T, E = logits.shape
+        if E != self.cfg.n_experts:
+            raise ValueError(f"logits of {E} experts, the router has {self.cfg.n_experts}")
+        self.cfg.logits_dtype = _dtype(logits)
+        return T, E
+
+    def route(self, logits, bias, topk_idx, topk_weight, scores_out=None, stream=None):
+        T, E = self._outer(logits)
+        if bias is not None:
+            _expect(bias, "bias", (E,), "torch.float32")
+        _expect(topk_idx, "topk_idx", (T, self.cfg.top_k), "torch.int32")
+        _expect(topk_weight, "topk_weight", (T, self.cfg.top_k), "torch.float32")
+        if scores_out is not None:
+            _expect(scores_out, "scores_out", (T, E), "torch.float32")
+        rc = lib.pgmoe_route(byref(self.cfg), _ptr(logits), _row_stride(logits, "logits"), _ptr(bias), T, _ptr(topk_idx), _ptr(topk_weight),
+                             _ptr(scores_out), _stream(stream))
+        if rc:
+            raise PgmoeError(rc, last_error())
+
+    def route_backward(self, logits, topk_idx, d_weight, d_scores, d_logits, stream=None):
+        T, E = self._outer(logits)
+        _expect(topk_idx, "topk_idx", (T, self.cfg.top_k), "torch.int32")
+        _expect(d_weight, "d_weight", (T, self.cfg.top_k), "torch.float32")
+        if d_scores is not None:
+            _expect(d_scores, "d_scores", (T, E), "torch.float32")
+        _expect(d_logits, "d_logits", (T, E), str(logits.dtype), strides=False)
+        rc = lib.pgmoe_route_backward(byref(self.cfg), _ptr(logits), _row_stride(logits, "logits"), _ptr(topk_idx), _ptr(d_weight), _ptr(d_scores), T,
+                                      _ptr(d_logits), _row_stride(d_logits, "d_logits"), _stream(stream))
+        if rc:
+            raise PgmoeError(rc, last_error())
+
+
+def quantize_rows(x, q, scale, row_of=None, copies=1, stream=None) -> None:
+    """x [T, cols] -> codes q [rows, 128 * blocks] and scales [blocks, rows]; row_of [T * copies] deals the rows out."""
+    out = _fp8_rows(q, scale, x.shape[1], "q")
+    if row_of is not None:
+        _expect(row_of, "row_of", (x.shape[0] * copies,), "torch.int32")
+    rc = lib.pgmoe_quantize_rows(_ptr(x), _row_stride(x, "x"), _dtype(x), x.shape[0], _ptr(row_of), copies, byref(out), _stream(stream))
+    if rc:
+        raise PgmoeError(rc, last_error())
+
+
+def quantize_weights(w, forward_q, forward_scale, backward_q=None, backward_scale=None, stream=None) -> None:
+    """w [E, n_in, n_out] -> the operand tiles and scales (fp8_weight_shapes) of x . W and, if given, of dy . W^T."""
+    E, n_in, n_out = w.shape
+    _expect(w, "w", (E, n_in, n_out), _FLOATS)
+    fwd = None if forward_q is None else _fp8_weights(forward_q, forward_scale, n_in, n_out, "forward_q")
+    bwd = None if backward_q is None else _fp8_weights(backward_q, backward_scale, n_out, n_in, "backward_q")
+    for f in (fwd, bwd):
+        if f is not None and f.n_experts != E:
+            raise ValueError(f"codes of {f.n_experts} experts for {E}")
+    rc = lib.pgmoe_quantize_weights(_ptr(w), _dtype(w), None if fwd is None else byref(fwd), None if bwd is None else byref(bwd), _stream(stream))
+    if rc:
+        raise PgmoeError(rc, last_error())
+
+
+def expert_matmul(x_q, x_scale, w_q, w_scale, expert_offsets, n_in, n_out, y, y_scale=None, relu=False, stream=None) -> None:
+    """y[rows] = act(x[rows] . W_e) for the rows of every expert e; y [rows, n_out], or codes with y_scale."""
+    x = _fp8_rows(x_q, x_scale, n_in, "x_q")
+    w = _fp8_weights(w_q, w_scale, n_in, n_out, "w_q")
+    _expect(expert_offsets, "expert_offsets", (w.n_experts + 1,), "torch.int32")
+    out = None
+    if y_scale is not None:
+        out = _fp8_rows(y, y_scale, n_out, "y")
+    else:
+        _expect(y, "y", (x.rows, n_out), _FLOATS, strides=False)
+    rc = lib.pgmoe_expert_matmul(byref(x), byref(w), _ptr(expert_offsets), 1 if relu else 0, None if out is not None else _ptr(y),
+                                 0 if out is not None else _row_stride(y, "y"), _dtype(y), None if out is None else byref(out), _stream(stream))
+    if rc:
+        raise PgmoeError(rc, last_error())
+
+
 class Context:
     """Owns a pgmoe_ctx*.  Methods take tensors (anything with data_ptr()) or raw addresses."""
 
@@ -243,6 +407,9 @@ class Context:
     def permute(self, x, topk_idx, T, x_perm, row_of, expert_offsets, stream=None):
         self._check(lib.pgmoe_permute(self._h, _ptr(x), _ptr(topk_idx), T, _ptr(x_perm), _ptr(row_of),
                                       _ptr(expert_offsets), _stream(stream)))
+
+    def group_rows(self, topk_idx, T, row_of, expert_offsets, stream=None):
+        self._check(lib.pgmoe_group_rows(self._h, _ptr(topk_idx), T, _ptr(row_of), _ptr(expert_offsets), _stream(stream)))
 
     def expert_ffn(self, block, x_perm, expert_offsets, n_rows, y_perm, workspace, stream=None):
         self._check(lib.pgmoe_expert_ffn(self._h, block, _ptr(x_perm), _ptr(expert_offsets), n_rows, _ptr(y_perm),

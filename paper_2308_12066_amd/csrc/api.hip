@@ -347,15 +347,6 @@ static int check_common(pgmoe_ctx *ctx, const char *fn, int T) {
     return PGMOE_OK;
 }
 
-#define NEED_PTR(ctx, fn, p, a)                                                                        \
-    do {                                                                                               \
-        if (!(p)) return fail(ctx, PGMOE_EINVAL, "%s: %s is NULL", fn, #p);                            \
-        if (!aligned(p, a)) return fail(ctx, PGMOE_EINVAL, "%s: %s is not %d-byte aligned", fn, #p, (int)(a)); \
-    } while (0)
-#define OPT_PTR(ctx, fn, p, a)                                                                         \
-    do {                                                                                               \
-        if ((p) && !aligned(p, a)) return fail(ctx, PGMOE_EINVAL, "%s: %s is not %d-byte aligned", fn, #p, (int)(a)); \
-    } while (0)
 #define NEED_DEVICE(ctx, fn)                                                                           \
     do {                                                                                               \
         if ((ctx)->host_only) return fail(ctx, PGMOE_ENODEVICE, "%s: context is host-only, nothing can be launched", fn); \
@@ -389,6 +380,17 @@ int pgmoe_permute(pgmoe_ctx *ctx, const void *x, const int32_t *topk_idx, int T,
     NEED_PTR(ctx, fn, expert_offsets, 4);
     NEED_DEVICE(ctx, fn);
     return launch_permute(ctx, x, topk_idx, T, x_perm, row_of, expert_offsets, (hipStream_t)stream);
+}
+
+int pgmoe_group_rows(pgmoe_ctx *ctx, const int32_t *topk_idx, int T, int32_t *row_of, int32_t *expert_offsets, void *stream) {
+    const char *fn = "pgmoe_group_rows";
+    int rc = check_common(ctx, fn, T);
+    if (rc) return rc;
+    NEED_PTR(ctx, fn, topk_idx, 4);
+    NEED_PTR(ctx, fn, row_of, 4);
+    NEED_PTR(ctx, fn, expert_offsets, 4);
+    NEED_DEVICE(ctx, fn);
+    return launch_route(ctx, topk_idx, T, row_of, expert_offsets, nullptr, (hipStream_t)stream);
 }
 
 int pgmoe_combine(pgmoe_ctx *ctx, const void *y_perm, const int32_t *row_of, const float *topk_prob,

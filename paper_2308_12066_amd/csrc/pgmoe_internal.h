@@ -132,6 +132,26 @@ int check_config(const pgmoe_config *cfg, char *buf, size_t n);
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Checks of pointer arguments at the entry points.
+#define NEED_PTR(ctx, fn, p, a)                                                                        \
+    do {                                                                                               \
+        if (!(p)) return fail(ctx, PGMOE_EINVAL, "%s: %s is NULL", fn, #p);                            \
+        if (!aligned(p, a)) return fail(ctx, PGMOE_EINVAL, "%s: %s is not %d-byte aligned", fn, #p, (int)(a)); \
+    } while (0)
+#define OPT_PTR(ctx, fn, p, a)                                                                         \
+    do {                                                                                               \
+        if ((p) && !aligned(p, a)) return fail(ctx, PGMOE_EINVAL, "%s: %s is not %d-byte aligned", fn, #p, (int)(a)); \
+    } while (0)
+
+// The context-free operators: bytes of an element, and the status of a launch.
+inline size_t dtype_bytes(int dtype) { return dtype == PGMOE_F32 ? 4 : (dtype == PGMOE_BF16 || dtype == PGMOE_F16 ? 2 : 1); }
+inline int launched(const char *fn) {
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return PGMOE_OK;
+    if (e == hipErrorNoDevice || e == hipErrorInvalidDevice) return fail(nullptr, PGMOE_ENODEVICE, "%s: no HIP device is visible", fn);
+    return hip_fail(nullptr, e, fn);
+}
+
 // A launch with more than 48 KiB of dynamic LDS needs the kernel's limit raised first, once per
 // kernel and device; the context remembers which of its kernels have had that done.
 inline int allow_dynamic_lds(pgmoe_ctx *ctx, const void *kernel, size_t bytes) {

@@ -1,0 +1,532 @@
+// Routing from logits (pgmoe_route) and its gradient (pgmoe_route_backward).
+//
+// A token belongs to 16 lanes, four tokens to a wavefront; lane l of them holds the experts l * PER .. l * PER + PER - 1
+// in registers (PER = experts / 16, rounded up to a power of two).  So a search for the largest value costs PER steps in
+// every lane and four exchanges, for four tokens at once, and the lowest lane that holds it has the lowest index.
+//
+// Selection.  Every expert's value becomes an integer key that orders as the value does, with places below all values for
+// an expert that is unavailable, outside the kept groups, or taken.  What is compared are 32-bit results, whose last bits
+// depend on how exp and the sums were rounded; so the chosen neighbours (and the two groups at the border) are looked at
+// once more, and a token where two of them lie closer than CLOSE is selected again with everything in 64 bits.
+// Values that are equal because logit and bias are equal are no such case: both ways the lowest index wins.
+#include <climits>
+#include <cmath>
+
+#include "pgmoe_internal.h"
+
+namespace pgmoe {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+struct RouteArgs {
+    const void *logits;
+    size_t stride;
+    const float *bias;
+    int T, E, k, n_groups, keep;
+    int renorm;
+    float scale;
+    int32_t *idx;
+    float *weight, *scores;
+};
+
+constexpr int ROUTE_LANES = 16;                                // of one token
+constexpr int ROUTE_THREADS = 256, ROUTE_TOKENS = ROUTE_THREADS / ROUTE_LANES;
+// Two selection values closer than this, relative to the larger of them and 2^-24, are compared in 64 bits: the scores carry
+// a few units of 2^-24 (exp, a sum of up to 256 terms in pairs, a division), the bias and the sum of a group's two one each.
+constexpr float CLOSE = 4e-6f;
+
+// Keys of values: integers in the order of the values, -0 as 0 and NaN as -infinity.
+template <typename V>
+struct Keys;
+template <>
+struct Keys<float> {
+    typedef int32_t T;
+    __device__ static T of(float v) {
+        const int32_t b = __float_as_int(v == v ? v + 0.f : -INFINITY);
+        return b ^ ((b >> 31) & INT_MAX);
+    }
+    __device__ static float value(T k) { return __int_as_float(k ^ ((k >> 31) & INT_MAX)); }
+    static constexpr T lowest = INT_MIN;
+};
+template <>
+struct Keys<double> {
+    typedef int64_t T;
+    __device__ static T of(double v) {
+        const int64_t b = __double_as_longlong(v == v ? v + 0.0 : -(double)INFINITY);
+        return b ^ ((b >> 63) & LLONG_MAX);
+    }
+    static constexpr T lowest = LLONG_MIN;
+};
+// below every value: taken, outside the kept groups, unavailable (in rising order, from Keys::lowest)
+enum { KEY_TAKEN = 0, KEY_OUTSIDE = 1, KEY_UNAVAILABLE = 2 };
+
+template <typename V>
+__device__ inline V lanes_sum(V v) {
+#pragma unroll
+    for (int m = 1; m < ROUTE_LANES; m <<= 1) v += __shfl_xor(v, m);
+    return v;
+}
+template <typename V>
+__device__ inline V lanes_max(V v) {
+#pragma unroll
+    for (int m = 1; m < ROUTE_LANES; m <<= 1) {
+        const V o = __shfl_xor(v, m);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
+// What the lanes of a wavefront wrote to LDS is there for its other lanes behind this (they run in lockstep and LDS
+// operations complete in order: nothing but the compiler has to be held back).
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+__device__ inline bool available(float z) { return z > -INFINITY; }  // false for NaN too
+
+__device__ inline float exp_of(float x) { return expf(x); }
+__device__ inline double exp_of(double x) { return exp(x); }
+// exp(z - m), 1 at the largest of infinite logits
+template <typename V>
+__device__ inline V exp_below(float z, float m) {
+    return z == m ? V(1) : exp_of(V(z) - V(m));
+}
+template <typename V>
+__device__ inline V sigmoid(float z) {
+    return V(1) / (V(1) + exp_of(-V(z)));
+}
+
+template <typename L>
+__device__ inline float logit_at(const RouteArgs &a, size_t t, int e) {
+    return (float)reinterpret_cast<const L *>(a.logits)[t * a.stride + e];
+}
+
+// This lane's logits of token t; unavailable (-infinity) past the last expert.
+template <typename L, int PER>
+__device__ inline void load_logits(const L *row, int E, int first, float (&z)[PER]) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const float v = (float)row[min(first + i, E - 1)];
+        z[i] = first + i < E && available(v) ? v : -INFINITY;
+    }
+}
+
+// Scores of this lane's experts from its logits; m: the token's largest logit.
+template <typename V, bool SIGMOID, int PER>
+__device__ inline void scores_of(const float (&z)[PER], float m, V (&s)[PER]) {
+    if (SIGMOID) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) s[i] = available(z[i]) ? sigmoid<V>(z[i]) : V(0);
+    } else {
+        V sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            s[i] = available(z[i]) ? exp_below<V>(z[i], m) : V(0);
+            sum += s[i];
+        }
+        sum = lanes_sum(sum);
+        const V inv = sum > V(0) ? V(1) / sum : V(0);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) s[i] *= inv;
+    }
+}
+
+// Selects the k experts of one token into chosen[0 .. k).  Returns whether 32 bits may have decided it (V = float only).
+// shared: at least n_experts V of this token, used with groups only.
+template <typename V, bool SIGMOID, int PER>
+__device__ bool select_experts(const RouteArgs &a, const float (&z)[PER], const float (&b)[PER], int first, int lane, float m, V *shared, int32_t *chosen) {
+    typedef typename Keys<V>::T Key;
+    constexpr Key low = Keys<V>::lowest;
+    const bool by_score = a.bias || a.n_groups > 1;
+    bool close = false;
+    Key key[PER];
+    {
+        V v[PER];
+        if (by_score) {
+            scores_of<V, SIGMOID, PER>(z, m, v);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) v[i] += V(b[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            // without a bias by the logit: scores rise with it, and it is exact
+            const Key of = a.bias ? Keys<V>::of(v[i]) : Keys<V>::of(V(z[i]));
+            key[i] = first + i >= a.E ? low + KEY_TAKEN : available(z[i]) ? of : low + KEY_UNAVAILABLE;
+        }
+        if (a.n_groups > 1) {
+            // the group's worth: lane g adds up group g
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (first + i < a.E) shared[first + i] = available(z[i]) ? v[i] : -(V)INFINITY;
+            wave_sync();
+            const int size = a.E / a.n_groups;
+            Key worth = low;
+            V value = -(V)INFINITY;
+            if (lane < a.n_groups) {
+                V one = -(V)INFINITY, two = -(V)INFINITY;
+                for (int j = 0; j < size; ++j) {
+                    const V x = shared[lane * size + j];
+                    two = x > one ? one : (x > two ? x : two);
+                    one = x > one ? x : one;
+                }
+                value = two > -(V)INFINITY ? one + two : one;
+                worth = value > -(V)INFINITY ? Keys<V>::of(value) : low;
+            }
+            // kept: fewer than `keep` groups are worthier, or as worthy and lower
+            int above = 0;
+            for (int g = 0; g < a.n_groups; ++g) {
+                const Key o = __shfl(worth, (threadIdx.x & 48) + g);
+                above += o > worth || (o == worth && g < lane) ? 1 : 0;
+            }
+            const bool kept = lane < a.n_groups && above < a.keep;
+            if (sizeof(V) == 4 && a.keep < a.n_groups) {
+                // the worst kept against the best other
+                const float inside = -lanes_max(kept ? -(float)value : -INFINITY);
+                const float outside = lanes_max(lane < a.n_groups && !kept && worth > low ? (float)value : -INFINITY);
+                close = outside > -INFINITY && !(inside - outside > CLOSE * fmaxf(fabsf(inside), 6e-8f));
+            }
+            const unsigned mask = (unsigned)(__ballot(kept) >> (threadIdx.x & 48)) & 0xffffu;
+            int g = first / size, in_group = first - g * size;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (first + i < a.E && !((mask >> g) & 1)) key[i] = low + KEY_OUTSIDE;
+                if (++in_group == size) {
+                    in_group = 0;
+                    ++g;
+                }
+            }
+        }
+    }
+    // one further than asked for, to compare the last chosen with the first that is not
+    const bool look = sizeof(V) == 4 && a.bias;
+    const int rounds = look ? min(a.k + 1, a.E) : a.k;
+    Key before = 0;
+    float z_before = 0.f, b_before = 0.f;
+    for (int j = 0; j < rounds; ++j) {
+        Key best = key[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) best = key[i] > best ? key[i] : best;
+        const Key top = lanes_max(best);
+        const unsigned holders = (unsigned)(__ballot(best == top) >> (threadIdx.x & 48)) & 0xffffu;
+        const int owner = __ffs(holders) - 1;
+        float z_won = 0.f, b_won = 0.f;
+        if (lane == owner) {
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const bool it = !found && key[i] == top;
+                if (it) {
+                    if (j < a.k) chosen[j] = first + i;
+                    key[i] = low + KEY_TAKEN;
+                    z_won = z[i];
+                    b_won = b[i];
+                }
+                found |= it;
+            }
+        }
+        if (look) {
+            z_won = __shfl(z_won, (threadIdx.x & 48) + owner);
+            b_won = __shfl(b_won, (threadIdx.x & 48) + owner);
+            if (j > 0 && top > low + KEY_UNAVAILABLE && !(z_won == z_before && b_won == b_before)) {
+                const float hi = Keys<float>::value((int32_t)before), lo = Keys<float>::value((int32_t)top);
+                close |= !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f)) && lo > -INFINITY;
+            }
+            before = top;
+            z_before = z_won;
+            b_before = b_won;
+        }
+    }
+    return close;
+}
+
+template <typename L, bool SIGMOID, int PER>
+__global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const RouteArgs a) {
+    extern __shared__ char lds[];
+    const int lane = threadIdx.x & (ROUTE_LANES - 1), token = threadIdx.x / ROUTE_LANES;
+    const size_t t = (size_t)blockIdx.x * ROUTE_TOKENS + token;
+    if (t >= (size_t)a.T) return;  // whole rows of 16 lanes; no workgroup barrier below
+    int32_t *chosen = reinterpret_cast<int32_t *>(lds) + token * a.k;
+    double *shared = reinterpret_cast<double *>(lds + ((ROUTE_TOKENS * a.k * 4 + 15) & ~15)) + (a.n_groups > 1 ? token * a.E : 0);
+    const int first = lane * PER;
+    float z[PER], b[PER];
+    load_logits<L, PER>(reinterpret_cast<const L *>(a.logits) + t * a.stride, a.E, first, z);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const float v = a.bias && first + i < a.E ? a.bias[first + i] : 0.f;
+        b[i] = v == v ? v : -INFINITY;
+    }
+    float m = z[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) m = fmaxf(m, z[i]);
+    m = lanes_max(m);
+
+    if (select_experts<float, SIGMOID, PER>(a, z, b, first, lane, m, reinterpret_cast<float *>(shared), chosen)) {
+        wave_sync();
+        select_experts<double, SIGMOID, PER>(a, z, b, first, lane, m, shared, chosen);
+    }
+    wave_sync();
+
+    float sum = 0.f;  // of exp(z - m) over all experts
+    if (a.scores || (!SIGMOID && !a.renorm)) {
+        float s[PER];
+        if (!SIGMOID) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                s[i] = available(z[i]) ? exp_below<float>(z[i], m) : 0.f;
+                sum += s[i];
+            }
+            sum = lanes_sum(sum);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) s[i] = available(z[i]) ? sigmoid<float>(z[i]) : 0.f;
+        }
+        if (a.scores) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (first + i < a.E) a.scores[t * a.E + first + i] = SIGMOID ? s[i] : (sum > 0.f ? s[i] / sum : 0.f);
+        }
+    }
+    // Weights, lane j the j-th.  Renormalised ones are taken relative to the largest selected logit, so that neither sum nor quotient
+    // underflows where all of them are small: sigmoid(z) = exp(min(z, 0)) / (1 + exp(-|z|)).
+    float top = -INFINITY, total = 0.f;
+    if (a.renorm) {
+        for (int j = lane; j < a.k; j += ROUTE_LANES) {
+            const float zj = logit_at<L>(a, t, chosen[j]);
+            if (available(zj)) top = fmaxf(top, SIGMOID ? fminf(zj, 0.f) : zj);
+        }
+        top = lanes_max(top);
+    }
+    auto part = [&](float zj) {
+        if (!available(zj)) return 0.f;
+        if (SIGMOID) return exp_below<float>(fminf(zj, 0.f), top) / (1.f + exp_of(-fabsf(zj)));
+        return exp_below<float>(zj, top);
+    };
+    if (a.renorm) {
+        for (int j = lane; j < a.k; j += ROUTE_LANES) total += part(logit_at<L>(a, t, chosen[j]));
+        total = lanes_sum(total);
+    }
+    for (int j = lane; j < a.k; j += ROUTE_LANES) {
+        const int e = chosen[j];
+        const float zj = logit_at<L>(a, t, e);
+        float w = 0.f;
+        if (available(zj)) w = a.renorm ? part(zj) / total : SIGMOID ? sigmoid<float>(zj) : exp_below<float>(zj, m) / sum;
+        a.idx[t * a.k + j] = e;
+        a.weight[t * a.k + j] = a.scale * w;
+    }
+}
+
+struct RouteBackwardArgs {
+    const void *logits;
+    size_t stride;
+    const int32_t *idx;
+    const float *d_weight, *d_scores;
+    void *d_logits;
+    size_t d_stride;
+    int T, E, k, renorm;
+    float scale;
+};
+
+// The selected experts' part of the gradient goes through LDS, one float an expert: what lane j works out for the j-th
+// belongs to the lane that holds that expert.  Renormalised, with r_j = s_j / total,
+//   s_j d_s[j] = c r_j (d_w[j] - sum_i d_w[i] r_i),
+// whose sum over j is 0: softmax's common term has nothing of it, and r is taken as in the forward kernel.
+template <typename L, bool SIGMOID, int PER>
+__global__ __launch_bounds__(ROUTE_THREADS) void route_logits_backward_kernel(const RouteBackwardArgs a) {
+    extern __shared__ float parts[];
+    const int lane = threadIdx.x & (ROUTE_LANES - 1), token = threadIdx.x / ROUTE_LANES;
+    const size_t t = (size_t)blockIdx.x * ROUTE_TOKENS + token;
+    if (t >= (size_t)a.T) return;  // whole rows of 16 lanes; no workgroup barrier below
+    float *part = parts + token * ROUTE_LANES * PER;
+    const int first = lane * PER;
+    const L *row = reinterpret_cast<const L *>(a.logits) + t * a.stride;
+    const bool every = a.d_scores || (!SIGMOID && !a.renorm);  // the gradient of every expert needs its score
+    float z[PER], s[PER], m = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        part[first + i] = 0.f;
+        s[i] = 0.f;
+    }
+    if (every) {
+        load_logits<L, PER>(row, a.E, first, z);
+        if (!SIGMOID) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) m = fmaxf(m, z[i]);
+            m = lanes_max(m);
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            s[i] = !available(z[i]) ? 0.f : SIGMOID ? sigmoid<float>(z[i]) : exp_below<float>(z[i], m);
+            sum += s[i];
+        }
+        if (!SIGMOID) {
+            sum = lanes_sum(sum);
+            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) s[i] *= inv;
+        }
+    }
+    // the selected ones: lane j the j-th
+    float top = -INFINITY, total = 0.f, dot = 0.f;
+    auto logit_of = [&](int j, int &e) {
+        e = a.idx[t * a.k + j];
+        const float zj = e >= 0 && e < a.E ? (float)row[e] : -INFINITY;
+        return available(zj) ? zj : -INFINITY;
+    };
+    auto ratio = [&](float zj) {  // s_j, up to a factor common to the token's
+        if (!available(zj)) return 0.f;
+        if (SIGMOID) return exp_below<float>(fminf(zj, 0.f), top) / (1.f + exp_of(-fabsf(zj)));
+        return exp_below<float>(zj, top);
+    };
+    int e;
+    if (a.renorm) {
+        for (int j = lane; j < a.k; j += ROUTE_LANES) {
+            const float zj = logit_of(j, e);
+            top = fmaxf(top, SIGMOID ? fminf(zj, 0.f) : zj);
+        }
+        top = lanes_max(top);
+        for (int j = lane; j < a.k; j += ROUTE_LANES) {
+            const float r = ratio(logit_of(j, e));
+            total += r;
+            dot += r == 0.f ? 0.f : r * a.d_weight[t * a.k + j];
+        }
+        total = lanes_sum(total);
+        dot = lanes_sum(dot) / total;
+    }
+    float common = 0.f;  // softmax: sum of s d_s
+    wave_sync();
+    for (int j = lane; j < a.k; j += ROUTE_LANES) {
+        const float zj = logit_of(j, e);
+        if (!available(zj)) continue;
+        const float g = a.d_weight[t * a.k + j];
+        float d;  // s_j times the part of d_s[j] that comes through the weights
+        if (a.renorm) d = ratio(zj) / total * (g - dot);
+        else d = (SIGMOID ? sigmoid<float>(zj) : exp_below<float>(zj, m) / sum) * g;
+        d *= a.scale;
+        if (SIGMOID) d *= sigmoid<float>(-zj);
+        else if (!a.renorm) common += d;
+        atomicAdd(&part[e], d);
+    }
+    float ds[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        ds[i] = a.d_scores && s[i] > 0.f ? a.d_scores[t * a.E + first + i] : 0.f;
+        if (!SIGMOID) common += s[i] * ds[i];
+    }
+    if (!SIGMOID && every) common = lanes_sum(common);
+    wave_sync();
+    L *out = reinterpret_cast<L *>(a.d_logits) + t * a.d_stride;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        float d = part[first + i];
+        if (every && s[i] > 0.f) d += SIGMOID ? s[i] * sigmoid<float>(-z[i]) * ds[i] : s[i] * (ds[i] - common);
+        if (first + i < a.E) out[first + i] = (L)d;
+    }
+}
+
+static int check_router(const pgmoe_router *r, const char *fn) {
+    if (!r) return fail(nullptr, PGMOE_EINVAL, "%s: router is NULL", fn);
+    if (r->n_experts < 1 || r->n_experts > PGMOE_MAX_EXPERTS)
+        return fail(nullptr, PGMOE_EINVAL, "%s: n_experts=%d outside 1..%d", fn, r->n_experts, PGMOE_MAX_EXPERTS);
+    const int groups = r->n_groups ? r->n_groups : 1, keep = r->topk_groups ? r->topk_groups : groups;
+    if (groups < 1 || groups > PGMOE_MAX_GROUPS || r->n_experts % groups)
+        return fail(nullptr, PGMOE_EINVAL, "%s: n_groups=%d is no divisor of n_experts=%d in 1..%d", fn, groups, r->n_experts, PGMOE_MAX_GROUPS);
+    if (keep < 1 || keep > groups) return fail(nullptr, PGMOE_EINVAL, "%s: topk_groups=%d outside 1..n_groups=%d", fn, keep, groups);
+    if (r->top_k < 1 || r->top_k > r->n_experts / groups * keep)
+        return fail(nullptr, PGMOE_EINVAL, "%s: top_k=%d outside 1..%d, the experts of the kept groups", fn, r->top_k, r->n_experts / groups * keep);
+    if (r->score != PGMOE_SCORE_SOFTMAX && r->score != PGMOE_SCORE_SIGMOID) return fail(nullptr, PGMOE_EINVAL, "%s: score=%d unknown", fn, r->score);
+    if (r->renormalize != 0 && r->renormalize != 1) return fail(nullptr, PGMOE_EINVAL, "%s: renormalize=%d is neither 0 nor 1", fn, r->renormalize);
+    if (!std::isfinite(r->scale)) return fail(nullptr, PGMOE_EINVAL, "%s: scale is not finite", fn);
+    if (r->logits_dtype != PGMOE_F32 && r->logits_dtype != PGMOE_BF16 && r->logits_dtype != PGMOE_F16)
+        return fail(nullptr, PGMOE_EINVAL, "%s: logits_dtype=%d is neither f32 nor bf16 nor f16", fn, r->logits_dtype);
+    return PGMOE_OK;
+}
+
+// The instantiation for a type of logits, a score and a number of experts: KERNEL<L, SIGMOID, PER>.
+#define ROUTE_LAUNCH_PER(KERNEL, L, SIG, PER, ...)                     \
+    do {                                                               \
+        constexpr int per_ = PER;                                      \
+        hipLaunchKernelGGL((KERNEL<L, SIG, per_>), __VA_ARGS__);       \
+    } while (0)
+#define ROUTE_LAUNCH_E(KERNEL, L, SIG, E, ...)                                          \
+    do {                                                                                \
+        if ((E) <= 16) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 1, __VA_ARGS__);                \
+        else if ((E) <= 32) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 2, __VA_ARGS__);           \
+        else if ((E) <= 64) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 4, __VA_ARGS__);           \
+        else if ((E) <= 128) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 8, __VA_ARGS__);          \
+        else ROUTE_LAUNCH_PER(KERNEL, L, SIG, 16, __VA_ARGS__);                         \
+    } while (0)
+#define ROUTE_LAUNCH(KERNEL, r, ...)                                                                     \
+    do {                                                                                                 \
+        const bool sig_ = (r)->score == PGMOE_SCORE_SIGMOID;                                             \
+        if ((r)->logits_dtype == PGMOE_F32) {                                                            \
+            if (sig_) ROUTE_LAUNCH_E(KERNEL, float, true, (r)->n_experts, __VA_ARGS__);                  \
+            else ROUTE_LAUNCH_E(KERNEL, float, false, (r)->n_experts, __VA_ARGS__);                      \
+        } else if ((r)->logits_dtype == PGMOE_BF16) {                                                    \
+            if (sig_) ROUTE_LAUNCH_E(KERNEL, __bf16, true, (r)->n_experts, __VA_ARGS__);                 \
+            else ROUTE_LAUNCH_E(KERNEL, __bf16, false, (r)->n_experts, __VA_ARGS__);                     \
+        } else {                                                                                         \
+            if (sig_) ROUTE_LAUNCH_E(KERNEL, _Float16, true, (r)->n_experts, __VA_ARGS__);               \
+            else ROUTE_LAUNCH_E(KERNEL, _Float16, false, (r)->n_experts, __VA_ARGS__);                   \
+        }                                                                                                \
+    } while (0)
+
+}  // namespace pgmoe
+
+using namespace pgmoe;
+
+extern "C" {
+
+int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_stride, const float *bias, int T,
+                int32_t *topk_idx, float *topk_weight, float *scores_out, void *stream) {
+    const char *fn = "pgmoe_route";
+    const int rc = check_router(router, fn);
+    if (rc) return rc;
+    if (T < 0) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d is negative", fn, T);
+    if (logits_stride < router->n_experts) return fail(nullptr, PGMOE_EINVAL, "%s: logits_stride=%lld is less than n_experts=%d", fn, (long long)logits_stride, router->n_experts);
+    if (T == 0) return PGMOE_OK;
+    const size_t elem = dtype_bytes(router->logits_dtype);
+    NEED_PTR(nullptr, fn, logits, elem);
+    OPT_PTR(nullptr, fn, bias, 4);
+    NEED_PTR(nullptr, fn, topk_idx, 4);
+    NEED_PTR(nullptr, fn, topk_weight, 4);
+    OPT_PTR(nullptr, fn, scores_out, 4);
+    const int groups = router->n_groups ? router->n_groups : 1, keep = router->topk_groups ? router->topk_groups : groups;
+    const RouteArgs a = {logits, (size_t)logits_stride, bias, T, router->n_experts, router->top_k, groups, keep, router->renormalize,
+                         router->scale, topk_idx, topk_weight, scores_out};
+    // at most 16 tokens x (256 indices of 4 bytes + 256 values of 8) = 48 KiB
+    const size_t lds = ((ROUTE_TOKENS * a.k * 4 + 15) & ~15) + (groups > 1 ? (size_t)ROUTE_TOKENS * a.E * 8 : 0);
+    const dim3 grid((T + ROUTE_TOKENS - 1) / ROUTE_TOKENS), block(ROUTE_THREADS);
+    ROUTE_LAUNCH(route_logits_kernel, router, grid, block, lds, (hipStream_t)stream, a);
+    return launched(fn);
+}
+
+int pgmoe_route_backward(const pgmoe_router *router, const void *logits, int64_t logits_stride, const int32_t *topk_idx,
+                         const float *d_weight, const float *d_scores, int T, void *d_logits, int64_t d_logits_stride, void *stream) {
+    const char *fn = "pgmoe_route_backward";
+    const int rc = check_router(router, fn);
+    if (rc) return rc;
+    if (T < 0) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d is negative", fn, T);
+    if (logits_stride < router->n_experts || d_logits_stride < router->n_experts)
+        return fail(nullptr, PGMOE_EINVAL, "%s: a stride (%lld, %lld) is less than n_experts=%d", fn, (long long)logits_stride, (long long)d_logits_stride, router->n_experts);
+    if (T == 0) return PGMOE_OK;
+    const size_t elem = dtype_bytes(router->logits_dtype);
+    NEED_PTR(nullptr, fn, logits, elem);
+    NEED_PTR(nullptr, fn, topk_idx, 4);
+    NEED_PTR(nullptr, fn, d_weight, 4);
+    OPT_PTR(nullptr, fn, d_scores, 4);
+    NEED_PTR(nullptr, fn, d_logits, elem);
+    const char *a0 = (const char *)logits, *b0 = (const char *)d_logits;
+    const char *a1 = a0 + ((T - 1) * logits_stride + router->n_experts) * elem, *b1 = b0 + ((T - 1) * d_logits_stride + router->n_experts) * elem;
+    if (a0 < b1 && b0 < a1) return fail(nullptr, PGMOE_EINVAL, "%s: d_logits overlaps logits", fn);
+    const RouteBackwardArgs a = {logits, (size_t)logits_stride, topk_idx, d_weight, d_scores, d_logits, (size_t)d_logits_stride,
+                                 T, router->n_experts, router->top_k, router->renormalize, router->scale};
+    int per = 1;
+    while (per * ROUTE_LANES < a.E) per *= 2;
+    const size_t lds = (size_t)ROUTE_THREADS * per * 4;  // at most 16 KiB
+    const dim3 grid((T + ROUTE_TOKENS - 1) / ROUTE_TOKENS), block(ROUTE_THREADS);
+    ROUTE_LAUNCH(route_logits_backward_kernel, router, grid, block, lds, (hipStream_t)stream, a);
+    return launched(fn);
+}
+
+}  // extern "C"
