@@ -10,6 +10,8 @@
 // results may be off, and more than scales of the next blocks should be.
 // The weights are the first operand, so that a lane's four results belong to one row: one product of the two scales serves
 // them all, and they are neighbours in y.
+#include <atomic>
+
 #include "ffn_common.h"
 #include "fp8.h"
 
@@ -64,11 +66,45 @@ __device__ inline floatx4 product(const Operand &w, const Operand &x) {
     return p;
 }
 
-// The rows of chunk number `chunk`, clamped to the rows there are whatever the offsets say.
-__device__ inline ChunkInfo matmul_chunk(const MatmulArgs &a, int rows_per_chunk, int chunk) {
-    ChunkInfo ci = find_chunk(a.offsets, a.E, rows_per_chunk, chunk);
-    if (ci.row0 < 0 || ci.row0 >= a.rows) ci.nrows = 0;
-    ci.nrows = min(ci.nrows, a.rows - ci.row0);
+// Which rows of which expert are chunk number `chunk`, the chunks of an expert being its rows dealt evenly, in whole 16s,
+// to as few chunks of at most MOST rows as hold them.  Offsets are clamped to the rows there are, whatever they say.  All
+// offsets are loaded at once (four experts a lane).
+struct MatmulChunk {
+    int expert, row0, nrows;  // nrows == 0: there is no such chunk
+};
+template <int MOST>
+__device__ inline MatmulChunk matmul_chunk(const MatmulArgs &a, int chunk) {
+    const int lane = threadIdx.x & 63;
+    int lo[4], n[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        lo[q] = n[q] = 0;
+        if (q * 64 < a.E) {  // uniform
+            const int e = q * 64 + lane;
+            lo[q] = a.offsets[min(e, a.E)];
+            n[q] = a.offsets[min(e + 1, a.E)];
+        }
+    }
+    MatmulChunk ci = {0, 0, 0};
+    int before = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (q * 64 >= a.E) break;
+        lo[q] = max(0, min(lo[q], a.rows));
+        n[q] = max(lo[q], min(n[q], a.rows)) - lo[q];
+        const int c = (n[q] + MOST - 1) / MOST, c_incl = before + wave_incl_scan(c);
+        const unsigned long long hit = __ballot(chunk >= c_incl - c && chunk < c_incl);
+        if (hit) {
+            const int src = __ffsll((long long)hit) - 1;  // uniform: read that lane's values directly
+            const int rows = __builtin_amdgcn_readlane(n[q], src), chunks = (rows + MOST - 1) / MOST;
+            const int each = ((rows + chunks - 1) / chunks + 15) & ~15, k = chunk - __builtin_amdgcn_readlane(c_incl - c, src);
+            ci.expert = q * 64 + src;
+            ci.row0 = __builtin_amdgcn_readlane(lo[q], src) + k * each;
+            ci.nrows = min(each, rows - k * each);
+            return ci;
+        }
+        before = __builtin_amdgcn_readlane(c_incl, 63);
+    }
     return ci;
 }
 
@@ -86,6 +122,8 @@ __device__ inline void store_four(const MatmulArgs &a, int r, int o, floatx4 v) 
     }
 }
 
+__device__ inline float relu_of(float v) { return v > 0.f || v != v ? v : 0.f; }  // NaN stays
+
 // Few rows an expert.  A workgroup takes 16 rows and one block of 128 outputs, a wavefront 16 of them, operands straight from
 // memory into registers.  Y = void: quantised again, YQ.
 constexpr int FEW_THREADS = 512;
@@ -93,7 +131,7 @@ template <int XQ, typename Y, int YQ, bool VEC>
 __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const MatmulArgs a) {
     __shared__ float amax_of[8][16];
     const int chunk = blockIdx.x / a.NB, nb = blockIdx.x - chunk * a.NB;
-    const ChunkInfo ci = matmul_chunk(a, 16, chunk);
+    const MatmulChunk ci = matmul_chunk<16>(a, chunk);
     if (ci.nrows <= 0) return;  // uniform over the workgroup
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int row = ci.row0 + min(lane & 15, ci.nrows - 1), piece = (lane >> 4) * 16;
@@ -114,7 +152,7 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
     }
     if (a.relu) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = acc[i] > 0.f || acc[i] != acc[i] ? acc[i] : 0.f;
+        for (int i = 0; i < 4; ++i) acc[i] = relu_of(acc[i]);
     }
     const bool live = (lane & 15) < ci.nrows;
     const int o = nb * FP8_BLOCK + wave * 16 + 4 * (lane >> 4);
@@ -138,20 +176,231 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
     }
 }
 
+// Many rows an expert.  A workgroup takes up to TM * 64 rows of one expert and 256 outputs; both operands go straight from memory
+// into a ring of NS stages in LDS, a stage being one block of 128 inputs, its scales among them.  Eight wavefronts as 2 x 4:
+// wavefront (wn, wm) has 128 outputs (one scale) and the row tiles wm, wm + 4, ..
+//
+// LDS, a stage: 16 weight tiles of 2 KiB, 64 bytes more behind every second; rows of 128 bytes whose 16-byte pieces are
+// exchanged among themselves, piece c of row r at place c ^ (r / 2 % 8); 256 bytes of scales from each wavefront (rows: the
+// first four; weights: the fifth's first two).  Both operands are then read without bank conflicts.
+//
+// The outputs are dealt to the matrix instruction's 16 rows so that a lane ends with 32 neighbouring outputs: row i of the a-th product
+// is output 32 * (i / 4) + 4 * a + i % 4 of the wavefront's 128, and a lane's four results of a product are rows 4 * (lane / 16) ..
+template <int TM>
+struct MatmulRing {
+    static constexpr int W = 16 * FP8_TILE + 8 * 64, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
+    static constexpr int NS = TM == 4 ? 2 : 3, BYTES = NS * STAGE, LOADS = 4 + TM + 1;
+};
+constexpr int TILE_THREADS = 512;
+
+struct MatmulTile {  // uniform
+    const uint8_t *w, *x;        // the expert's tiles of the first output block; the chunk's first row
+    const float *sw, *sx;
+    size_t x_stride, sx_stride;  // bytes; floats
+    int KB, nrows, tiles;        // tiles: weight tiles there are from w on (16, or 8 past the last whole pair of blocks)
+};
+
+template <int XQ, int TM, int MC>
+__device__ inline void matmul_k_loop(const MatmulTile &t, char *ring, int wave, floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
+    typedef MatmulRing<TM> R;
+    const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
+    const unsigned lds = __builtin_amdgcn_readfirstlane(lds_address(ring));
+    const uint8_t *w_src[4];
+    unsigned w_to[4], x_off[TM];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int tile = wave * 2 + (i >> 1), from = min(tile, t.tiles - 1);
+        w_src[i] = t.w + (size_t)from * t.KB * FP8_TILE + (i & 1) * 1024;
+        w_to[i] = lds + tile * FP8_TILE + (tile >> 1) * 64 + (i & 1) * 1024;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int row = (wave * TM + i) * 8 + (lane >> 3);
+        x_off[i] = (unsigned)min(row, t.nrows - 1) * (unsigned)t.x_stride + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+    }
+    const unsigned x_to = lds + R::W + wave * TM * 1024, s_to = lds + R::W + R::X + wave * 256;
+    const float *s_src = wave < 4 ? t.sx : t.sw;
+    const size_t s_step = wave < 4 ? t.sx_stride : 1;
+    const unsigned s_off = 4u * (wave < 4 ? (unsigned)min(wave * 64 + lane, t.nrows - 1) : (unsigned)((lane & 1) && t.tiles > 8 ? t.KB : 0));
+    const uint8_t *x_src = t.x;
+    auto request = [&](unsigned stage) {  // of the next block of inputs
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            load_tile_to_lds((const char *)w_src[i], lane * 16, w_to[i] + stage);
+            w_src[i] += FP8_TILE;
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) load_tile_to_lds((const char *)x_src, x_off[i], x_to + i * 1024 + stage);
+        x_src += FP8_BLOCK;
+        load_dwords_to_lds(s_src, s_off, s_to + stage);
+        s_src += s_step;
+    };
+#pragma unroll
+    for (int st = 0; st < R::NS; ++st)
+        if (st < t.KB) request(st * R::STAGE);
+
+    const int g = lane >> 4, i16 = lane & 15;
+    const char *w_at = ring + (wn * 8 + 2 * (i16 >> 2)) * FP8_TILE + (wn * 4 + (i16 >> 2)) * 64 + g * 256 + (i16 & 3) * 16;
+    const char *x_at = ring + R::W + (wm * 16 + i16) * FP8_BLOCK;
+    const int x_low = (g ^ (i16 >> 1)) << 4, x_high = ((4 + g) ^ (i16 >> 1)) << 4;
+    const char *s_at = ring + R::W + R::X;
+    unsigned stage = 0;
+    for (int kb = 0; kb < t.KB; ++kb) {
+        // this block's loads have landed: those of at most NS - 1 later ones are outstanding
+        const int later = t.KB - 1 - kb;
+        if (later >= R::NS - 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS * (R::NS - 1)) : "memory");
+        else if (R::NS > 2 && later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_barrier" ::: "memory");
+        if (MC > 0) {
+            Operand x[MC > 0 ? MC : 1];
+            float s[MC > 0 ? MC : 1];
+            const float sw = *reinterpret_cast<const float *>(s_at + stage + 4 * 256 + wn * 4);
+#pragma unroll
+            for (int m = 0; m < MC; ++m) {
+                const char *r = x_at + stage + m * 64 * FP8_BLOCK;
+                x[m] = operand<XQ>(*reinterpret_cast<const intx4 *>(r + x_low), *reinterpret_cast<const intx4 *>(r + x_high));
+                s[m] = sw * *reinterpret_cast<const float *>(s_at + stage + ((wm + 4 * m) * 16 + i16) * 4);
+            }
+            // one output tile's codes are read while the one before is multiplied; nothing may move further ahead, for want of registers
+            intx4 low = *reinterpret_cast<const intx4 *>(w_at + stage), high = *reinterpret_cast<const intx4 *>(w_at + stage + 1024);
+#pragma unroll
+            for (int a = 0; a < 8; ++a) {
+                __builtin_amdgcn_sched_barrier(0);
+                const Operand w = operand<PGMOE_E4M3>(low, high);
+                if (a < 7) {
+                    const char *c = w_at + stage + ((a + 1) >> 2) * FP8_TILE + ((a + 1) & 3) * 64;
+                    low = *reinterpret_cast<const intx4 *>(c);
+                    high = *reinterpret_cast<const intx4 *>(c + 1024);
+                }
+                floatx4 p[MC > 0 ? MC : 1];
+#pragma unroll
+                for (int m = 0; m < MC; ++m) p[m] = product(w, x[m]);
+#pragma unroll
+                for (int m = 0; m < MC; ++m)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[a][m][v] = fmaf(s[m], p[m][v], acc[a][m][v]);
+#pragma unroll
+                for (int m = 0; m < MC; ++m) asm volatile("" : "+v"(acc[a][m]));  // here, not behind the loop's last branch with every p alive
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (kb + R::NS < t.KB) {
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // everyone has read this stage
+            request(stage);
+        }
+        stage = stage + R::STAGE == R::BYTES ? 0 : stage + R::STAGE;
+    }
+}
+
+template <int XQ, typename Y, int YQ, bool VEC, int TM, int MC>
+__device__ inline void matmul_tile_body(const MatmulArgs &a, const MatmulTile &t, char *ring, int wave, int row0, int nb) {
+    floatx4 acc[8][MC > 0 ? MC : 1];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int m = 0; m < MC; ++m) acc[i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+    matmul_k_loop<XQ, TM, MC>(t, ring, wave, acc);
+    const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
+    const int block = nb + wn, o = block * FP8_BLOCK + 32 * (lane >> 4);
+    if (block >= a.NB) return;
+#pragma unroll
+    for (int m = 0; m < MC; ++m) {
+        const int in_chunk = (wm + 4 * m) * 16 + (lane & 15), row = row0 + in_chunk;
+        const bool live = in_chunk < t.nrows;
+        if (a.relu) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][m][v] = relu_of(acc[i][m][v]);
+        }
+        if constexpr (std::is_void<Y>::value) {
+            float amax = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) amax = fmaxf(amax, finite_magnitude(acc[i][m][v]));
+            amax = fmaxf(amax, __shfl_xor(amax, 16));
+            amax = fmaxf(amax, __shfl_xor(amax, 32));
+            const float scale = fp8_scale<YQ>(amax);
+            if (live) {
+                uint32_t codes[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) codes[i] = fp8_pack<YQ>(acc[i][m][0] / scale, acc[i][m][1] / scale, acc[i][m][2] / scale, acc[i][m][3] / scale);
+                uint4 *q = reinterpret_cast<uint4 *>(a.y_q + (size_t)row * a.y_q_stride + o);
+                q[0] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+                q[1] = make_uint4(codes[4], codes[5], codes[6], codes[7]);
+                if (lane < 16) a.y_scale[(size_t)block * a.y_scale_stride + row] = scale;
+            }
+        } else if (live) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) store_four<Y, VEC>(a, row, o + 4 * i, acc[i][m]);
+        }
+    }
+}
+
+template <int XQ, typename Y, int YQ, bool VEC, int TM>
+__global__ __launch_bounds__(TILE_THREADS, 2) void matmul_tiles_kernel(const MatmulArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char ring[];
+    // column blocks of a chunk go to one XCD (workgroups are dealt to the eight in turn) and share its rows there
+    const int cols = (a.NB + 1) / 2, turn = blockIdx.x >> 3, chunk = turn / cols * 8 + (blockIdx.x & 7), nb = (turn - turn / cols * cols) * 2;
+    const MatmulChunk ci = matmul_chunk<TM * 64>(a, chunk);
+    if (ci.nrows <= 0) return;  // uniform over the workgroup
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const size_t block = (size_t)ci.expert * a.NB + nb;
+    const MatmulTile t = {a.w + block * 8 * a.KB * FP8_TILE, a.x + (size_t)ci.row0 * a.x_stride, a.w_scale + block * a.KB, a.x_scale + ci.row0,
+                          a.x_stride, a.x_scale_stride, a.KB, ci.nrows, nb + 1 < a.NB ? 16 : 8};
+    const int rt = (ci.nrows + 15) >> 4, own = max(0, (rt - (wave >> 1) + 3) >> 2);
+    switch (own) {  // uniform over the wavefront
+#define PG_BODY(MC_)                                                                                              \
+    case MC_:                                                                                                     \
+        if constexpr (MC_ <= TM) matmul_tile_body<XQ, Y, YQ, VEC, TM, MC_>(a, t, ring, wave, ci.row0, nb);         \
+        asm volatile("; %0 row tiles" ::"n"(MC_)); /* keeps the bodies' stores apart */                            \
+        return;
+        PG_BODY(0) PG_BODY(1) PG_BODY(2) PG_BODY(3) PG_BODY(4)
+#undef PG_BODY
+    }
+}
+
+constexpr int64_t TILE_STRIDE_MAX = 1 << 23;  // bytes: offsets within a chunk of 256 rows have 31 bits
+
+template <int XQ, typename Y, int YQ, bool VEC, int TM>
+static int launch_tiles(const MatmulArgs &a, hipStream_t s) {
+    // more than 48 KiB of LDS: the kernel's limit is raised once per device
+    static std::atomic<uint64_t> raised{0};
+    int device = 0;
+    if (const hipError_t e = hipGetDevice(&device)) return e == hipErrorNoDevice ? fail(nullptr, PGMOE_ENODEVICE, "pgmoe_expert_matmul: no HIP device is visible") : hip_fail(nullptr, e, "hipGetDevice");
+    if (!(raised.load(std::memory_order_relaxed) >> (device & 63) & 1)) {
+        const void *kernel = reinterpret_cast<const void *>(&matmul_tiles_kernel<XQ, Y, YQ, VEC, TM>);
+        PG_HIP(nullptr, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, MatmulRing<TM>::BYTES));
+        raised.fetch_or(1ull << (device & 63), std::memory_order_relaxed);
+    }
+    // chunks: sum over the experts of ceil(rows / (TM * 64)), in whole eights
+    const int64_t chunks = ((a.rows + (int64_t)(TM * 64 - 1) * std::min(a.E, a.rows)) / (TM * 64) + 7) & ~(int64_t)7;
+    hipLaunchKernelGGL((matmul_tiles_kernel<XQ, Y, YQ, VEC, TM>), dim3((unsigned)(chunks * ((a.NB + 1) / 2))), dim3(TILE_THREADS), MatmulRing<TM>::BYTES, s, a);
+    return PGMOE_OK;
+}
 template <int XQ, typename Y, int YQ, bool VEC>
-static void launch_matmul(const MatmulArgs &a, hipStream_t s) {
+static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
+    const int mean = a.rows / std::min(a.E, a.rows);  // rows an expert
+    if (mean > 16 && (int64_t)a.x_stride < TILE_STRIDE_MAX) {
+        if (mean > 128) return launch_tiles<XQ, Y, YQ, VEC, 4>(a, s);
+        if (mean > 64) return launch_tiles<XQ, Y, YQ, VEC, 2>(a, s);
+        return launch_tiles<XQ, Y, YQ, VEC, 1>(a, s);
+    }
     // chunks: sum over the experts of ceil(rows / 16)
     const int64_t chunks = (a.rows + (int64_t)15 * std::min(a.E, a.rows)) / 16;
     hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC>), dim3((unsigned)(chunks * a.NB)), dim3(FEW_THREADS), 0, s, a);
+    return PGMOE_OK;
 }
 template <int XQ, typename Y>
-static void launch_matmul_to(const MatmulArgs &a, hipStream_t s) {
+static int launch_matmul_to(const MatmulArgs &a, hipStream_t s) {
     // whole fours of outputs, each at an address that four results' bytes divide
-    if (a.n_out % 4 == 0 && a.y_stride % 4 == 0 && aligned(a.y, 4 * sizeof(Y))) launch_matmul<XQ, Y, 0, true>(a, s);
-    else launch_matmul<XQ, Y, 0, false>(a, s);
+    if (a.n_out % 4 == 0 && a.y_stride % 4 == 0 && aligned(a.y, 4 * sizeof(Y))) return launch_matmul<XQ, Y, 0, true>(a, s);
+    return launch_matmul<XQ, Y, 0, false>(a, s);
 }
 template <int XQ>
-static void launch_matmul(const MatmulArgs &a, int y_dtype, hipStream_t s) {
+static int launch_matmul(const MatmulArgs &a, int y_dtype, hipStream_t s) {
     switch (y_dtype) {
     case PGMOE_F32: return launch_matmul_to<XQ, float>(a, s);
     case PGMOE_BF16: return launch_matmul_to<XQ, __bf16>(a, s);
@@ -212,7 +461,6 @@ extern "C" int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weig
         a.y_scale_stride = (size_t)y_q->scale_stride;
         y_dtype = y_q->dtype;
     }
-    if (x->dtype == PGMOE_E4M3) launch_matmul<PGMOE_E4M3>(a, y_dtype, (hipStream_t)stream);
-    else launch_matmul<PGMOE_E5M2>(a, y_dtype, (hipStream_t)stream);
-    return launched(fn);
+    rc = x->dtype == PGMOE_E4M3 ? launch_matmul<PGMOE_E4M3>(a, y_dtype, (hipStream_t)stream) : launch_matmul<PGMOE_E5M2>(a, y_dtype, (hipStream_t)stream);
+    return rc ? rc : launched(fn);
 }

@@ -75,6 +75,20 @@ __device__ inline void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Loads straight from memory into LDS, issued from inline assembly so that the compiler does not wait for them: the kernel
+// counts its own (they complete in order).  M0 (the LDS base; a lane's bytes land behind it in lane order) is written
+// inside the statement, one instruction before the load.
+__device__ inline unsigned lds_address(const void *p) {
+    return (unsigned)(size_t)(__attribute__((address_space(3))) const char *)p;
+}
+__device__ inline void load_tile_to_lds(const char *src, unsigned lane_off, unsigned lds_tile) {  // src: uniform; lane_off: 16 bytes a lane
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(src), "s"(lds_tile) : "memory", "m0");
+}
+
+__device__ inline void load_dwords_to_lds(const void *src, unsigned lane_off, unsigned lds) {  // four bytes a lane
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_off), "s"(src), "s"(lds) : "memory", "m0");
+}
+
 // ---- host side, defined in ffn.hip
 // Bytes of the float32 partial sums of a fused or decode-sized launch of n_rows rows.
 size_t ffn_partial_bytes(const pgmoe_config &c, int n_rows);

@@ -225,14 +225,7 @@ __global__ __launch_bounds__(512) void ffn_gemm_pack_rows_kernel(
 // complete in order) and waits with explicit s_waitcnt vmcnt.  M0 (the LDS base of such a load)
 // is written inside the statement; nothing else in this kernel keeps a value in M0.  The hardware needs one wait
 // state between a scalar write of M0 and a direct-to-LDS load (without it the tile may land at the address of the load
-// before); the compiler inserts it behind its own writes only, so the statement carries it.
-__device__ inline unsigned lds_address(const void *p) {
-    return (unsigned)(size_t)(__attribute__((address_space(3))) const char *)p;
-}
-__device__ inline void load_tile_to_lds(const char *src, unsigned lane_off, unsigned lds_tile) {  // src: uniform; lane_off: 16 bytes a lane
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(src), "s"(lds_tile) : "memory", "m0");
-}
-
+// before); the compiler inserts it behind its own writes only, so the statement (load_tile_to_lds, ffn_common.h) carries it.
 // What a workgroup of the tile kernel works on (all uniform).
 struct GemmTile {
     const char *a;   // the chunk's packed operand tiles of the first k-tile: [n_kt][rt][1 KiB]
