@@ -166,19 +166,21 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) amax = fmaxf(amax, amax_of[i][lane & 15]);
-        const float scale = fp8_scale<YQ>(amax);
+        const Fp8Divisor by = fp8_divisor<YQ>(amax);
         if (live) {
-            *reinterpret_cast<uint32_t *>(a.y_q + (size_t)row * a.y_q_stride + o) = fp8_pack<YQ>(acc[0] / scale, acc[1] / scale, acc[2] / scale, acc[3] / scale);
-            if (wave == 0 && lane < 16) a.y_scale[(size_t)nb * a.y_scale_stride + row] = scale;
+            *reinterpret_cast<uint32_t *>(a.y_q + (size_t)row * a.y_q_stride + o) = fp8_pack<YQ>(by(acc[0]), by(acc[1]), by(acc[2]), by(acc[3]));
+            if (wave == 0 && lane < 16) a.y_scale[(size_t)nb * a.y_scale_stride + row] = by.scale;
         }
     } else {
         if (live) store_four<Y, VEC>(a, row, o, acc);
     }
 }
 
-// Many rows an expert.  A workgroup takes up to TM * 64 rows of one expert and 256 outputs; both operands go straight from memory
-// into a ring of NS stages in LDS, a stage being one block of 128 inputs, its scales among them.  Eight wavefronts as 2 x 4:
-// wavefront (wn, wm) has 128 outputs (one scale) and the row tiles wm, wm + 4, ..
+// Many rows an expert.  An item is up to TM * 64 rows of one expert and 256 outputs; a workgroup, one per CU, takes every
+// gridDim-th of them.  Both operands go straight from memory into a ring of NS stages in LDS, a stage being one block of 128
+// inputs, its scales among them; the requests run ahead of the products without regard to where an item ends, so the first
+// stages of an item arrive, and the results of the one before leave, under products.  Eight wavefronts as 2 x 4: wavefront
+// (wn, wm) has 128 outputs (one scale) and the row tiles wm, wm + 4, ..
 //
 // LDS, a stage: 16 weight tiles of 2 KiB, 64 bytes more behind every second; rows of 128 bytes whose 16-byte pieces are
 // exchanged among themselves, piece c of row r at place c ^ (r / 2 % 8); 256 bytes of scales from each wavefront (rows: the
@@ -189,69 +191,139 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 template <int TM>
 struct MatmulRing {
     static constexpr int W = 16 * FP8_TILE + 8 * 64, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
-    static constexpr int NS = TM == 4 ? 2 : 3, BYTES = NS * STAGE, LOADS = 4 + TM + 1;
+    static constexpr int NS = TM == 4 ? 2 : 3, TABLE = NS * STAGE, BYTES = TABLE + 3 * PGMOE_MAX_EXPERTS * 4, LOADS = 4 + TM + 1;
 };
-constexpr int TILE_THREADS = 512;
+constexpr int TILE_THREADS = 512, TILE_GROUPS = 256;  // workgroups: one per CU
 
-struct MatmulTile {  // uniform
-    const uint8_t *w, *x;        // the expert's tiles of the first output block; the chunk's first row
-    const float *sw, *sx;
-    size_t x_stride, sx_stride;  // bytes; floats
-    int KB, nrows, tiles;        // tiles: weight tiles there are from w on (16, or 8 past the last whole pair of blocks)
+// The items of a launch, looked up in a table of the experts in LDS: chunks up to and with the expert, its first row, its rows.
+struct MatmulItem {
+    int expert, row0, nrows, nb;  // nrows == 0: there are no more
 };
-
-template <int XQ, int TM, int MC>
-__device__ inline void matmul_k_loop(const MatmulTile &t, char *ring, int wave, floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
-    typedef MatmulRing<TM> R;
-    const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
-    const unsigned lds = __builtin_amdgcn_readfirstlane(lds_address(ring));
-    const uint8_t *w_src[4];
-    unsigned w_to[4], x_off[TM];
+template <int TM>
+struct MatmulItems {
+    const int *incl;
+    int cols, total;  // column blocks; chunks
+    // Offsets are clamped to the rows there are, whatever they say.
+    __device__ void build(const MatmulArgs &a, int *table) {
+        constexpr int MOST = TM * 64;
+        const int lane = threadIdx.x & 63;
+        int lo[4], hi[4], before = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int tile = wave * 2 + (i >> 1), from = min(tile, t.tiles - 1);
-        w_src[i] = t.w + (size_t)from * t.KB * FP8_TILE + (i & 1) * 1024;
-        w_to[i] = lds + tile * FP8_TILE + (tile >> 1) * 64 + (i & 1) * 1024;
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int row = (wave * TM + i) * 8 + (lane >> 3);
-        x_off[i] = (unsigned)min(row, t.nrows - 1) * (unsigned)t.x_stride + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
-    }
-    const unsigned x_to = lds + R::W + wave * TM * 1024, s_to = lds + R::W + R::X + wave * 256;
-    const float *s_src = wave < 4 ? t.sx : t.sw;
-    const size_t s_step = wave < 4 ? t.sx_stride : 1;
-    const unsigned s_off = 4u * (wave < 4 ? (unsigned)min(wave * 64 + lane, t.nrows - 1) : (unsigned)((lane & 1) && t.tiles > 8 ? t.KB : 0));
-    const uint8_t *x_src = t.x;
-    auto request = [&](unsigned stage) {  // of the next block of inputs
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            load_tile_to_lds((const char *)w_src[i], lane * 16, w_to[i] + stage);
-            w_src[i] += FP8_TILE;
+        for (int q = 0; q < 4; ++q) {  // all at once
+            const int e = q * 64 + lane;
+            lo[q] = a.offsets[min(e, a.E)];
+            hi[q] = a.offsets[min(e + 1, a.E)];
         }
 #pragma unroll
-        for (int i = 0; i < TM; ++i) load_tile_to_lds((const char *)x_src, x_off[i], x_to + i * 1024 + stage);
-        x_src += FP8_BLOCK;
-        load_dwords_to_lds(s_src, s_off, s_to + stage);
-        s_src += s_step;
-    };
+        for (int q = 0; q < 4; ++q) {
+            const int e = q * 64 + lane, first = max(0, min(lo[q], a.rows)), n = max(first, min(hi[q], a.rows)) - first;
+            const int c_incl = before + wave_incl_scan((n + MOST - 1) / MOST);
+            before = __builtin_amdgcn_readlane(c_incl, 63);
+            if (threadIdx.x < 64) {
+                table[e] = c_incl;
+                table[PGMOE_MAX_EXPERTS + e] = first;
+                table[2 * PGMOE_MAX_EXPERTS + e] = n;
+            }
+        }
+        incl = table;
+        cols = (a.NB + 1) / 2;
+        total = before;
+    }
+    // Item number i.  Workgroups go to the 8 XCDs in turn: the column blocks of a chunk stay on one and share its rows in its L2.
+    __device__ MatmulItem at(int i) const {
+        constexpr int MOST = TM * 64;
+        const int turn = i >> 3, group = turn / cols, chunk = group * 8 + (i & 7);
+        if (chunk >= total) return {0, 0, 0, 0};
+        const intx4 c = *reinterpret_cast<const intx4 *>(incl + 4 * (threadIdx.x & 63));
+        int e = 0;
 #pragma unroll
-    for (int st = 0; st < R::NS; ++st)
-        if (st < t.KB) request(st * R::STAGE);
+        for (int q = 0; q < 4; ++q) e += __popcll(__ballot(c[q] <= chunk));
+        const int rows = __builtin_amdgcn_readfirstlane(incl[2 * PGMOE_MAX_EXPERTS + e]), first = __builtin_amdgcn_readfirstlane(incl[PGMOE_MAX_EXPERTS + e]);
+        const int chunks = (rows + MOST - 1) / MOST, k = chunk - (__builtin_amdgcn_readfirstlane(incl[e]) - chunks);
+        const int each = ((rows + chunks - 1) / chunks + 15) & ~15;
+        return {e, first + k * each, max(1, min(each, rows - k * each)), (turn - group * cols) * 2};
+    }
+};
 
+// What a wavefront requests: the blocks of its workgroup's items one after the other.  What a lane adds to the addresses is worked out
+// for each request: in registers across the products it would push accumulators out of them.
+template <int TM>
+struct MatmulRequests {
+    typedef MatmulRing<TM> R;
+    const uint8_t *w_src, *x_src;
+    const float *s_src;
+    unsigned w_second, lds, stage;  // bytes to the wavefront's second weight tile; LDS address of the ring
+    int s_last, s_by, x_last;
+    size_t s_step;
+    int item, left, ahead;  // next item to look up; blocks of the present one that are not requested; requested blocks not yet multiplied
+    __device__ void start(char *ring, int first_item) {
+        lds = __builtin_amdgcn_readfirstlane(lds_address(ring));
+        item = first_item;
+        left = ahead = 0;
+        stage = 0;
+    }
+    __device__ void next(const MatmulArgs &a, const MatmulItems<TM> &items, int wave) {
+        const int lane = threadIdx.x & 63;
+        if (left == 0) {  // uniform
+            const MatmulItem it = items.at(item);
+            if (it.nrows == 0) return;
+            item += gridDim.x;
+            left = a.KB;
+            const size_t block = (size_t)it.expert * a.NB + it.nb;
+            const int last = it.nb + 1 < a.NB ? 15 : 7;  // an odd last block of outputs has no neighbour
+            w_src = a.w + (block * 8 + min(wave * 2, last)) * a.KB * FP8_TILE;
+            w_second = wave * 2 < last ? (unsigned)a.KB * FP8_TILE : 0;
+            x_src = a.x + (size_t)it.row0 * a.x_stride;
+            x_last = it.nrows - 1;
+            // scales: of the rows, 64 from each of the first four wavefronts; of the two blocks of outputs
+            s_src = wave < 4 ? a.x_scale + it.row0 : a.w_scale + block * a.KB;
+            s_step = wave < 4 ? a.x_scale_stride : 1;
+            s_by = wave < 4 ? 4 : 4 * a.KB;
+            s_last = wave < 4 ? it.nrows - 1 : (last == 15 ? 1 : 0);
+        }
+        const unsigned to = lds + stage;
+        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * (2 * FP8_TILE + 64));
+        load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + wave * (2 * FP8_TILE + 64) + FP8_TILE);
+        w_src += FP8_TILE;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int row = (wave * TM + i) * 8 + (lane >> 3);
+            const unsigned off = (unsigned)min(row, x_last) * (unsigned)a.x_stride + (((lane & 7) ^ ((row >> 1) & 7)) << 4);
+            load_tile_to_lds((const char *)x_src, off, to + R::W + (wave * TM + i) * 1024);
+        }
+        x_src += FP8_BLOCK;
+        load_dwords_to_lds(s_src, (unsigned)min((wave & 3) * 64 + lane, s_last) * (unsigned)s_by, to + R::W + R::X + wave * 256);
+        s_src += s_step;
+        stage = stage + R::STAGE == R::NS * R::STAGE ? 0 : stage + R::STAGE;
+        --left;
+        ++ahead;
+    }
+};
+
+// The products of one item.  stores: how many the wavefront issued, at least, behind the requests that are outstanding (they complete in order).
+template <int XQ, int TM, int MC, int STORES>
+__device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const char *ring, unsigned &stage, int wave, bool stored,
+                                     floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
+    typedef MatmulRing<TM> R;
+    const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
     const int g = lane >> 4, i16 = lane & 15;
     const char *w_at = ring + (wn * 8 + 2 * (i16 >> 2)) * FP8_TILE + (wn * 4 + (i16 >> 2)) * 64 + g * 256 + (i16 & 3) * 16;
     const char *x_at = ring + R::W + (wm * 16 + i16) * FP8_BLOCK;
     const int x_low = (g ^ (i16 >> 1)) << 4, x_high = ((4 + g) ^ (i16 >> 1)) << 4;
     const char *s_at = ring + R::W + R::X;
-    unsigned stage = 0;
-    for (int kb = 0; kb < t.KB; ++kb) {
-        // this block's loads have landed: those of at most NS - 1 later ones are outstanding
-        const int later = t.KB - 1 - kb;
-        if (later >= R::NS - 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS * (R::NS - 1)) : "memory");
-        else if (R::NS > 2 && later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        asm volatile("s_barrier" ::: "memory");
+    for (int kb = 0; kb < a.KB; ++kb) {
+        // This block's loads have landed: those of the later ones, and stores behind them all, may be outstanding.
+        if (R::NS == 2 || rq.ahead == 1) {
+            if (kb == 0 && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STORES) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+            if (kb < 2 && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS + STORES) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
+        }
+        // Behind the barrier they have for everyone, and everyone has read the block before, whose stage the next request takes.
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        rq.next(a, items, wave);
+        --rq.ahead;
         if (MC > 0) {
             Operand x[MC > 0 ? MC : 1];
             float s[MC > 0 ? MC : 1];
@@ -265,11 +337,11 @@ __device__ inline void matmul_k_loop(const MatmulTile &t, char *ring, int wave, 
             // one output tile's codes are read while the one before is multiplied; nothing may move further ahead, for want of registers
             intx4 low = *reinterpret_cast<const intx4 *>(w_at + stage), high = *reinterpret_cast<const intx4 *>(w_at + stage + 1024);
 #pragma unroll
-            for (int a = 0; a < 8; ++a) {
+            for (int t = 0; t < 8; ++t) {
                 __builtin_amdgcn_sched_barrier(0);
                 const Operand w = operand<PGMOE_E4M3>(low, high);
-                if (a < 7) {
-                    const char *c = w_at + stage + ((a + 1) >> 2) * FP8_TILE + ((a + 1) & 3) * 64;
+                if (t < 7) {
+                    const char *c = w_at + stage + ((t + 1) >> 2) * FP8_TILE + ((t + 1) & 3) * 64;
                     low = *reinterpret_cast<const intx4 *>(c);
                     high = *reinterpret_cast<const intx4 *>(c + 1024);
                 }
@@ -279,35 +351,40 @@ __device__ inline void matmul_k_loop(const MatmulTile &t, char *ring, int wave, 
 #pragma unroll
                 for (int m = 0; m < MC; ++m)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[a][m][v] = fmaf(s[m], p[m][v], acc[a][m][v]);
+                    for (int v = 0; v < 4; ++v) acc[t][m][v] = fmaf(s[m], p[m][v], acc[t][m][v]);
 #pragma unroll
-                for (int m = 0; m < MC; ++m) asm volatile("" : "+v"(acc[a][m]));  // here, not behind the loop's last branch with every p alive
+                for (int m = 0; m < MC; ++m) asm volatile("" : "+v"(acc[t][m]));  // here, not behind the loop's last branch with every p alive
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (kb + R::NS < t.KB) {
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // everyone has read this stage
-            request(stage);
-        }
-        stage = stage + R::STAGE == R::BYTES ? 0 : stage + R::STAGE;
+        stage = stage + R::STAGE == R::NS * R::STAGE ? 0 : stage + R::STAGE;
     }
 }
 
+// Stores of one row tile of a wavefront whose 128 outputs are all there.
+template <typename Y, bool VEC>
+constexpr int tile_stores() {
+    if constexpr (std::is_void<Y>::value) return 3;
+    else return VEC ? (sizeof(Y) == 4 ? 8 : 4) : 32;
+}
+
 template <int XQ, typename Y, int YQ, bool VEC, int TM, int MC>
-__device__ inline void matmul_tile_body(const MatmulArgs &a, const MatmulTile &t, char *ring, int wave, int row0, int nb) {
+__device__ inline bool matmul_item(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const MatmulItem &it, char *ring, unsigned &stage, int wave,
+                                   bool stored) {
+    constexpr int STORES = tile_stores<Y, VEC>() <= 24 ? tile_stores<Y, VEC>() : 24;
     floatx4 acc[8][MC > 0 ? MC : 1];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int m = 0; m < MC; ++m) acc[i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-    matmul_k_loop<XQ, TM, MC>(t, ring, wave, acc);
+    matmul_k_loop<XQ, TM, MC, STORES>(a, items, rq, ring, stage, wave, stored, acc);
     const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
-    const int block = nb + wn, o = block * FP8_BLOCK + 32 * (lane >> 4);
-    if (block >= a.NB) return;
+    const int block = it.nb + wn, o = block * FP8_BLOCK + 32 * (lane >> 4);
+    if (block >= a.NB) return false;
 #pragma unroll
     for (int m = 0; m < MC; ++m) {
-        const int in_chunk = (wm + 4 * m) * 16 + (lane & 15), row = row0 + in_chunk;
-        const bool live = in_chunk < t.nrows;
+        const int in_chunk = (wm + 4 * m) * 16 + (lane & 15), row = it.row0 + in_chunk;
+        const bool live = in_chunk < it.nrows;
         if (a.relu) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -322,43 +399,67 @@ __device__ inline void matmul_tile_body(const MatmulArgs &a, const MatmulTile &t
                 for (int v = 0; v < 4; ++v) amax = fmaxf(amax, finite_magnitude(acc[i][m][v]));
             amax = fmaxf(amax, __shfl_xor(amax, 16));
             amax = fmaxf(amax, __shfl_xor(amax, 32));
-            const float scale = fp8_scale<YQ>(amax);
+            const Fp8Divisor by = fp8_divisor<YQ>(amax);
             if (live) {
                 uint32_t codes[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) codes[i] = fp8_pack<YQ>(acc[i][m][0] / scale, acc[i][m][1] / scale, acc[i][m][2] / scale, acc[i][m][3] / scale);
+                for (int i = 0; i < 8; ++i) codes[i] = fp8_pack<YQ>(by(acc[i][m][0]), by(acc[i][m][1]), by(acc[i][m][2]), by(acc[i][m][3]));
                 uint4 *q = reinterpret_cast<uint4 *>(a.y_q + (size_t)row * a.y_q_stride + o);
                 q[0] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
                 q[1] = make_uint4(codes[4], codes[5], codes[6], codes[7]);
-                if (lane < 16) a.y_scale[(size_t)block * a.y_scale_stride + row] = scale;
+                if (lane < 16) a.y_scale[(size_t)block * a.y_scale_stride + row] = by.scale;
             }
         } else if (live) {
+            if constexpr (VEC) {
+                typedef Y Yx4 __attribute__((ext_vector_type(4)));
+                Y *p = reinterpret_cast<Y *>(a.y) + (size_t)row * a.y_stride + o;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) store_four<Y, VEC>(a, row, o + 4 * i, acc[i][m]);
+                for (int i = 0; i < 8; i += 2) {
+                    if constexpr (sizeof(Y) == 2) {
+                        typedef Y Yx8 __attribute__((ext_vector_type(8), aligned(8)));
+                        const floatx4 u = acc[i][m], v = acc[i + 1][m];
+                        if (o + 4 * i + 4 < a.n_out) *reinterpret_cast<Yx8 *>(p + 4 * i) = Yx8{(Y)u[0], (Y)u[1], (Y)u[2], (Y)u[3], (Y)v[0], (Y)v[1], (Y)v[2], (Y)v[3]};
+                        else if (o + 4 * i < a.n_out) *reinterpret_cast<Yx4 *>(p + 4 * i) = Yx4{(Y)u[0], (Y)u[1], (Y)u[2], (Y)u[3]};
+                    } else {
+                        store_four<Y, true>(a, row, o + 4 * i, acc[i][m]);
+                        store_four<Y, true>(a, row, o + 4 * i + 4, acc[i + 1][m]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) store_four<Y, false>(a, row, o + 4 * i, acc[i][m]);
+            }
         }
     }
+    return MC > 0 && (block + 1) * FP8_BLOCK <= a.n_out;  // every row tile has a live row: at least STORES were issued
 }
 
 template <int XQ, typename Y, int YQ, bool VEC, int TM>
 __global__ __launch_bounds__(TILE_THREADS, 2) void matmul_tiles_kernel(const MatmulArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char ring[];
-    // column blocks of a chunk go to one XCD (workgroups are dealt to the eight in turn) and share its rows there
-    const int cols = (a.NB + 1) / 2, turn = blockIdx.x >> 3, chunk = turn / cols * 8 + (blockIdx.x & 7), nb = (turn - turn / cols * cols) * 2;
-    const MatmulChunk ci = matmul_chunk<TM * 64>(a, chunk);
-    if (ci.nrows <= 0) return;  // uniform over the workgroup
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const size_t block = (size_t)ci.expert * a.NB + nb;
-    const MatmulTile t = {a.w + block * 8 * a.KB * FP8_TILE, a.x + (size_t)ci.row0 * a.x_stride, a.w_scale + block * a.KB, a.x_scale + ci.row0,
-                          a.x_stride, a.x_scale_stride, a.KB, ci.nrows, nb + 1 < a.NB ? 16 : 8};
-    const int rt = (ci.nrows + 15) >> 4, own = max(0, (rt - (wave >> 1) + 3) >> 2);
-    switch (own) {  // uniform over the wavefront
-#define PG_BODY(MC_)                                                                                              \
-    case MC_:                                                                                                     \
-        if constexpr (MC_ <= TM) matmul_tile_body<XQ, Y, YQ, VEC, TM, MC_>(a, t, ring, wave, ci.row0, nb);         \
-        asm volatile("; %0 row tiles" ::"n"(MC_)); /* keeps the bodies' stores apart */                            \
-        return;
-        PG_BODY(0) PG_BODY(1) PG_BODY(2) PG_BODY(3) PG_BODY(4)
+    MatmulItems<TM> items;
+    items.build(a, reinterpret_cast<int *>(ring + MatmulRing<TM>::TABLE));
+    __syncthreads();
+    MatmulRequests<TM> rq;
+    rq.start(ring, blockIdx.x);
+#pragma unroll
+    for (int st = 0; st < MatmulRing<TM>::NS - 1; ++st) rq.next(a, items, wave);
+    unsigned stage = 0;
+    bool stored = false;
+    for (int i = blockIdx.x;; i += gridDim.x) {
+        const MatmulItem it = items.at(i);
+        if (it.nrows == 0) break;  // uniform over the workgroup; every request has been waited for
+        const int rt = (it.nrows + 15) >> 4, own = max(0, (rt - (wave >> 1) + 3) >> 2);
+        switch (own) {  // uniform over the wavefront
+#define PG_BODY(MC_)                                                                                                                        \
+    case MC_:                                                                                                                               \
+        if constexpr (MC_ <= TM) stored = matmul_item<XQ, Y, YQ, VEC, TM, MC_>(a, items, rq, it, ring, stage, wave, stored);                 \
+        asm volatile("; %0 row tiles" ::"n"(MC_)); /* keeps the bodies' stores apart */                                                      \
+        break;
+            PG_BODY(0) PG_BODY(1) PG_BODY(2) PG_BODY(3) PG_BODY(4)
 #undef PG_BODY
+        }
     }
 }
 
@@ -377,7 +478,8 @@ static int launch_tiles(const MatmulArgs &a, hipStream_t s) {
     }
     // chunks: sum over the experts of ceil(rows / (TM * 64)), in whole eights
     const int64_t chunks = ((a.rows + (int64_t)(TM * 64 - 1) * std::min(a.E, a.rows)) / (TM * 64) + 7) & ~(int64_t)7;
-    hipLaunchKernelGGL((matmul_tiles_kernel<XQ, Y, YQ, VEC, TM>), dim3((unsigned)(chunks * ((a.NB + 1) / 2))), dim3(TILE_THREADS), MatmulRing<TM>::BYTES, s, a);
+    const unsigned groups = (unsigned)std::min<int64_t>(TILE_GROUPS, chunks * ((a.NB + 1) / 2));
+    hipLaunchKernelGGL((matmul_tiles_kernel<XQ, Y, YQ, VEC, TM>), dim3(groups), dim3(TILE_THREADS), MatmulRing<TM>::BYTES, s, a);
     return PGMOE_OK;
 }
 template <int XQ, typename Y, int YQ, bool VEC>
@@ -434,7 +536,7 @@ extern "C" int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weig
     }
     if (x->rows == 0) return PGMOE_OK;
     // (chunk, block of outputs) items are numbered with 31 bits
-    if ((x->rows / 16 + (int64_t)w->n_experts) * fp8_blocks(w->n_out) > 0x7fffffff)
+    if ((x->rows / 16 + (int64_t)w->n_experts + 8) * fp8_blocks(w->n_out) > 0x7fffff00)
         return fail(nullptr, PGMOE_EINVAL, "%s: %d rows by n_out=%d are more than one launch holds", fn, x->rows, w->n_out);
     if (y) NEED_PTR(nullptr, fn, y, dtype_bytes(y_dtype));
     NEED_PTR(nullptr, fn, expert_offsets, 4);

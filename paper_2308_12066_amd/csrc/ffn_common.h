@@ -85,6 +85,11 @@ __device__ inline void load_tile_to_lds(const char *src, unsigned lane_off, unsi
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_off), "s"(src), "s"(lds_tile) : "memory", "m0");
 }
 
+// Two neighbouring KiB (the offset of the instruction counts on both sides).
+__device__ inline void load_two_tiles_to_lds(const char *src, unsigned lane_off, unsigned lds_tile) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %0, %1 offset:1024" ::"v"(lane_off), "s"(src), "s"(lds_tile)
+                 : "memory", "m0");
+}
 __device__ inline void load_dwords_to_lds(const void *src, unsigned lane_off, unsigned lds) {  // four bytes a lane
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_off), "s"(src), "s"(lds) : "memory", "m0");
 }

@@ -15,10 +15,22 @@ __host__ __device__ inline int fp8_blocks(int n) { return (n + FP8_BLOCK - 1) / 
 template <int Q>
 constexpr float fp8_largest = Q == PGMOE_E4M3 ? 448.f : 57344.f;
 
-// Scale of a block whose largest finite magnitude is amax.
+// Scale of a block whose largest finite magnitude is amax, and quotients by it, correctly rounded: with the rounded inverse, the
+// remainder of the first quotient (exact in one multiply-add) corrects it (Markstein).  The remainder of what does not
+// round to zero is a multiple of 2^-63 times the scale's leading bit, exact from scales of 2^-86 on; below 2^-80 the quotients are divisions.
+struct Fp8Divisor {
+    float scale, inverse;
+    __device__ float operator()(float x) const {
+        const float q = x * inverse;
+        const float corrected = fmaf(fmaf(-q, scale, x), inverse, q);
+        if (scale < 0x1p-80f) return x / scale;
+        return fabsf(q) < INFINITY ? corrected : q;  // of an infinity or NaN as it is
+    }
+};
 template <int Q>
-__device__ inline float fp8_scale(float amax) {
-    return fmaxf(amax / fp8_largest<Q>, 0x1p-126f);
+__device__ inline Fp8Divisor fp8_divisor(float amax) {
+    const float scale = fmaxf(amax / fp8_largest<Q>, 0x1p-126f);
+    return {scale, 1.f / scale};
 }
 __device__ inline float finite_magnitude(float x) {  // 0 for infinities and NaN
     const float a = fabsf(x);

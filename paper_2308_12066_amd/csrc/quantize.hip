@@ -32,15 +32,15 @@ __global__ __launch_bounds__(QR_THREADS) void quantize_rows_kernel(const Quantiz
     for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_magnitude(v[j]));
 #pragma unroll
     for (int m = 1; m < 16; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
-    const float scale = fp8_scale<Q>(amax);
+    const Fp8Divisor by = fp8_divisor<Q>(amax);
     uint2 codes;
-    codes.x = fp8_pack<Q>(v[0] / scale, v[1] / scale, v[2] / scale, v[3] / scale);
-    codes.y = fp8_pack<Q>(v[4] / scale, v[5] / scale, v[6] / scale, v[7] / scale);
+    codes.x = fp8_pack<Q>(by(v[0]), by(v[1]), by(v[2]), by(v[3]));
+    codes.y = fp8_pack<Q>(by(v[4]), by(v[5]), by(v[6]), by(v[7]));
     for (int j = 0; j < a.copies; ++j) {
         const int r = a.row_of ? a.row_of[(size_t)t * a.copies + j] : t;
         if (r < 0 || r >= a.rows) continue;
         *reinterpret_cast<uint2 *>(a.q + (size_t)r * a.q_stride + b * FP8_BLOCK + lane * 8) = codes;
-        if (lane == 0) a.scale[(size_t)b * a.scale_stride + r] = scale;
+        if (lane == 0) a.scale[(size_t)b * a.scale_stride + r] = by.scale;
     }
 }
 
@@ -80,11 +80,11 @@ __global__ __launch_bounds__(QW_THREADS) void quantize_weights_kernel(const Quan
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < QW_THREADS / 64; ++i) amax = fmaxf(amax, wave_max[i]);
-    const float scale = fp8_scale<PGMOE_E4M3>(amax);
+    const Fp8Divisor by = fp8_divisor<PGMOE_E4M3>(amax);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] / scale;
+        for (int j = 0; j < 8; ++j) v[i][j] = by(v[i][j]);
     if (a.fwd_q) {
         const int o0 = nq * 8;
 #pragma unroll
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(QW_THREADS) void quantize_weights_kernel(const Quan
             *reinterpret_cast<uint4 *>(a.fwd_q + ((((size_t)e * NB + nb) * 8 + tile) * KB + kb) * FP8_TILE + in_tile) =
                 *reinterpret_cast<const uint4 *>(image + tile * QW_TILE + in_tile);
         }
-        if (threadIdx.x == 0) a.fwd_scale[((size_t)e * NB + nb) * KB + kb] = scale;
+        if (threadIdx.x == 0) a.fwd_scale[((size_t)e * NB + nb) * KB + kb] = by.scale;
     }
     if (a.bwd_q) {
         if (a.fwd_q) __syncthreads();
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(QW_THREADS) void quantize_weights_kernel(const Quan
             *reinterpret_cast<uint4 *>(a.bwd_q + ((((size_t)e * KB + kb) * 8 + tile) * NB + nb) * FP8_TILE + in_tile) =
                 *reinterpret_cast<const uint4 *>(image + tile * QW_TILE + in_tile);
         }
-        if (threadIdx.x == 0) a.bwd_scale[((size_t)e * KB + kb) * NB + nb] = scale;
+        if (threadIdx.x == 0) a.bwd_scale[((size_t)e * KB + kb) * NB + nb] = by.scale;
     }
 }
 
