@@ -122,8 +122,6 @@ __device__ inline void store_four(const MatmulArgs &a, int r, int o, floatx4 v) 
     }
 }
 
-__device__ inline float relu_of(float v) { return v > 0.f || v != v ? v : 0.f; }  // NaN stays
-
 // Few rows an expert.  A workgroup takes 16 rows and one block of 128 outputs, a wavefront 16 of them, operands straight from
 // memory into registers.  Y = void: quantised again, YQ.
 constexpr int FEW_THREADS = 512;
@@ -157,19 +155,26 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
     const bool live = (lane & 15) < ci.nrows;
     const int o = nb * FP8_BLOCK + wave * 16 + 4 * (lane >> 4);
     if constexpr (std::is_void<Y>::value) {
-        float amax = 0.f;
+        auto largest = [&](auto of) {  // of the row's 128 results: four a lane, 16 a wavefront
+            float m = maximum(maximum(of(acc[0]), of(acc[1])), maximum(of(acc[2]), of(acc[3])));
+            m = maximum(m, __shfl_xor(m, 16));
+            m = maximum(m, __shfl_xor(m, 32));
+            if (lane < 16) amax_of[wave][lane] = m;
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) amax = fmaxf(amax, finite_magnitude(acc[i]));
-        amax = fmaxf(amax, __shfl_xor(amax, 16));
-        amax = fmaxf(amax, __shfl_xor(amax, 32));
-        if (lane < 16) amax_of[wave][lane] = amax;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, amax_of[i][lane & 15]);
-        const Fp8Divisor by = fp8_divisor<YQ>(amax);
+            for (int i = 0; i < 8; ++i) m = maximum(m, amax_of[i][lane & 15]);
+            return m;
+        };
+        float amax = largest([](float v) { return fabsf(v); });
+        if (fp8_unusual<YQ>(amax)) {  // of the same 16 rows in every wavefront
+            __syncthreads();
+            amax = largest(finite_magnitude);
+        }
+        const float scale = fp8_scale<YQ>(amax);
+        const Fp8CarefulDivisor by(scale);
         if (live) {
             *reinterpret_cast<uint32_t *>(a.y_q + (size_t)row * a.y_q_stride + o) = fp8_pack<YQ>(by(acc[0]), by(acc[1]), by(acc[2]), by(acc[3]));
-            if (wave == 0 && lane < 16) a.y_scale[(size_t)nb * a.y_scale_stride + row] = by.scale;
+            if (wave == 0 && lane < 16) a.y_scale[(size_t)nb * a.y_scale_stride + row] = scale;
         }
     } else {
         if (live) store_four<Y, VEC>(a, row, o, acc);
@@ -191,56 +196,89 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 template <int TM>
 struct MatmulRing {
     static constexpr int W = 16 * FP8_TILE + 8 * 64, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
-    static constexpr int NS = TM == 4 ? 2 : 3, TABLE = NS * STAGE, BYTES = TABLE + 3 * PGMOE_MAX_EXPERTS * 4, LOADS = 4 + TM + 1;
+    static constexpr int NS = TM == 4 ? 2 : 3, TABLE = NS * STAGE, BYTES = TABLE + 4 * PGMOE_MAX_EXPERTS * 4, LOADS = 4 + TM + 1;
 };
 constexpr int TILE_THREADS = 512, TILE_GROUPS = 256;  // workgroups: one per CU
 
-// The items of a launch, looked up in a table of the experts in LDS: chunks up to and with the expert, its first row, its rows.
+// The items of a launch, looked up in a table of the experts in LDS: chunks up to and with the expert, its first row, its rows, rows of a chunk.
+// The chunks of an expert are its rows dealt evenly, in whole 16s, to as few chunks of at most 64 u rows as hold them.  u is the one
+// of 1 .. TM for which the launch should end first: rounds of one item a workgroup, times what a block of inputs costs an
+// item of u units on the mean, which is MATMUL_COST + u.
 struct MatmulItem {
     int expert, row0, nrows, nb;  // nrows == 0: there are no more
 };
+constexpr int MATMUL_COST = 1;
 template <int TM>
 struct MatmulItems {
-    const int *incl;
+    const int *table;
     int cols, total;  // column blocks; chunks
+    __device__ static int each_of(int n, int chunks) { return (((n + chunks - 1) / chunks) + 15) & ~15; }
     // Offsets are clamped to the rows there are, whatever they say.
-    __device__ void build(const MatmulArgs &a, int *table) {
-        constexpr int MOST = TM * 64;
+    __device__ void build(const MatmulArgs &a, int *to) {
         const int lane = threadIdx.x & 63;
-        int lo[4], hi[4], before = 0;
+        int lo[4], n[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {  // all at once
             const int e = q * 64 + lane;
             lo[q] = a.offsets[min(e, a.E)];
-            hi[q] = a.offsets[min(e + 1, a.E)];
+            n[q] = a.offsets[min(e + 1, a.E)];
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int e = q * 64 + lane, first = max(0, min(lo[q], a.rows)), n = max(first, min(hi[q], a.rows)) - first;
-            const int c_incl = before + wave_incl_scan((n + MOST - 1) / MOST);
+            lo[q] = max(0, min(lo[q], a.rows));
+            n[q] = max(lo[q], min(n[q], a.rows)) - lo[q];
+        }
+        cols = (a.NB + 1) / 2;
+        int most = TM * 64;
+        if (TM > 1) {
+            float best = INFINITY;
+            static_for<TM>([&](auto u_) {
+                constexpr int MOST = 64 * (TM - decltype(u_)::value);
+                int sum = 0;
+                float cost = 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = (n[q] + MOST - 1) / MOST;
+                    sum += c;
+                    cost += c ? (float)c * (float)(MATMUL_COST + ((each_of(n[q], c) + 63) >> 6)) : 0.f;
+                }
+                const int chunks = __builtin_amdgcn_readlane(wave_incl_scan(sum), 63);
+#pragma unroll
+                for (int m = 1; m < 64; m <<= 1) cost += __shfl_xor(cost, m);
+                const float t = (float)((chunks * (int64_t)cols + gridDim.x - 1) / gridDim.x) * cost / (float)max(1, chunks);
+                if (t < best) {  // uniform
+                    best = t;
+                    most = MOST;
+                }
+            });
+        }
+        int before = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = (n[q] + most - 1) / most, c_incl = before + wave_incl_scan(c);
             before = __builtin_amdgcn_readlane(c_incl, 63);
             if (threadIdx.x < 64) {
-                table[e] = c_incl;
-                table[PGMOE_MAX_EXPERTS + e] = first;
-                table[2 * PGMOE_MAX_EXPERTS + e] = n;
+                const int e = q * 64 + lane;
+                to[e] = c_incl;
+                to[PGMOE_MAX_EXPERTS + e] = lo[q];
+                to[2 * PGMOE_MAX_EXPERTS + e] = n[q];
+                to[3 * PGMOE_MAX_EXPERTS + e] = c ? each_of(n[q], c) : 0;
             }
         }
-        incl = table;
-        cols = (a.NB + 1) / 2;
+        table = to;
         total = before;
     }
     // Item number i.  Workgroups go to the 8 XCDs in turn: the column blocks of a chunk stay on one and share its rows in its L2.
     __device__ MatmulItem at(int i) const {
-        constexpr int MOST = TM * 64;
         const int turn = i >> 3, group = turn / cols, chunk = group * 8 + (i & 7);
         if (chunk >= total) return {0, 0, 0, 0};
-        const intx4 c = *reinterpret_cast<const intx4 *>(incl + 4 * (threadIdx.x & 63));
+        const intx4 c = *reinterpret_cast<const intx4 *>(table + 4 * (threadIdx.x & 63));
         int e = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) e += __popcll(__ballot(c[q] <= chunk));
-        const int rows = __builtin_amdgcn_readfirstlane(incl[2 * PGMOE_MAX_EXPERTS + e]), first = __builtin_amdgcn_readfirstlane(incl[PGMOE_MAX_EXPERTS + e]);
-        const int chunks = (rows + MOST - 1) / MOST, k = chunk - (__builtin_amdgcn_readfirstlane(incl[e]) - chunks);
-        const int each = ((rows + chunks - 1) / chunks + 15) & ~15;
+        const int before = e ? __builtin_amdgcn_readfirstlane(table[e - 1]) : 0, first = __builtin_amdgcn_readfirstlane(table[PGMOE_MAX_EXPERTS + e]);
+        const int rows = __builtin_amdgcn_readfirstlane(table[2 * PGMOE_MAX_EXPERTS + e]), each = __builtin_amdgcn_readfirstlane(table[3 * PGMOE_MAX_EXPERTS + e]);
+        const int k = chunk - before;
         return {e, first + k * each, max(1, min(each, rows - k * each)), (turn - group * cols) * 2};
     }
 };
@@ -300,9 +338,23 @@ struct MatmulRequests {
     }
 };
 
-// The products of one item.  stores: how many the wavefront issued, at least, behind the requests that are outstanding (they complete in order).
+// Waits until, at most, the loads of one more request (two) and the stores of `tiles` row tiles are outstanding: operations complete in order.
+template <int LOADS, int STORES>
+__device__ inline void wait_for_loads(bool two, int tiles) {  // uniform
+#define PG_WAIT(T_)                                                                                              \
+    case T_:                                                                                                     \
+        if (two) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS + T_ * STORES < 63 ? LOADS + T_ * STORES : 63) : "memory"); \
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T_ * STORES < 63 ? T_ * STORES : 63) : "memory");          \
+        return;
+    switch (tiles) {
+        PG_WAIT(0) PG_WAIT(1) PG_WAIT(2) PG_WAIT(3) PG_WAIT(4)
+    }
+#undef PG_WAIT
+}
+
+// The products of one item.  stored: row tiles whose results the wavefront stored behind the requests that are outstanding.
 template <int XQ, int TM, int MC, int STORES>
-__device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const char *ring, unsigned &stage, int wave, bool stored,
+__device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const char *ring, unsigned &stage, int wave, int stored,
                                      floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
     typedef MatmulRing<TM> R;
     const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
@@ -313,13 +365,8 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> 
     const char *s_at = ring + R::W + R::X;
     for (int kb = 0; kb < a.KB; ++kb) {
         // This block's loads have landed: those of the later ones, and stores behind them all, may be outstanding.
-        if (R::NS == 2 || rq.ahead == 1) {
-            if (kb == 0 && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STORES) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        } else {
-            if (kb < 2 && stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS + STORES) : "memory");
-            else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(R::LOADS) : "memory");
-        }
+        const bool two = R::NS > 2 && rq.ahead > 1;
+        wait_for_loads<(R::NS > 2 ? R::LOADS : 0), STORES>(two, kb < (two ? 2 : 1) ? stored : 0);
         // Behind the barrier they have for everyone, and everyone has read the block before, whose stage the next request takes.
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         rq.next(a, items, wave);
@@ -369,9 +416,9 @@ constexpr int tile_stores() {
 }
 
 template <int XQ, typename Y, int YQ, bool VEC, int TM, int MC>
-__device__ inline bool matmul_item(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const MatmulItem &it, char *ring, unsigned &stage, int wave,
-                                   bool stored) {
-    constexpr int STORES = tile_stores<Y, VEC>() <= 24 ? tile_stores<Y, VEC>() : 24;
+__device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const MatmulItem &it, char *ring, unsigned &stage, int wave,
+                                  int stored) {
+    constexpr int STORES = tile_stores<Y, VEC>();
     floatx4 acc[8][MC > 0 ? MC : 1];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -380,7 +427,7 @@ __device__ inline bool matmul_item(const MatmulArgs &a, const MatmulItems<TM> &i
     matmul_k_loop<XQ, TM, MC, STORES>(a, items, rq, ring, stage, wave, stored, acc);
     const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
     const int block = it.nb + wn, o = block * FP8_BLOCK + 32 * (lane >> 4);
-    if (block >= a.NB) return false;
+    if (block >= a.NB) return 0;
 #pragma unroll
     for (int m = 0; m < MC; ++m) {
         const int in_chunk = (wm + 4 * m) * 16 + (lane & 15), row = it.row0 + in_chunk;
@@ -392,22 +439,31 @@ __device__ inline bool matmul_item(const MatmulArgs &a, const MatmulItems<TM> &i
                 for (int v = 0; v < 4; ++v) acc[i][m][v] = relu_of(acc[i][m][v]);
         }
         if constexpr (std::is_void<Y>::value) {
-            float amax = 0.f;
+            auto largest = [&](auto of) {
+                float l = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) amax = fmaxf(amax, finite_magnitude(acc[i][m][v]));
-            amax = fmaxf(amax, __shfl_xor(amax, 16));
-            amax = fmaxf(amax, __shfl_xor(amax, 32));
-            const Fp8Divisor by = fp8_divisor<YQ>(amax);
-            if (live) {
-                uint32_t codes[8];
+                    for (int v = 0; v < 4; ++v) l = maximum(l, of(acc[i][m][v]));
+                l = maximum(l, __shfl_xor(l, 16));
+                return maximum(l, __shfl_xor(l, 32));
+            };
+            float amax = largest([](float v) { return fabsf(v); });
+            const bool unusual = fp8_unusual<YQ>(amax);
+            if (unusual) amax = largest(finite_magnitude);
+            const float scale = fp8_scale<YQ>(amax);
+            uint32_t codes[8];
+            auto quantise = [&](auto by) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) codes[i] = fp8_pack<YQ>(by(acc[i][m][0]), by(acc[i][m][1]), by(acc[i][m][2]), by(acc[i][m][3]));
+            };
+            if (unusual) quantise(Fp8CarefulDivisor(scale));
+            else quantise(Fp8Divisor(scale));
+            if (live) {
                 uint4 *q = reinterpret_cast<uint4 *>(a.y_q + (size_t)row * a.y_q_stride + o);
                 q[0] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
                 q[1] = make_uint4(codes[4], codes[5], codes[6], codes[7]);
-                if (lane < 16) a.y_scale[(size_t)block * a.y_scale_stride + row] = by.scale;
+                if (lane < 16) a.y_scale[(size_t)block * a.y_scale_stride + row] = scale;
             }
         } else if (live) {
             if constexpr (VEC) {
@@ -431,7 +487,7 @@ __device__ inline bool matmul_item(const MatmulArgs &a, const MatmulItems<TM> &i
             }
         }
     }
-    return MC > 0 && (block + 1) * FP8_BLOCK <= a.n_out;  // every row tile has a live row: at least STORES were issued
+    return (block + 1) * FP8_BLOCK <= a.n_out ? MC : 0;  // every row tile has a live row: STORES were issued for each
 }
 
 template <int XQ, typename Y, int YQ, bool VEC, int TM>
@@ -446,7 +502,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void matmul_tiles_kernel(const Mat
 #pragma unroll
     for (int st = 0; st < MatmulRing<TM>::NS - 1; ++st) rq.next(a, items, wave);
     unsigned stage = 0;
-    bool stored = false;
+    int stored = 0;
     for (int i = blockIdx.x;; i += gridDim.x) {
         const MatmulItem it = items.at(i);
         if (it.nrows == 0) break;  // uniform over the workgroup; every request has been waited for

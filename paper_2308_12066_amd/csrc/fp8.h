@@ -15,22 +15,40 @@ __host__ __device__ inline int fp8_blocks(int n) { return (n + FP8_BLOCK - 1) / 
 template <int Q>
 constexpr float fp8_largest = Q == PGMOE_E4M3 ? 448.f : 57344.f;
 
-// Scale of a block whose largest finite magnitude is amax, and quotients by it, correctly rounded: with the rounded inverse, the
-// remainder of the first quotient (exact in one multiply-add) corrects it (Markstein).  The remainder of what does not
-// round to zero is a multiple of 2^-63 times the scale's leading bit, exact from scales of 2^-86 on; below 2^-80 the quotients are divisions.
+// The larger of both; NaN if one is (one instruction on this chip, with magnitudes taken on the way).
+__device__ inline float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ inline float relu_of(float v) { return maximum(v, 0.f); }
+
+// Quotients by the scale of a block.  A block's largest magnitude is first taken with infinities and NaN among its values: it is finite
+// nearly always, and then three instructions give the correctly rounded quotient: with the rounded inverse, the remainder
+// of the first quotient (exact in one multiply-add) corrects it (Markstein).  The remainder of what does not round to zero is a
+// multiple of 2^-63 times the scale's leading bit, exact from scales of 2^-86 on.  Blocks with infinities or NaN, whose largest finite
+// magnitude has to be looked for, and scales below 2^-80 take the careful form: both sides raised, what is not finite left alone.
 struct Fp8Divisor {
     float scale, inverse;
+    __device__ explicit Fp8Divisor(float s) : scale(s), inverse(1.f / s) {}
     __device__ float operator()(float x) const {
         const float q = x * inverse;
-        const float corrected = fmaf(fmaf(-q, scale, x), inverse, q);
-        if (scale < 0x1p-80f) return x / scale;
-        return fabsf(q) < INFINITY ? corrected : q;  // of an infinity or NaN as it is
+        return fmaf(fmaf(-q, scale, x), inverse, q);
+    }
+};
+struct Fp8CarefulDivisor {
+    float up;
+    Fp8Divisor by;
+    __device__ explicit Fp8CarefulDivisor(float s) : up(s < 0x1p-80f ? 0x1p64f : 1.f), by(s * up) {}
+    __device__ float operator()(float x) const {
+        const float q = x * up * by.inverse;
+        return fabsf(q) < INFINITY ? by(x * up) : q;
     }
 };
 template <int Q>
-__device__ inline Fp8Divisor fp8_divisor(float amax) {
-    const float scale = fmaxf(amax / fp8_largest<Q>, 0x1p-126f);
-    return {scale, 1.f / scale};
+__device__ inline float fp8_scale(float amax) {
+    return fmaxf(amax / fp8_largest<Q>, 0x1p-126f);
+}
+// Is there a block among the wavefront's, of largest magnitude amax, that needs the careful form?
+template <int Q>
+__device__ inline bool fp8_unusual(float amax) {
+    return __any(!(amax < INFINITY && (amax >= 0x1p-79f * fp8_largest<Q> || amax == 0.f)));
 }
 __device__ inline float finite_magnitude(float x) {  // 0 for infinities and NaN
     const float a = fabsf(x);

@@ -27,20 +27,30 @@ __global__ __launch_bounds__(QR_THREADS) void quantize_rows_kernel(const Quantiz
     if (t >= a.T) return;  // whole groups of 16 lanes
     float v[8];
     load_eight<L, VEC>(reinterpret_cast<const L *>(a.x) + (size_t)t * a.x_stride, b * FP8_BLOCK + lane * 8, a.cols, v);
-    float amax = 0.f;
+    auto largest = [&](auto of) {
+        float l = of(v[0]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_magnitude(v[j]));
+        for (int j = 1; j < 8; ++j) l = maximum(l, of(v[j]));
 #pragma unroll
-    for (int m = 1; m < 16; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
-    const Fp8Divisor by = fp8_divisor<Q>(amax);
-    uint2 codes;
-    codes.x = fp8_pack<Q>(by(v[0]), by(v[1]), by(v[2]), by(v[3]));
-    codes.y = fp8_pack<Q>(by(v[4]), by(v[5]), by(v[6]), by(v[7]));
+        for (int m = 1; m < 16; m <<= 1) l = maximum(l, __shfl_xor(l, m));
+        return l;
+    };
+    float amax = largest([](float x) { return fabsf(x); });
+    const bool unusual = fp8_unusual<Q>(amax);
+    if (unusual) amax = largest(finite_magnitude);
+    const float scale = fp8_scale<Q>(amax);
+    auto quantise = [&](auto by) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = by(v[j]);
+    };
+    if (unusual) quantise(Fp8CarefulDivisor(scale));
+    else quantise(Fp8Divisor(scale));
+    const uint2 codes = make_uint2(fp8_pack<Q>(v[0], v[1], v[2], v[3]), fp8_pack<Q>(v[4], v[5], v[6], v[7]));
     for (int j = 0; j < a.copies; ++j) {
         const int r = a.row_of ? a.row_of[(size_t)t * a.copies + j] : t;
         if (r < 0 || r >= a.rows) continue;
         *reinterpret_cast<uint2 *>(a.q + (size_t)r * a.q_stride + b * FP8_BLOCK + lane * 8) = codes;
-        if (lane == 0) a.scale[(size_t)b * a.scale_stride + r] = by.scale;
+        if (lane == 0) a.scale[(size_t)b * a.scale_stride + r] = scale;
     }
 }
 
@@ -66,25 +76,40 @@ __global__ __launch_bounds__(QW_THREADS) void quantize_weights_kernel(const Quan
     const int nq = threadIdx.x & 15, kq = threadIdx.x >> 4;
     const L *w = reinterpret_cast<const L *>(a.w) + (size_t)e * a.n_in * a.n_out;
     float v[8][8];  // [patch * 4 + input][output]
-    float amax = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int in = kb * FP8_BLOCK + (i >> 2) * 64 + kq * 4 + (i & 3);
         load_eight<L, VEC>(w + (size_t)min(in, a.n_in - 1) * a.n_out, nb * FP8_BLOCK + nq * 8, in < a.n_in ? a.n_out : 0, v[i]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_magnitude(v[i][j]));
     }
+    auto largest = [&](auto of) {
+        float l = 0.f;
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
-    if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = amax;
-    __syncthreads();
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int i = 0; i < QW_THREADS / 64; ++i) amax = fmaxf(amax, wave_max[i]);
-    const Fp8Divisor by = fp8_divisor<PGMOE_E4M3>(amax);
+            for (int j = 0; j < 8; ++j) l = maximum(l, of(v[i][j]));
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+        for (int m = 1; m < 64; m <<= 1) l = maximum(l, __shfl_xor(l, m));
+        if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = l;
+        __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = by(v[i][j]);
+        for (int i = 0; i < QW_THREADS / 64; ++i) l = maximum(l, wave_max[i]);
+        return l;
+    };
+    float amax = largest([](float x) { return fabsf(x); });
+    const bool unusual = fp8_unusual<PGMOE_E4M3>(amax);  // the same in every wavefront
+    if (unusual) {
+        __syncthreads();
+        amax = largest(finite_magnitude);
+    }
+    const float scale = fp8_scale<PGMOE_E4M3>(amax);
+    auto quantise = [&](auto by) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = by(v[i][j]);
+    };
+    if (unusual) quantise(Fp8CarefulDivisor(scale));
+    else quantise(Fp8Divisor(scale));
     if (a.fwd_q) {
         const int o0 = nq * 8;
 #pragma unroll
@@ -102,7 +127,7 @@ __global__ __launch_bounds__(QW_THREADS) void quantize_weights_kernel(const Quan
             *reinterpret_cast<uint4 *>(a.fwd_q + ((((size_t)e * NB + nb) * 8 + tile) * KB + kb) * FP8_TILE + in_tile) =
                 *reinterpret_cast<const uint4 *>(image + tile * QW_TILE + in_tile);
         }
-        if (threadIdx.x == 0) a.fwd_scale[((size_t)e * NB + nb) * KB + kb] = by.scale;
+        if (threadIdx.x == 0) a.fwd_scale[((size_t)e * NB + nb) * KB + kb] = scale;
     }
     if (a.bwd_q) {
         if (a.fwd_q) __syncthreads();
@@ -121,7 +146,7 @@ __global__ __launch_bounds__(QW_THREADS) void quantize_weights_kernel(const Quan
             *reinterpret_cast<uint4 *>(a.bwd_q + ((((size_t)e * KB + kb) * 8 + tile) * NB + nb) * FP8_TILE + in_tile) =
                 *reinterpret_cast<const uint4 *>(image + tile * QW_TILE + in_tile);
         }
-        if (threadIdx.x == 0) a.bwd_scale[((size_t)e * KB + kb) * NB + nb] = by.scale;
+        if (threadIdx.x == 0) a.bwd_scale[((size_t)e * KB + kb) * NB + nb] = scale;
     }
 }
 
