@@ -187,15 +187,18 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 // stages of an item arrive, and the results of the one before leave, under products.  Eight wavefronts as 2 x 4: wavefront
 // (wn, wm) has 128 outputs (one scale) and the row tiles wm, wm + 4, ..
 //
-// LDS, a stage: 16 weight tiles of 2 KiB, 64 bytes more behind every second; rows of 128 bytes whose 16-byte pieces are
+// LDS, a stage: 16 weight tiles of 2 KiB, 64 bytes more behind each; rows of 128 bytes whose 16-byte pieces are
 // exchanged among themselves, piece c of row r at place c ^ (r / 2 % 8); 256 bytes of scales from each wavefront (rows: the
 // first four; weights: the fifth's first two).  Both operands are then read without bank conflicts.
 //
-// The outputs are dealt to the matrix instruction's 16 rows so that a lane ends with 32 neighbouring outputs: row i of the a-th product
-// is output 32 * (i / 4) + 4 * a + i % 4 of the wavefront's 128, and a lane's four results of a product are rows 4 * (lane / 16) ..
+// The outputs are dealt to the matrix instruction's 16 rows so that what a lane stores at once is 16 bytes, and what the four lanes of
+// a row store is 64 bytes side by side: with RUN = 16 / bytes of a result, row i of the a-th product is output
+// 4 RUN (4 a / RUN) + RUN (i / 4) + 4 a % RUN + i % 4 of the wavefront's 128 (a lane's four results of a product are rows 4 (lane / 16) ..).
+// With 64 bytes a lane in a row, stores of 16 bytes went to 64 places at once: an item ended 5 us later.
+constexpr int MATMUL_W_TILE = FP8_TILE + 64;
 template <int TM>
 struct MatmulRing {
-    static constexpr int W = 16 * FP8_TILE + 8 * 64, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
+    static constexpr int W = 16 * MATMUL_W_TILE, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
     static constexpr int NS = TM == 4 ? 2 : 3, TABLE = NS * STAGE, BYTES = TABLE + 4 * PGMOE_MAX_EXPERTS * 4, LOADS = 4 + TM + 1;
 };
 constexpr int TILE_THREADS = 512, TILE_GROUPS = 256;  // workgroups: one per CU
@@ -320,8 +323,8 @@ struct MatmulRequests {
             s_last = wave < 4 ? it.nrows - 1 : (last == 15 ? 1 : 0);
         }
         const unsigned to = lds + stage;
-        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * (2 * FP8_TILE + 64));
-        load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + wave * (2 * FP8_TILE + 64) + FP8_TILE);
+        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * 2 * MATMUL_W_TILE);
+        load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
         w_src += FP8_TILE;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -353,13 +356,17 @@ __device__ inline void wait_for_loads(bool two, int tiles) {  // uniform
 }
 
 // The products of one item.  stored: row tiles whose results the wavefront stored behind the requests that are outstanding.
-template <int XQ, int TM, int MC, int STORES>
+template <int XQ, int TM, int MC, int RUN, int STORES>
 __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const char *ring, unsigned &stage, int wave, int stored,
                                      floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
     typedef MatmulRing<TM> R;
     const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
     const int g = lane >> 4, i16 = lane & 15;
-    const char *w_at = ring + (wn * 8 + 2 * (i16 >> 2)) * FP8_TILE + (wn * 4 + (i16 >> 2)) * 64 + g * 256 + (i16 & 3) * 16;
+    // the output of product t, in 16ths of the wavefront's 128: lane's place for t = 0 and what t adds
+    constexpr int PER = RUN / 4;  // products of a run
+    const int o0 = RUN * (i16 >> 2) + (i16 & 3);
+    const char *w_at = ring + (wn * 8 + (o0 >> 4)) * MATMUL_W_TILE + (o0 & 15) * 16 + g * 256;
+    auto place = [](int t) { return t / PER * PER * MATMUL_W_TILE + t % PER * 64; };
     const char *x_at = ring + R::W + (wm * 16 + i16) * FP8_BLOCK;
     const int x_low = (g ^ (i16 >> 1)) << 4, x_high = ((4 + g) ^ (i16 >> 1)) << 4;
     const char *s_at = ring + R::W + R::X;
@@ -388,7 +395,7 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> 
                 __builtin_amdgcn_sched_barrier(0);
                 const Operand w = operand<PGMOE_E4M3>(low, high);
                 if (t < 7) {
-                    const char *c = w_at + stage + ((t + 1) >> 2) * FP8_TILE + ((t + 1) & 3) * 64;
+                    const char *c = w_at + stage + place(t + 1);
                     low = *reinterpret_cast<const intx4 *>(c);
                     high = *reinterpret_cast<const intx4 *>(c + 1024);
                 }
@@ -414,19 +421,24 @@ constexpr int tile_stores() {
     if constexpr (std::is_void<Y>::value) return 3;
     else return VEC ? (sizeof(Y) == 4 ? 8 : 4) : 32;
 }
+template <typename Y>
+constexpr int run_of() {  // results in 16 bytes
+    if constexpr (std::is_void<Y>::value) return 16;
+    else return 16 / sizeof(Y);
+}
 
 template <int XQ, typename Y, int YQ, bool VEC, int TM, int MC>
 __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const MatmulItem &it, char *ring, unsigned &stage, int wave,
                                   int stored) {
-    constexpr int STORES = tile_stores<Y, VEC>();
+    constexpr int STORES = tile_stores<Y, VEC>(), RUN = run_of<Y>();
     floatx4 acc[8][MC > 0 ? MC : 1];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int m = 0; m < MC; ++m) acc[i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-    matmul_k_loop<XQ, TM, MC, STORES>(a, items, rq, ring, stage, wave, stored, acc);
+    matmul_k_loop<XQ, TM, MC, RUN, STORES>(a, items, rq, ring, stage, wave, stored, acc);
     const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
-    const int block = it.nb + wn, o = block * FP8_BLOCK + 32 * (lane >> 4);
+    const int block = it.nb + wn, o = block * FP8_BLOCK + RUN * (lane >> 4);  // run r of the lane begins at o + 4 RUN r
     if (block >= a.NB) return 0;
 #pragma unroll
     for (int m = 0; m < MC; ++m) {
@@ -462,28 +474,24 @@ __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<TM> &it
             if (live) {
                 uint4 *q = reinterpret_cast<uint4 *>(a.y_q + (size_t)row * a.y_q_stride + o);
                 q[0] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
-                q[1] = make_uint4(codes[4], codes[5], codes[6], codes[7]);
+                q[4] = make_uint4(codes[4], codes[5], codes[6], codes[7]);
                 if (lane < 16) a.y_scale[(size_t)block * a.y_scale_stride + row] = scale;
             }
         } else if (live) {
-            if constexpr (VEC) {
-                typedef Y Yx4 __attribute__((ext_vector_type(4)));
-                Y *p = reinterpret_cast<Y *>(a.y) + (size_t)row * a.y_stride + o;
+            if constexpr (VEC && sizeof(Y) == 2) {
+                typedef Y Yx8 __attribute__((ext_vector_type(8), aligned(8)));
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
-                    if constexpr (sizeof(Y) == 2) {
-                        typedef Y Yx8 __attribute__((ext_vector_type(8), aligned(8)));
-                        const floatx4 u = acc[i][m], v = acc[i + 1][m];
-                        if (o + 4 * i + 4 < a.n_out) *reinterpret_cast<Yx8 *>(p + 4 * i) = Yx8{(Y)u[0], (Y)u[1], (Y)u[2], (Y)u[3], (Y)v[0], (Y)v[1], (Y)v[2], (Y)v[3]};
-                        else if (o + 4 * i < a.n_out) *reinterpret_cast<Yx4 *>(p + 4 * i) = Yx4{(Y)u[0], (Y)u[1], (Y)u[2], (Y)u[3]};
-                    } else {
-                        store_four<Y, true>(a, row, o + 4 * i, acc[i][m]);
-                        store_four<Y, true>(a, row, o + 4 * i + 4, acc[i + 1][m]);
-                    }
+                    const int at = o + 16 * i;
+                    const floatx4 u = acc[i][m], v = acc[i + 1][m];
+                    if (at + 4 < a.n_out)
+                        *reinterpret_cast<Yx8 *>(reinterpret_cast<Y *>(a.y) + (size_t)row * a.y_stride + at) =
+                            Yx8{(Y)u[0], (Y)u[1], (Y)u[2], (Y)u[3], (Y)v[0], (Y)v[1], (Y)v[2], (Y)v[3]};
+                    else store_four<Y, true>(a, row, at, u);
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) store_four<Y, false>(a, row, o + 4 * i, acc[i][m]);
+                for (int i = 0; i < 8; ++i) store_four<Y, VEC>(a, row, o + 4 * RUN * (4 * i / RUN) + 4 * i % RUN, acc[i][m]);
             }
         }
     }
