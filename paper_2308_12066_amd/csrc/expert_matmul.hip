@@ -203,6 +203,14 @@ struct MatmulRing {
 };
 constexpr int TILE_THREADS = 512, TILE_GROUPS = 256;  // workgroups: one per CU
 
+// The lane's number, worked out where it is asked for: what depends on it is then not kept in registers across the products, where
+// every register is in use (one value reloaded from scratch memory is a wait for all requests before it).
+__device__ inline int lane_again() {
+    int lane;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+    return lane;
+}
+
 // The items of a launch, looked up in a table of the experts in LDS: chunks up to and with the expert, its first row, its rows, rows of a chunk.
 // The chunks of an expert are its rows dealt evenly, in whole 16s, to as few chunks of at most 64 u rows as hold them.  u is the one
 // of 1 .. TM for which the launch should end first: rounds of one item a workgroup, times what a block of inputs costs an
@@ -275,7 +283,7 @@ struct MatmulItems {
     __device__ MatmulItem at(int i) const {
         const int turn = i >> 3, group = turn / cols, chunk = group * 8 + (i & 7);
         if (chunk >= total) return {0, 0, 0, 0};
-        const intx4 c = *reinterpret_cast<const intx4 *>(table + 4 * (threadIdx.x & 63));
+        const intx4 c = *reinterpret_cast<const intx4 *>(table + 4 * lane_again());
         int e = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) e += __popcll(__ballot(c[q] <= chunk));
@@ -286,8 +294,7 @@ struct MatmulItems {
     }
 };
 
-// What a wavefront requests: the blocks of its workgroup's items one after the other.  What a lane adds to the addresses is worked out
-// for each request: in registers across the products it would push accumulators out of them.
+// What a wavefront requests: the blocks of its workgroup's items one after the other.
 template <int TM>
 struct MatmulRequests {
     typedef MatmulRing<TM> R;
@@ -304,7 +311,7 @@ struct MatmulRequests {
         stage = 0;
     }
     __device__ void next(const MatmulArgs &a, const MatmulItems<TM> &items, int wave) {
-        const int lane = threadIdx.x & 63;
+        const int lane = lane_again();
         if (left == 0) {  // uniform
             const MatmulItem it = items.at(item);
             if (it.nrows == 0) return;
@@ -360,16 +367,9 @@ template <int XQ, int TM, int MC, int RUN, int STORES>
 __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const char *ring, unsigned &stage, int wave, int stored,
                                      floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
     typedef MatmulRing<TM> R;
-    const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
-    const int g = lane >> 4, i16 = lane & 15;
-    // the output of product t, in 16ths of the wavefront's 128: lane's place for t = 0 and what t adds
+    const int wn = wave & 1, wm = wave >> 1;
     constexpr int PER = RUN / 4;  // products of a run
-    const int o0 = RUN * (i16 >> 2) + (i16 & 3);
-    const char *w_at = ring + (wn * 8 + (o0 >> 4)) * MATMUL_W_TILE + (o0 & 15) * 16 + g * 256;
     auto place = [](int t) { return t / PER * PER * MATMUL_W_TILE + t % PER * 64; };
-    const char *x_at = ring + R::W + (wm * 16 + i16) * FP8_BLOCK;
-    const int x_low = (g ^ (i16 >> 1)) << 4, x_high = ((4 + g) ^ (i16 >> 1)) << 4;
-    const char *s_at = ring + R::W + R::X;
     for (int kb = 0; kb < a.KB; ++kb) {
         // This block's loads have landed: those of the later ones, and stores behind them all, may be outstanding.
         const bool two = R::NS > 2 && rq.ahead > 1;
@@ -379,6 +379,12 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> 
         rq.next(a, items, wave);
         --rq.ahead;
         if (MC > 0) {
+            const int lane = lane_again(), g = lane >> 4, i16 = lane & 15;
+            const int o0 = RUN * (i16 >> 2) + (i16 & 3);  // this lane's output of product 0
+            const char *w_at = ring + (wn * 8 + (o0 >> 4)) * MATMUL_W_TILE + (o0 & 15) * 16 + g * 256;
+            const char *x_at = ring + R::W + (wm * 16 + i16) * FP8_BLOCK;
+            const int x_low = (g ^ (i16 >> 1)) << 4, x_high = ((4 + g) ^ (i16 >> 1)) << 4;
+            const char *s_at = ring + R::W + R::X;
             Operand x[MC > 0 ? MC : 1];
             float s[MC > 0 ? MC : 1];
             const float sw = *reinterpret_cast<const float *>(s_at + stage + 4 * 256 + wn * 4);
@@ -388,28 +394,61 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> 
                 x[m] = operand<XQ>(*reinterpret_cast<const intx4 *>(r + x_low), *reinterpret_cast<const intx4 *>(r + x_high));
                 s[m] = sw * *reinterpret_cast<const float *>(s_at + stage + ((wm + 4 * m) * 16 + i16) * 4);
             }
-            // one output tile's codes are read while the one before is multiplied; nothing may move further ahead, for want of registers
-            intx4 low = *reinterpret_cast<const intx4 *>(w_at + stage), high = *reinterpret_cast<const intx4 *>(w_at + stage + 1024);
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
+            // Half a step is the products of one output tile and two row tiles.  Beside them run what the half before left to do (its sums into the
+            // accumulators) and half of the next output tile's conversion, dealt out behind the products one by one: the vector
+            // unit's work fits under the matrix cores' then, in a wavefront by itself.
+            constexpr int HALVES = MC > 2 ? 2 : 1, HM = MC > 1 ? 2 : 1;
+            Operand w = operand<PGMOE_E4M3>(*reinterpret_cast<const intx4 *>(w_at + stage), *reinterpret_cast<const intx4 *>(w_at + stage + 1024)), w_next;
+            intx4 low = *reinterpret_cast<const intx4 *>(w_at + stage + place(1)), high;
+            floatx4 before[HM];
+            static_for<8 * HALVES>([&](auto step_) {
+                constexpr int step = decltype(step_)::value, t = step / HALVES, h = step % HALVES;
                 __builtin_amdgcn_sched_barrier(0);
-                const Operand w = operand<PGMOE_E4M3>(low, high);
-                if (t < 7) {
-                    const char *c = w_at + stage + place(t + 1);
-                    low = *reinterpret_cast<const intx4 *>(c);
-                    high = *reinterpret_cast<const intx4 *>(c + 1024);
+                floatx4 p[HM];
+#pragma unroll
+                for (int j = 0; j < HM; ++j) p[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < HM; ++j)
+                        if (2 * h + j < MC) p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.part[i], x[2 * h + j].part[i], p[j], 0, 0, 0);
+                if constexpr (step > 0) {
+                    constexpr int tb = (step - 1) / HALVES, hb = (step - 1) % HALVES;
+#pragma unroll
+                    for (int j = 0; j < HM; ++j)
+                        if (2 * hb + j < MC) {
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[tb][2 * hb + j][v] = fmaf(s[2 * hb + j], before[j][v], acc[tb][2 * hb + j][v]);
+                        }
                 }
-                floatx4 p[MC > 0 ? MC : 1];
+                if constexpr (t < 7) {
+                    if constexpr (h == 0) {
+                        w_next.part[0] = widen<PGMOE_E4M3>(low[0], low[1]);
+                        w_next.part[1] = widen<PGMOE_E4M3>(low[2], low[3]);
+                        high = *reinterpret_cast<const intx4 *>(w_at + stage + place(t + 1) + 1024);
+                    }
+                    if constexpr (h == HALVES - 1) {
+                        w_next.part[2] = widen<PGMOE_E4M3>(high[0], high[1]);
+                        w_next.part[3] = widen<PGMOE_E4M3>(high[2], high[3]);
+                        if constexpr (t < 6) low = *reinterpret_cast<const intx4 *>(w_at + stage + place(t + 2));
+                    }
+                }
 #pragma unroll
-                for (int m = 0; m < MC; ++m) p[m] = product(w, x[m]);
+                for (int i = 0; i < 4 * HM; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);   // a product
+                    __builtin_amdgcn_sched_group_barrier(0x2, HALVES == 1 ? 3 : 2, 0);  // what runs beside it
+                }
 #pragma unroll
-                for (int m = 0; m < MC; ++m)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[t][m][v] = fmaf(s[m], p[m][v], acc[t][m][v]);
-#pragma unroll
-                for (int m = 0; m < MC; ++m) asm volatile("" : "+v"(acc[t][m]));  // here, not behind the loop's last branch with every p alive
-            }
+                for (int j = 0; j < HM; ++j) before[j] = p[j];
+                if constexpr (h == HALVES - 1) w = w_next;
+            });
             __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < HM; ++j)
+                if (2 * (HALVES - 1) + j < MC) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[7][2 * (HALVES - 1) + j][v] = fmaf(s[2 * (HALVES - 1) + j], before[j][v], acc[7][2 * (HALVES - 1) + j][v]);
+                }
         }
         stage = stage + R::STAGE == R::NS * R::STAGE ? 0 : stage + R::STAGE;
     }
@@ -437,7 +476,7 @@ __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<TM> &it
 #pragma unroll
         for (int m = 0; m < MC; ++m) acc[i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
     matmul_k_loop<XQ, TM, MC, RUN, STORES>(a, items, rq, ring, stage, wave, stored, acc);
-    const int lane = threadIdx.x & 63, wn = wave & 1, wm = wave >> 1;
+    const int lane = lane_again(), wn = wave & 1, wm = wave >> 1;
     const int block = it.nb + wn, o = block * FP8_BLOCK + RUN * (lane >> 4);  // run r of the lane begins at o + 4 RUN r
     if (block >= a.NB) return 0;
 #pragma unroll
