@@ -9,6 +9,7 @@
 // depend on how exp and the sums were rounded; so the chosen neighbours (and the two groups at the border) are looked at
 // once more, and a token where two of them lie closer than CLOSE is selected again with everything in 64 bits.
 // Values that are equal because logit and bias are equal are no such case: both ways the lowest index wins.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -60,20 +61,42 @@ struct Keys<double> {
 // below every value: taken, outside the kept groups, unavailable (in rising order, from Keys::lowest)
 enum { KEY_TAKEN = 0, KEY_OUTSIDE = 1, KEY_UNAVAILABLE = 2 };
 
+// Reductions over the 16 lanes of a token (a row of the wavefront): rotations by 8, 4, 2 and 1 inside the row, which the vector unit
+// does on the way (a shuffle through LDS takes some hundred clocks, and a selection is a chain of them).
+template <int CTRL>
+__device__ inline int row_moved(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false);
+}
+template <int CTRL>
+__device__ inline float row_moved(float v) {
+    return __int_as_float(row_moved<CTRL>(__float_as_int(v)));
+}
+template <int CTRL>
+__device__ inline int64_t row_moved(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)row_moved<CTRL>((int)v) | (uint64_t)(uint32_t)row_moved<CTRL>((int)(v >> 32)) << 32);
+}
+template <int CTRL>
+__device__ inline double row_moved(double v) {
+    return __longlong_as_double(row_moved<CTRL>((int64_t)__double_as_longlong(v)));
+}
+template <typename V, typename F>
+__device__ inline V lanes_reduce(V v, F f) {
+    v = f(v, row_moved<0x128>(v));  // row_ror:8
+    v = f(v, row_moved<0x124>(v));
+    v = f(v, row_moved<0x122>(v));
+    return f(v, row_moved<0x121>(v));
+}
 template <typename V>
 __device__ inline V lanes_sum(V v) {
-#pragma unroll
-    for (int m = 1; m < ROUTE_LANES; m <<= 1) v += __shfl_xor(v, m);
-    return v;
+    return lanes_reduce(v, [](V a, V b) { return a + b; });
 }
 template <typename V>
 __device__ inline V lanes_max(V v) {
-#pragma unroll
-    for (int m = 1; m < ROUTE_LANES; m <<= 1) {
-        const V o = __shfl_xor(v, m);
-        v = o > v ? o : v;
-    }
-    return v;
+    return lanes_reduce(v, [](V a, V b) { return b > a ? b : a; });
+}
+template <typename V>
+__device__ inline V lanes_min(V v) {
+    return lanes_reduce(v, [](V a, V b) { return b < a ? b : a; });
 }
 
 // What the lanes of a wavefront wrote to LDS is there for its other lanes behind this (they run in lockstep and LDS
@@ -85,8 +108,16 @@ __device__ inline void wave_sync() {
 
 __device__ inline bool available(float z) { return z > -INFINITY; }  // false for NaN too
 
-__device__ inline float exp_of(float x) { return expf(x); }
+// exp(x), x <= 0 or any finite: 2^t with the rest of the product by log2 e put back, three half-steps of 2^-24 from exact.
+// Results below 2^-126 may be 0.
+__device__ inline float exp_of(float x) {
+    const float t = x * 1.44269502f, rest = fmaf(x, 1.92596303e-8f, fmaf(x, 1.44269502f, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fabsf(t) < 200.f ? fmaf(e, rest * 0.693147182f, e) : e;  // beyond, 0 or infinity (and no infinity less infinity)
+}
+__device__ inline float inverse_of(float x) { return __builtin_amdgcn_rcpf(x); }  // one step of 2^-24
 __device__ inline double exp_of(double x) { return exp(x); }
+__device__ inline double inverse_of(double x) { return 1.0 / x; }
 // exp(z - m), 1 at the largest of infinite logits
 template <typename V>
 __device__ inline V exp_below(float z, float m) {
@@ -94,7 +125,7 @@ __device__ inline V exp_below(float z, float m) {
 }
 template <typename V>
 __device__ inline V sigmoid(float z) {
-    return V(1) / (V(1) + exp_of(-V(z)));
+    return inverse_of(V(1) + exp_of(-V(z)));
 }
 
 template <typename L>
@@ -102,13 +133,39 @@ __device__ inline float logit_at(const RouteArgs &a, size_t t, int e) {
     return (float)reinterpret_cast<const L *>(a.logits)[t * a.stride + e];
 }
 
-// This lane's logits of token t; unavailable (-infinity) past the last expert.
-template <typename L, int PER>
+// This lane's logits of token t; unavailable (-infinity) past the last expert.  VEC: all PER exist, at an address that their bytes (or 16) divide.
+template <bool VEC, typename L, int PER>
 __device__ inline void load_logits(const L *row, int E, int first, float (&z)[PER]) {
+    if (VEC) {
+        constexpr int N = PER * sizeof(L) > 16 ? 16 / sizeof(L) : PER;
+        typedef L Lx __attribute__((ext_vector_type(N)));
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const float v = (float)row[min(first + i, E - 1)];
-        z[i] = first + i < E && available(v) ? v : -INFINITY;
+        for (int i = 0; i < PER; i += N) {
+            const Lx v = *reinterpret_cast<const Lx *>(row + (first < E ? first : 0) + i);
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[i + j] = (float)v[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) z[i] = (float)row[min(first + i, E - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) z[i] = first + i < E && available(z[i]) ? z[i] : -INFINITY;
+}
+
+template <bool VEC, int PER>
+__device__ inline void load_floats(const float *row, int E, int first, float (&v)[PER]) {
+    typedef float floatx4 __attribute__((ext_vector_type(4)));
+    if (VEC && PER % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < PER; i += 4) {
+            const floatx4 x = *reinterpret_cast<const floatx4 *>(row + (first < E ? first : 0) + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i + j] = x[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = row[min(first + i, E - 1)];
     }
 }
 
@@ -126,16 +183,16 @@ __device__ inline void scores_of(const float (&z)[PER], float m, V (&s)[PER]) {
             sum += s[i];
         }
         sum = lanes_sum(sum);
-        const V inv = sum > V(0) ? V(1) / sum : V(0);
+        const V inv = sum > V(0) ? inverse_of(sum) : V(0);
 #pragma unroll
         for (int i = 0; i < PER; ++i) s[i] *= inv;
     }
 }
 
 // Selects the k experts of one token into chosen[0 .. k).  Returns whether 32 bits may have decided it (V = float only).
-// shared: at least n_experts V of this token, used with groups only.
-template <typename V, bool SIGMOID, int PER>
-__device__ bool select_experts(const RouteArgs &a, const float (&z)[PER], const float (&b)[PER], int first, int lane, float m, V *shared, int32_t *chosen) {
+// chosen: 2 k + 2 places of this token.  shared: n_experts V of it, used with groups only.  same(e, f): have both the same logit and bias?
+template <typename V, bool SIGMOID, int PER, typename S>
+__device__ bool select_experts(const RouteArgs &a, const float (&z)[PER], const float (&b)[PER], int first, int lane, float m, V *shared, int32_t *chosen, S same) {
     typedef typename Keys<V>::T Key;
     constexpr Key low = Keys<V>::lowest;
     const bool by_score = a.bias || a.n_groups > 1;
@@ -155,42 +212,59 @@ __device__ bool select_experts(const RouteArgs &a, const float (&z)[PER], const 
             key[i] = first + i >= a.E ? low + KEY_TAKEN : available(z[i]) ? of : low + KEY_UNAVAILABLE;
         }
         if (a.n_groups > 1) {
-            // the group's worth: lane g adds up group g
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (first + i < a.E) shared[first + i] = available(z[i]) ? v[i] : -(V)INFINITY;
-            wave_sync();
+            // The worth of a group: 16 / n_groups lanes, a power of two, look for the two largest of a part of it each.
             const int size = a.E / a.n_groups;
+            int part = 1;
+            while (part * 2 * a.n_groups <= ROUTE_LANES) part *= 2;
+            const int mine = lane / part;
+            V one = -(V)INFINITY, two = -(V)INFINITY;
+            auto take = [&](V x) {
+                const V low_one = x > one ? one : x;
+                one = x > one ? x : one;
+                two = low_one > two ? low_one : two;
+            };
+            if (size == part * PER) {  // which are this lane's own
+#pragma unroll
+                for (int i = 0; i < PER; ++i) take(available(z[i]) ? v[i] : -(V)INFINITY);
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (first + i < a.E) shared[first + i] = available(z[i]) ? v[i] : -(V)INFINITY;
+                wave_sync();
+                if (mine < a.n_groups) {
+                    const int from = size * (lane - mine * part) / part, to = size * (lane - mine * part + 1) / part;
+                    for (int j = from; j < to; ++j) take(shared[mine * size + j]);
+                }
+            }
+            for (int m = 1; m < part; m <<= 1) {
+                const V other_two = __shfl_xor(two, m);
+                take(__shfl_xor(one, m));
+                take(other_two);
+            }
             Key worth = low;
             V value = -(V)INFINITY;
-            if (lane < a.n_groups) {
-                V one = -(V)INFINITY, two = -(V)INFINITY;
-                for (int j = 0; j < size; ++j) {
-                    const V x = shared[lane * size + j];
-                    two = x > one ? one : (x > two ? x : two);
-                    one = x > one ? x : one;
-                }
+            if (mine < a.n_groups) {
                 value = two > -(V)INFINITY ? one + two : one;
                 worth = value > -(V)INFINITY ? Keys<V>::of(value) : low;
             }
-            // kept: fewer than `keep` groups are worthier, or as worthy and lower
+            // kept: fewer than `keep` groups are worthier, or as worthy and lower (all lanes of a group say the same)
             int above = 0;
             for (int g = 0; g < a.n_groups; ++g) {
-                const Key o = __shfl(worth, (threadIdx.x & 48) + g);
-                above += o > worth || (o == worth && g < lane) ? 1 : 0;
+                const Key o = __shfl(worth, (threadIdx.x & 48) + g * part);
+                above += o > worth || (o == worth && g < mine) ? 1 : 0;
             }
-            const bool kept = lane < a.n_groups && above < a.keep;
+            const bool kept = mine < a.n_groups && above < a.keep;
             if (sizeof(V) == 4 && a.keep < a.n_groups) {
                 // the worst kept against the best other
                 const float inside = -lanes_max(kept ? -(float)value : -INFINITY);
-                const float outside = lanes_max(lane < a.n_groups && !kept && worth > low ? (float)value : -INFINITY);
+                const float outside = lanes_max(mine < a.n_groups && !kept && worth > low ? (float)value : -INFINITY);
                 close = outside > -INFINITY && !(inside - outside > CLOSE * fmaxf(fabsf(inside), 6e-8f));
             }
             const unsigned mask = (unsigned)(__ballot(kept) >> (threadIdx.x & 48)) & 0xffffu;
             int g = first / size, in_group = first - g * size;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                if (first + i < a.E && !((mask >> g) & 1)) key[i] = low + KEY_OUTSIDE;
+                if (first + i < a.E && !((mask >> (g * part)) & 1)) key[i] = low + KEY_OUTSIDE;
                 if (++in_group == size) {
                     in_group = 0;
                     ++g;
@@ -201,56 +275,46 @@ __device__ bool select_experts(const RouteArgs &a, const float (&z)[PER], const 
     // one further than asked for, to compare the last chosen with the first that is not
     const bool look = sizeof(V) == 4 && a.bias;
     const int rounds = look ? min(a.k + 1, a.E) : a.k;
-    Key before = 0;
-    float z_before = 0.f, b_before = 0.f;
     for (int j = 0; j < rounds; ++j) {
         Key best = key[0];
 #pragma unroll
         for (int i = 1; i < PER; ++i) best = key[i] > best ? key[i] : best;
         const Key top = lanes_max(best);
-        const unsigned holders = (unsigned)(__ballot(best == top) >> (threadIdx.x & 48)) & 0xffffu;
-        const int owner = __ffs(holders) - 1;
-        float z_won = 0.f, b_won = 0.f;
-        if (lane == owner) {
-            bool found = false;
+        int won = INT_MAX;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const bool it = !found && key[i] == top;
-                if (it) {
-                    if (j < a.k) chosen[j] = first + i;
-                    key[i] = low + KEY_TAKEN;
-                    z_won = z[i];
-                    b_won = b[i];
-                }
-                found |= it;
-            }
+        for (int i = PER - 1; i >= 0; --i) won = key[i] == top ? first + i : won;
+        won = lanes_min(won);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) key[i] = first + i == won ? low + KEY_TAKEN : key[i];
+        if (lane == 0) {
+            chosen[j] = won;
+            if (look) reinterpret_cast<int32_t *>(chosen + a.k + 1)[j] = (int32_t)top;
         }
-        if (look) {
-            z_won = __shfl(z_won, (threadIdx.x & 48) + owner);
-            b_won = __shfl(b_won, (threadIdx.x & 48) + owner);
-            if (j > 0 && top > low + KEY_UNAVAILABLE && !(z_won == z_before && b_won == b_before)) {
-                const float hi = Keys<float>::value((int32_t)before), lo = Keys<float>::value((int32_t)top);
-                close |= !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f)) && lo > -INFINITY;
-            }
-            before = top;
-            z_before = z_won;
-            b_before = b_won;
+    }
+    if (look) {
+        wave_sync();
+        const int32_t *keys = chosen + a.k + 1;
+        for (int j = lane; j + 1 < rounds; j += ROUTE_LANES) {
+            const float hi = Keys<float>::value(keys[j]), lo = Keys<float>::value(keys[j + 1]);
+            if (keys[j + 1] > INT_MIN + KEY_UNAVAILABLE && lo > -INFINITY && !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f)))
+                close |= !same(chosen[j], chosen[j + 1]);
         }
+        close = lanes_max(close ? 1 : 0);
     }
     return close;
 }
 
-template <typename L, bool SIGMOID, int PER>
+template <typename L, bool SIGMOID, int PER, bool VEC>
 __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const RouteArgs a) {
     extern __shared__ char lds[];
     const int lane = threadIdx.x & (ROUTE_LANES - 1), token = threadIdx.x / ROUTE_LANES;
     const size_t t = (size_t)blockIdx.x * ROUTE_TOKENS + token;
     if (t >= (size_t)a.T) return;  // whole rows of 16 lanes; no workgroup barrier below
-    int32_t *chosen = reinterpret_cast<int32_t *>(lds) + token * a.k;
-    double *shared = reinterpret_cast<double *>(lds + ((ROUTE_TOKENS * a.k * 4 + 15) & ~15)) + (a.n_groups > 1 ? token * a.E : 0);
+    int32_t *chosen = reinterpret_cast<int32_t *>(lds) + token * (2 * a.k + 2);
+    double *shared = reinterpret_cast<double *>(lds + ROUTE_TOKENS * (2 * a.k + 2) * 4) + token * a.E;  // there where groups straddle lanes
     const int first = lane * PER;
     float z[PER], b[PER];
-    load_logits<L, PER>(reinterpret_cast<const L *>(a.logits) + t * a.stride, a.E, first, z);
+    load_logits<VEC>(reinterpret_cast<const L *>(a.logits) + t * a.stride, a.E, first, z);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const float v = a.bias && first + i < a.E ? a.bias[first + i] : 0.f;
@@ -261,9 +325,13 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
     for (int i = 1; i < PER; ++i) m = fmaxf(m, z[i]);
     m = lanes_max(m);
 
-    if (select_experts<float, SIGMOID, PER>(a, z, b, first, lane, m, reinterpret_cast<float *>(shared), chosen)) {
+    auto same = [&](int e, int f) {
+        const float be = a.bias[e], bf = a.bias[f];
+        return logit_at<L>(a, t, e) == logit_at<L>(a, t, f) && be == bf;
+    };
+    if (select_experts<float, SIGMOID, PER>(a, z, b, first, lane, m, reinterpret_cast<float *>(shared), chosen, same)) {
         wave_sync();
-        select_experts<double, SIGMOID, PER>(a, z, b, first, lane, m, shared, chosen);
+        select_experts<double, SIGMOID, PER>(a, z, b, first, lane, m, shared, chosen, same);
     }
     wave_sync();
 
@@ -331,7 +399,7 @@ struct RouteBackwardArgs {
 // belongs to the lane that holds that expert.  Renormalised, with r_j = s_j / total,
 //   s_j d_s[j] = c r_j (d_w[j] - sum_i d_w[i] r_i),
 // whose sum over j is 0: softmax's common term has nothing of it, and r is taken as in the forward kernel.
-template <typename L, bool SIGMOID, int PER>
+template <typename L, bool SIGMOID, int PER, bool VEC>
 __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_backward_kernel(const RouteBackwardArgs a) {
     extern __shared__ float parts[];
     const int lane = threadIdx.x & (ROUTE_LANES - 1), token = threadIdx.x / ROUTE_LANES;
@@ -348,7 +416,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_backward_kernel(co
         s[i] = 0.f;
     }
     if (every) {
-        load_logits<L, PER>(row, a.E, first, z);
+        load_logits<VEC>(row, a.E, first, z);
         if (!SIGMOID) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) m = fmaxf(m, z[i]);
@@ -408,19 +476,37 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_backward_kernel(co
         atomicAdd(&part[e], d);
     }
     float ds[PER];
+    if (a.d_scores) load_floats<VEC>(a.d_scores + t * a.E, a.E, first, ds);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        ds[i] = a.d_scores && s[i] > 0.f ? a.d_scores[t * a.E + first + i] : 0.f;
+        ds[i] = a.d_scores && s[i] > 0.f ? ds[i] : 0.f;
         if (!SIGMOID) common += s[i] * ds[i];
     }
     if (!SIGMOID && every) common = lanes_sum(common);
     wave_sync();
-    L *out = reinterpret_cast<L *>(a.d_logits) + t * a.d_stride;
+    float d[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        float d = part[first + i];
-        if (every && s[i] > 0.f) d += SIGMOID ? s[i] * sigmoid<float>(-z[i]) * ds[i] : s[i] * (ds[i] - common);
-        if (first + i < a.E) out[first + i] = (L)d;
+        d[i] = part[first + i];
+        if (every && s[i] > 0.f) d[i] += SIGMOID ? s[i] * sigmoid<float>(-z[i]) * ds[i] : s[i] * (ds[i] - common);
+    }
+    L *out = reinterpret_cast<L *>(a.d_logits) + t * a.d_stride + first;
+    if (VEC) {
+        constexpr int N = PER * sizeof(L) > 16 ? 16 / sizeof(L) : PER;
+        typedef L Lx __attribute__((ext_vector_type(N)));
+        if (first < a.E) {
+#pragma unroll
+            for (int i = 0; i < PER; i += N) {
+                Lx v;
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = (L)d[i + j];
+                *reinterpret_cast<Lx *>(out + i) = v;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (first + i < a.E) out[i] = (L)d[i];
     }
 }
 
@@ -442,19 +528,34 @@ static int check_router(const pgmoe_router *r, const char *fn) {
     return PGMOE_OK;
 }
 
-// The instantiation for a type of logits, a score and a number of experts: KERNEL<L, SIGMOID, PER>.
-#define ROUTE_LAUNCH_PER(KERNEL, L, SIG, PER, ...)                     \
-    do {                                                               \
-        constexpr int per_ = PER;                                      \
-        hipLaunchKernelGGL((KERNEL<L, SIG, per_>), __VA_ARGS__);       \
+// Experts a lane holds.
+static int route_per(int E) {
+    int per = 1;
+    while (per * ROUTE_LANES < E) per *= 2;
+    return per;
+}
+// Do all lanes that hold experts hold PER of them, at addresses of whole loads?
+static bool route_vec(const pgmoe_router *r, const void *rows, int64_t stride) {
+    const int per = route_per(r->n_experts);
+    const size_t bytes = std::min<size_t>(16, per * dtype_bytes(r->logits_dtype));
+    return r->n_experts % per == 0 && aligned(rows, bytes) && stride * dtype_bytes(r->logits_dtype) % bytes == 0;
+}
+
+// The instantiation for a type of logits, a score, a number of experts and the form of the loads: KERNEL<L, SIGMOID, PER, VEC>.
+#define ROUTE_LAUNCH_PER(KERNEL, L, SIG, PER, vec, ...)                                      \
+    do {                                                                                     \
+        if (vec) hipLaunchKernelGGL((KERNEL<L, SIG, PER, true>), __VA_ARGS__);               \
+        else hipLaunchKernelGGL((KERNEL<L, SIG, PER, false>), __VA_ARGS__);                  \
     } while (0)
-#define ROUTE_LAUNCH_E(KERNEL, L, SIG, E, ...)                                          \
-    do {                                                                                \
-        if ((E) <= 16) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 1, __VA_ARGS__);                \
-        else if ((E) <= 32) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 2, __VA_ARGS__);           \
-        else if ((E) <= 64) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 4, __VA_ARGS__);           \
-        else if ((E) <= 128) ROUTE_LAUNCH_PER(KERNEL, L, SIG, 8, __VA_ARGS__);          \
-        else ROUTE_LAUNCH_PER(KERNEL, L, SIG, 16, __VA_ARGS__);                         \
+#define ROUTE_LAUNCH_E(KERNEL, L, SIG, E, ...)                                               \
+    do {                                                                                     \
+        switch (route_per(E)) {                                                              \
+        case 1: ROUTE_LAUNCH_PER(KERNEL, L, SIG, 1, __VA_ARGS__); break;                     \
+        case 2: ROUTE_LAUNCH_PER(KERNEL, L, SIG, 2, __VA_ARGS__); break;                     \
+        case 4: ROUTE_LAUNCH_PER(KERNEL, L, SIG, 4, __VA_ARGS__); break;                     \
+        case 8: ROUTE_LAUNCH_PER(KERNEL, L, SIG, 8, __VA_ARGS__); break;                     \
+        default: ROUTE_LAUNCH_PER(KERNEL, L, SIG, 16, __VA_ARGS__);                          \
+        }                                                                                    \
     } while (0)
 #define ROUTE_LAUNCH(KERNEL, r, ...)                                                                     \
     do {                                                                                                 \
@@ -494,10 +595,14 @@ int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_s
     const int groups = router->n_groups ? router->n_groups : 1, keep = router->topk_groups ? router->topk_groups : groups;
     const RouteArgs a = {logits, (size_t)logits_stride, bias, T, router->n_experts, router->top_k, groups, keep, router->renormalize,
                          router->scale, topk_idx, topk_weight, scores_out};
-    // at most 16 tokens x (256 indices of 4 bytes + 256 values of 8) = 48 KiB
-    const size_t lds = ((ROUTE_TOKENS * a.k * 4 + 15) & ~15) + (groups > 1 ? (size_t)ROUTE_TOKENS * a.E * 8 : 0);
+    // 16 tokens x (2 k + 2 words, and n_experts values of 8 bytes where groups straddle lanes, which 256 experts' never do): below 64 KiB
+    int part = 1;
+    while (part * 2 * groups <= ROUTE_LANES) part *= 2;
+    const bool straddle = groups > 1 && a.E / groups != part * route_per(a.E);
+    const size_t lds = (size_t)ROUTE_TOKENS * ((2 * a.k + 2) * 4 + (straddle ? a.E * 8 : 0));
+    const bool vec = route_vec(router, logits, logits_stride);
     const dim3 grid((T + ROUTE_TOKENS - 1) / ROUTE_TOKENS), block(ROUTE_THREADS);
-    ROUTE_LAUNCH(route_logits_kernel, router, grid, block, lds, (hipStream_t)stream, a);
+    ROUTE_LAUNCH(route_logits_kernel, router, vec, grid, block, lds, (hipStream_t)stream, a);
     return launched(fn);
 }
 
@@ -521,11 +626,10 @@ int pgmoe_route_backward(const pgmoe_router *router, const void *logits, int64_t
     if (a0 < b1 && b0 < a1) return fail(nullptr, PGMOE_EINVAL, "%s: d_logits overlaps logits", fn);
     const RouteBackwardArgs a = {logits, (size_t)logits_stride, topk_idx, d_weight, d_scores, d_logits, (size_t)d_logits_stride,
                                  T, router->n_experts, router->top_k, router->renormalize, router->scale};
-    int per = 1;
-    while (per * ROUTE_LANES < a.E) per *= 2;
-    const size_t lds = (size_t)ROUTE_THREADS * per * 4;  // at most 16 KiB
+    const size_t lds = (size_t)ROUTE_THREADS * route_per(a.E) * 4;  // at most 16 KiB
     const dim3 grid((T + ROUTE_TOKENS - 1) / ROUTE_TOKENS), block(ROUTE_THREADS);
-    ROUTE_LAUNCH(route_logits_backward_kernel, router, grid, block, lds, (hipStream_t)stream, a);
+    const bool vec = route_vec(router, logits, logits_stride) && route_vec(router, d_logits, d_logits_stride) && aligned(d_scores, 16);
+    ROUTE_LAUNCH(route_logits_backward_kernel, router, vec, grid, block, lds, (hipStream_t)stream, a);
     return launched(fn);
 }
 
