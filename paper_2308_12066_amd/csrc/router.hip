@@ -28,6 +28,9 @@ struct RouteArgs {
     float scale;
     int32_t *idx;
     float *weight, *scores;
+    int straddle;  // groups that are not whole lanes
+    int capacity;
+    int lds;       // bytes of a token
 };
 
 constexpr int ROUTE_LANES = 16;                                // of one token
@@ -189,82 +192,124 @@ __device__ inline void scores_of(const float (&z)[PER], float m, V (&s)[PER]) {
     }
 }
 
-// Selects the k experts of one token into chosen[0 .. k).  Returns whether 32 bits may have decided it (V = float only).
-// chosen: 2 k + 2 places of this token.  shared: n_experts V of it, used with groups only.  same(e, f): have both the same logit and bias?
-template <typename V, bool SIGMOID, int PER, typename S>
-__device__ bool select_experts(const RouteArgs &a, const float (&z)[PER], const float (&b)[PER], int first, int lane, float m, V *shared, int32_t *chosen, S same) {
+// A token's places in LDS: what a selection leaves (experts and their keys, and, where 32 bits do not decide, 64-bit values), and
+// the experts' values where groups straddle lanes.
+struct RoutePlaces {
+    int32_t *chosen, *keys;  // [capacity]
+    double *exact;           // [capacity]
+    double *values;          // [n_experts]
+    int capacity;
+};
+constexpr int ROUTE_MORE = 32;  // candidates beyond the k that are looked at before all experts are
+
+// Which groups are kept, as a bit for each in the first of its lanes.  Returns whether 32 bits may have decided it (V = float only).
+template <typename V, int PER>
+__device__ bool keep_groups(const RouteArgs &a, const float (&z)[PER], const V (&v)[PER], int first, int lane, V *values, int part, unsigned *mask) {
     typedef typename Keys<V>::T Key;
     constexpr Key low = Keys<V>::lowest;
-    const bool by_score = a.bias || a.n_groups > 1;
-    bool close = false;
-    Key key[PER];
-    {
-        V v[PER];
-        if (by_score) {
-            scores_of<V, SIGMOID, PER>(z, m, v);
+    // The worth of a group: `part` lanes, the largest power of two there are for each, look for the two largest of a part of it each.
+    const int size = a.E / a.n_groups, mine = lane / part;
+    V one = -(V)INFINITY, two = -(V)INFINITY;
+    auto take = [&](V x) {
+        const V low_one = x > one ? one : x;
+        one = x > one ? x : one;
+        two = low_one > two ? low_one : two;
+    };
+    if (size == part * PER) {  // which are this lane's own
 #pragma unroll
-            for (int i = 0; i < PER; ++i) v[i] += V(b[i]);
+        for (int i = 0; i < PER; ++i) take(available(z[i]) ? v[i] : -(V)INFINITY);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (first + i < a.E) values[first + i] = available(z[i]) ? v[i] : -(V)INFINITY;
+        wave_sync();
+        if (mine < a.n_groups) {
+            const int from = size * (lane - mine * part) / part, to = size * (lane - mine * part + 1) / part;
+            for (int j = from; j < to; ++j) take(values[mine * size + j]);
+        }
+        wave_sync();
+    }
+    for (int m = 1; m < part; m <<= 1) {
+        const V other_two = __shfl_xor(two, m);
+        take(__shfl_xor(one, m));
+        take(other_two);
+    }
+    Key worth = low;
+    V value = -(V)INFINITY;
+    if (mine < a.n_groups) {
+        value = two > -(V)INFINITY ? one + two : one;
+        worth = value > -(V)INFINITY ? Keys<V>::of(value) : low;
+    }
+    // kept: fewer than `keep` groups are worthier, or as worthy and lower (all lanes of a group say the same)
+    int above = 0;
+    for (int g = 0; g < a.n_groups; ++g) {
+        const Key o = __shfl(worth, (threadIdx.x & 48) + g * part);
+        above += o > worth || (o == worth && g < mine) ? 1 : 0;
+    }
+    const bool kept = mine < a.n_groups && above < a.keep;
+    *mask = (unsigned)(__ballot(kept) >> (threadIdx.x & 48)) & 0xffffu;
+    if (sizeof(V) == 8 || a.keep == a.n_groups) return false;
+    // the worst kept against the best other
+    const float inside = -lanes_max(kept ? -(float)value : -INFINITY);
+    const float outside = lanes_max(mine < a.n_groups && !kept && worth > low ? (float)value : -INFINITY);
+    return outside > -INFINITY && !(inside - outside > CLOSE * fmaxf(fabsf(inside), 6e-8f));
+}
+
+// Takes the expert of the largest key: the lowest of those that have it.
+template <typename Key, int PER>
+__device__ inline int take_largest(Key (&key)[PER], int first, Key *top) {
+    constexpr Key lowest = sizeof(Key) == 4 ? (Key)Keys<float>::lowest : (Key)Keys<double>::lowest;
+    Key best = key[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) best = key[i] > best ? key[i] : best;
+    best = lanes_max(best);
+    int won = INT_MAX;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i) won = key[i] == best ? first + i : won;
+    won = lanes_min(won);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = first + i == won ? lowest + KEY_TAKEN : key[i];
+    *top = best;
+    return won;
+}
+
+// Selects the k experts of one token; returns where they are: at.chosen or at.keys.  logit(e): a logit of this token.
+template <bool SIGMOID, int PER, typename F>
+__device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PER], const float (&b)[PER], int first, int lane, float m, const RoutePlaces &at, F logit) {
+    int32_t key[PER];
+    unsigned outside = 0;  // of the kept groups, a bit an expert
+    {
+        float v[PER];
+        if (a.bias || a.n_groups > 1) {
+            scores_of<float, SIGMOID, PER>(z, m, v);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) v[i] += b[i];
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             // without a bias by the logit: scores rise with it, and it is exact
-            const Key of = a.bias ? Keys<V>::of(v[i]) : Keys<V>::of(V(z[i]));
-            key[i] = first + i >= a.E ? low + KEY_TAKEN : available(z[i]) ? of : low + KEY_UNAVAILABLE;
+            const int32_t of = Keys<float>::of(a.bias ? v[i] : z[i]);
+            key[i] = first + i >= a.E ? INT_MIN + KEY_TAKEN : available(z[i]) ? of : INT_MIN + KEY_UNAVAILABLE;
         }
         if (a.n_groups > 1) {
-            // The worth of a group: 16 / n_groups lanes, a power of two, look for the two largest of a part of it each.
-            const int size = a.E / a.n_groups;
             int part = 1;
             while (part * 2 * a.n_groups <= ROUTE_LANES) part *= 2;
-            const int mine = lane / part;
-            V one = -(V)INFINITY, two = -(V)INFINITY;
-            auto take = [&](V x) {
-                const V low_one = x > one ? one : x;
-                one = x > one ? x : one;
-                two = low_one > two ? low_one : two;
-            };
-            if (size == part * PER) {  // which are this lane's own
+            unsigned mask;
+            if (keep_groups<float, PER>(a, z, v, first, lane, reinterpret_cast<float *>(at.values), part, &mask)) {
+                double exact[PER];
+                scores_of<double, SIGMOID, PER>(z, m, exact);
 #pragma unroll
-                for (int i = 0; i < PER; ++i) take(available(z[i]) ? v[i] : -(V)INFINITY);
-            } else {
-#pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (first + i < a.E) shared[first + i] = available(z[i]) ? v[i] : -(V)INFINITY;
-                wave_sync();
-                if (mine < a.n_groups) {
-                    const int from = size * (lane - mine * part) / part, to = size * (lane - mine * part + 1) / part;
-                    for (int j = from; j < to; ++j) take(shared[mine * size + j]);
-                }
+                for (int i = 0; i < PER; ++i) exact[i] += (double)b[i];
+                keep_groups<double, PER>(a, z, exact, first, lane, at.values, part, &mask);
             }
-            for (int m = 1; m < part; m <<= 1) {
-                const V other_two = __shfl_xor(two, m);
-                take(__shfl_xor(one, m));
-                take(other_two);
-            }
-            Key worth = low;
-            V value = -(V)INFINITY;
-            if (mine < a.n_groups) {
-                value = two > -(V)INFINITY ? one + two : one;
-                worth = value > -(V)INFINITY ? Keys<V>::of(value) : low;
-            }
-            // kept: fewer than `keep` groups are worthier, or as worthy and lower (all lanes of a group say the same)
-            int above = 0;
-            for (int g = 0; g < a.n_groups; ++g) {
-                const Key o = __shfl(worth, (threadIdx.x & 48) + g * part);
-                above += o > worth || (o == worth && g < mine) ? 1 : 0;
-            }
-            const bool kept = mine < a.n_groups && above < a.keep;
-            if (sizeof(V) == 4 && a.keep < a.n_groups) {
-                // the worst kept against the best other
-                const float inside = -lanes_max(kept ? -(float)value : -INFINITY);
-                const float outside = lanes_max(mine < a.n_groups && !kept && worth > low ? (float)value : -INFINITY);
-                close = outside > -INFINITY && !(inside - outside > CLOSE * fmaxf(fabsf(inside), 6e-8f));
-            }
-            const unsigned mask = (unsigned)(__ballot(kept) >> (threadIdx.x & 48)) & 0xffffu;
+            const int size = a.E / a.n_groups;
             int g = first / size, in_group = first - g * size;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                if (first + i < a.E && !((mask >> (g * part)) & 1)) key[i] = low + KEY_OUTSIDE;
+                if (first + i < a.E && !((mask >> (g * part)) & 1)) {
+                    key[i] = INT_MIN + KEY_OUTSIDE;
+                    outside |= 1u << i;
+                }
                 if (++in_group == size) {
                     in_group = 0;
                     ++g;
@@ -272,46 +317,105 @@ __device__ bool select_experts(const RouteArgs &a, const float (&z)[PER], const 
             }
         }
     }
-    // one further than asked for, to compare the last chosen with the first that is not
-    const bool look = sizeof(V) == 4 && a.bias;
-    const int rounds = look ? min(a.k + 1, a.E) : a.k;
-    for (int j = 0; j < rounds; ++j) {
-        Key best = key[0];
-#pragma unroll
-        for (int i = 1; i < PER; ++i) best = key[i] > best ? key[i] : best;
-        const Key top = lanes_max(best);
-        int won = INT_MAX;
-#pragma unroll
-        for (int i = PER - 1; i >= 0; --i) won = key[i] == top ? first + i : won;
-        won = lanes_min(won);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) key[i] = first + i == won ? low + KEY_TAKEN : key[i];
+    // with a bias one further than asked for, to compare the last chosen with the first that is not
+    int n = a.bias ? min(a.k + 1, a.E) : a.k;
+    int32_t top = 0;
+    for (int j = 0; j < n; ++j) {
+        const int won = take_largest(key, first, &top);
         if (lane == 0) {
-            chosen[j] = won;
-            if (look) reinterpret_cast<int32_t *>(chosen + a.k + 1)[j] = (int32_t)top;
+            at.chosen[j] = won;
+            if (a.bias) at.keys[j] = top;
         }
     }
-    if (look) {
-        wave_sync();
-        const int32_t *keys = chosen + a.k + 1;
-        for (int j = lane; j + 1 < rounds; j += ROUTE_LANES) {
-            const float hi = Keys<float>::value(keys[j]), lo = Keys<float>::value(keys[j + 1]);
-            if (keys[j + 1] > INT_MIN + KEY_UNAVAILABLE && lo > -INFINITY && !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f)))
-                close |= !same(chosen[j], chosen[j + 1]);
+    if (!a.bias) return at.chosen;
+    wave_sync();
+    auto near = [&](int32_t upper, int32_t lower) {  // might the order be another in 64 bits?
+        const float hi = Keys<float>::value(upper), lo = Keys<float>::value(lower);
+        return lower > INT_MIN + KEY_UNAVAILABLE && lo > -INFINITY && !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f));
+    };
+    bool close = false;
+    for (int j = lane; j + 1 < n; j += ROUTE_LANES)
+        if (near(at.keys[j], at.keys[j + 1])) {
+            const int e = at.chosen[j], f = at.chosen[j + 1];
+            close |= logit(e) != logit(f) || !(a.bias[e] == a.bias[f]);
         }
-        close = lanes_max(close ? 1 : 0);
+    if (!lanes_max(close ? 1 : 0)) return at.chosen;
+
+    // all that may belong to the k: as many more as lie close to each other
+    int32_t last = at.keys[n - 1], before = n > 1 ? at.keys[n - 2] : last;
+    bool all = false;
+    while (n > a.k && n < a.E && near(before, last)) {
+        if (n == at.capacity) {
+            all = true;
+            break;
+        }
+        before = last;
+        const int won = take_largest(key, first, &last);
+        if (lane == 0) at.chosen[n] = won;
+        ++n;
     }
-    return close;
+    wave_sync();
+    if (all) {  // too many: all experts again, in 64 bits
+        double v[PER];
+        int64_t wide[PER], unused;
+        scores_of<double, SIGMOID, PER>(z, m, v);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            wide[i] = first + i >= a.E       ? Keys<double>::lowest + KEY_TAKEN
+                      : (outside >> i) & 1   ? Keys<double>::lowest + KEY_OUTSIDE
+                      : available(z[i])      ? Keys<double>::of(v[i] + (double)b[i])
+                                             : Keys<double>::lowest + KEY_UNAVAILABLE;
+        for (int j = 0; j < a.k; ++j) {
+            const int won = take_largest(wide, first, &unused);
+            if (lane == 0) at.chosen[j] = won;
+        }
+        return at.chosen;
+    }
+    double sum = 1.0;
+    if (!SIGMOID) {
+        sum = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < a.E; i += ROUTE_LANES) {
+            const float zi = i + lane < a.E ? logit(i + lane) : -INFINITY;
+            sum += available(zi) ? exp_below<double>(zi, m) : 0.0;
+        }
+        sum = lanes_sum(sum);
+    }
+    auto value = [&](int e) {
+        const float ze = logit(e), be = a.bias[e];
+        if (!available(ze) || !(be > -INFINITY)) return -(double)INFINITY;
+        return (SIGMOID ? sigmoid<double>(ze) : exp_below<double>(ze, m) / sum) + (double)be;
+    };
+    for (int j = lane; j < n; j += ROUTE_LANES) at.exact[j] = value(at.chosen[j]);
+    wave_sync();
+    for (int j = lane; j < n; j += ROUTE_LANES) {
+        const double x = at.exact[j];
+        const int e = at.chosen[j];
+        int rank = 0;
+        for (int i = 0; i < n; ++i) {
+            const double y = at.exact[i];
+            // equal ones by index; of those at -infinity the order found holds
+            rank += y > x || (y == x && (x > -(double)INFINITY ? at.chosen[i] < e : i < j)) ? 1 : 0;
+        }
+        at.keys[rank] = e;  // (the keys have been read)
+    }
+    wave_sync();
+    return at.keys;
 }
 
 template <typename L, bool SIGMOID, int PER, bool VEC>
 __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const RouteArgs a) {
     extern __shared__ char lds[];
     const int lane = threadIdx.x & (ROUTE_LANES - 1), token = threadIdx.x / ROUTE_LANES;
-    const size_t t = (size_t)blockIdx.x * ROUTE_TOKENS + token;
+    const size_t t = (size_t)blockIdx.x * (blockDim.x / ROUTE_LANES) + token;
     if (t >= (size_t)a.T) return;  // whole rows of 16 lanes; no workgroup barrier below
-    int32_t *chosen = reinterpret_cast<int32_t *>(lds) + token * (2 * a.k + 2);
-    double *shared = reinterpret_cast<double *>(lds + ROUTE_TOKENS * (2 * a.k + 2) * 4) + token * a.E;  // there where groups straddle lanes
+    // per token: with a bias `capacity` experts, keys and values, without k experts; n_experts values where groups straddle lanes
+    RoutePlaces at;
+    at.exact = reinterpret_cast<double *>(lds + (size_t)token * a.lds);
+    at.values = at.exact + (a.bias ? a.capacity : 0);
+    at.chosen = reinterpret_cast<int32_t *>(at.values + (a.straddle ? a.E : 0));
+    at.keys = at.chosen + a.capacity;
+    at.capacity = a.capacity;
     const int first = lane * PER;
     float z[PER], b[PER];
     load_logits<VEC>(reinterpret_cast<const L *>(a.logits) + t * a.stride, a.E, first, z);
@@ -325,14 +429,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
     for (int i = 1; i < PER; ++i) m = fmaxf(m, z[i]);
     m = lanes_max(m);
 
-    auto same = [&](int e, int f) {
-        const float be = a.bias[e], bf = a.bias[f];
-        return logit_at<L>(a, t, e) == logit_at<L>(a, t, f) && be == bf;
-    };
-    if (select_experts<float, SIGMOID, PER>(a, z, b, first, lane, m, reinterpret_cast<float *>(shared), chosen, same)) {
-        wave_sync();
-        select_experts<double, SIGMOID, PER>(a, z, b, first, lane, m, shared, chosen, same);
-    }
+    const int32_t *chosen = select_experts<SIGMOID, PER>(a, z, b, first, lane, m, at, [&](int e) { return logit_at<L>(a, t, e); });
     wave_sync();
 
     float sum = 0.f;  // of exp(z - m) over all experts
@@ -593,15 +690,18 @@ int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_s
     NEED_PTR(nullptr, fn, topk_weight, 4);
     OPT_PTR(nullptr, fn, scores_out, 4);
     const int groups = router->n_groups ? router->n_groups : 1, keep = router->topk_groups ? router->topk_groups : groups;
-    const RouteArgs a = {logits, (size_t)logits_stride, bias, T, router->n_experts, router->top_k, groups, keep, router->renormalize,
-                         router->scale, topk_idx, topk_weight, scores_out};
-    // 16 tokens x (2 k + 2 words, and n_experts values of 8 bytes where groups straddle lanes, which 256 experts' never do): below 64 KiB
+    RouteArgs a = {logits, (size_t)logits_stride, bias, T, router->n_experts, router->top_k, groups, keep, router->renormalize,
+                   router->scale, topk_idx, topk_weight, scores_out, 0, 0, 0};
     int part = 1;
     while (part * 2 * groups <= ROUTE_LANES) part *= 2;
-    const bool straddle = groups > 1 && a.E / groups != part * route_per(a.E);
-    const size_t lds = (size_t)ROUTE_TOKENS * ((2 * a.k + 2) * 4 + (straddle ? a.E * 8 : 0));
+    a.straddle = groups > 1 && a.E / groups != part * route_per(a.E);
+    a.capacity = std::min(a.E, a.k + ROUTE_MORE);
+    a.lds = ((bias ? 16 * a.capacity : 4 * a.k) + (a.straddle ? 8 * a.E : 0) + 15) & ~15;
+    // sixteen tokens a workgroup, four where that would take more than 40 KiB of LDS: four workgroups a CU either way
+    const int threads = ROUTE_TOKENS * a.lds > 40 * 1024 ? 64 : ROUTE_THREADS, tokens = threads / ROUTE_LANES;
+    const size_t lds = (size_t)tokens * a.lds;
     const bool vec = route_vec(router, logits, logits_stride);
-    const dim3 grid((T + ROUTE_TOKENS - 1) / ROUTE_TOKENS), block(ROUTE_THREADS);
+    const dim3 grid((T + tokens - 1) / tokens), block(threads);
     ROUTE_LAUNCH(route_logits_kernel, router, vec, grid, block, lds, (hipStream_t)stream, a);
     return launched(fn);
 }
