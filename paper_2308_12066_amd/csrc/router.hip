@@ -13,11 +13,9 @@
 #include <climits>
 #include <cmath>
 
-#include "pgmoe_internal.h"
+#include "ffn_common.h"
 
 namespace pgmoe {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 struct RouteArgs {
     const void *logits;
@@ -121,11 +119,14 @@ __device__ inline float exp_of(float x) {
 __device__ inline float inverse_of(float x) { return __builtin_amdgcn_rcpf(x); }  // one step of 2^-24
 __device__ inline double exp_of(double x) { return exp(x); }
 __device__ inline double inverse_of(double x) { return 1.0 / x; }
-// exp(z - m), 1 at the largest of infinite logits
+// exp(z - m), 1 at the largest of infinite logits and 0 for an unavailable one.  (Values first, choices afterwards: no branches.)
 template <typename V>
 __device__ inline V exp_below(float z, float m) {
-    return z == m ? V(1) : exp_of(V(z) - V(m));
+    const V e = exp_of(V(z) - V(m));
+    const V one_at_m = z == m ? V(1) : e;
+    return available(z) ? one_at_m : V(0);
 }
+// 0 for an unavailable logit, which is -infinity here
 template <typename V>
 __device__ inline V sigmoid(float z) {
     return inverse_of(V(1) + exp_of(-V(z)));
@@ -133,7 +134,8 @@ __device__ inline V sigmoid(float z) {
 
 template <typename L>
 __device__ inline float logit_at(const RouteArgs &a, size_t t, int e) {
-    return (float)reinterpret_cast<const L *>(a.logits)[t * a.stride + e];
+    const float z = (float)reinterpret_cast<const L *>(a.logits)[t * a.stride + e];
+    return available(z) ? z : -INFINITY;
 }
 
 // This lane's logits of token t; unavailable (-infinity) past the last expert.  VEC: all PER exist, at an address that their bytes (or 16) divide.
@@ -158,7 +160,6 @@ __device__ inline void load_logits(const L *row, int E, int first, float (&z)[PE
 
 template <bool VEC, int PER>
 __device__ inline void load_floats(const float *row, int E, int first, float (&v)[PER]) {
-    typedef float floatx4 __attribute__((ext_vector_type(4)));
     if (VEC && PER % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < PER; i += 4) {
@@ -172,17 +173,39 @@ __device__ inline void load_floats(const float *row, int E, int first, float (&v
     }
 }
 
+// This lane's results into a row.
+template <bool VEC, typename L, int PER>
+__device__ inline void store_row(L *row, int E, int first, const float (&v)[PER]) {
+    constexpr int N = PER * sizeof(L) > 16 ? 16 / sizeof(L) : PER;
+    typedef L Lx __attribute__((ext_vector_type(N)));
+    if (VEC) {
+        if (first < E) {
+#pragma unroll
+            for (int i = 0; i < PER; i += N) {
+                Lx x;
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[j] = (L)v[i + j];
+                *reinterpret_cast<Lx *>(row + first + i) = x;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (first + i < E) row[first + i] = (L)v[i];
+    }
+}
+
 // Scores of this lane's experts from its logits; m: the token's largest logit.
 template <typename V, bool SIGMOID, int PER>
 __device__ inline void scores_of(const float (&z)[PER], float m, V (&s)[PER]) {
     if (SIGMOID) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) s[i] = available(z[i]) ? sigmoid<V>(z[i]) : V(0);
+        for (int i = 0; i < PER; ++i) s[i] = sigmoid<V>(z[i]);
     } else {
         V sum = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            s[i] = available(z[i]) ? exp_below<V>(z[i], m) : V(0);
+            s[i] = exp_below<V>(z[i], m);
             sum += s[i];
         }
         sum = lanes_sum(sum);
@@ -229,24 +252,29 @@ __device__ bool keep_groups(const RouteArgs &a, const float (&z)[PER], const V (
         }
         wave_sync();
     }
-    for (int m = 1; m < part; m <<= 1) {
-        const V other_two = __shfl_xor(two, m);
-        take(__shfl_xor(one, m));
+    auto join = [&](V other_one, V other_two) {
+        take(other_one);
         take(other_two);
-    }
+    };
+    if (part > 1) join(row_moved<0xB1>(one), row_moved<0xB1>(two));      // quad_perm 1 0 3 2
+    if (part > 2) join(row_moved<0x4E>(one), row_moved<0x4E>(two));      // quad_perm 2 3 0 1
+    if (part > 4) join(row_moved<0x141>(one), row_moved<0x141>(two));    // row_half_mirror: quads are of one mind
+    if (part > 8) join(row_moved<0x140>(one), row_moved<0x140>(two));    // row_mirror
     Key worth = low;
     V value = -(V)INFINITY;
     if (mine < a.n_groups) {
         value = two > -(V)INFINITY ? one + two : one;
         worth = value > -(V)INFINITY ? Keys<V>::of(value) : low;
     }
-    // kept: fewer than `keep` groups are worthier, or as worthy and lower (all lanes of a group say the same)
+    // kept: fewer than `keep` groups are worthier, or as worthy and lower.  All lanes of a group say the same, so each group counts `part` times.
     int above = 0;
-    for (int g = 0; g < a.n_groups; ++g) {
-        const Key o = __shfl(worth, (threadIdx.x & 48) + g * part);
-        above += o > worth || (o == worth && g < mine) ? 1 : 0;
-    }
-    const bool kept = mine < a.n_groups && above < a.keep;
+    static_for<ROUTE_LANES - 1>([&](auto r_) {
+        constexpr int R = decltype(r_)::value + 1;
+        const Key o = row_moved<0x120 + R>(worth);
+        const int theirs = ((lane - R) & (ROUTE_LANES - 1)) / part;  // row_ror:R brings what is R lanes below
+        above += theirs < a.n_groups && (o > worth || (o == worth && theirs < mine)) ? 1 : 0;
+    });
+    const bool kept = mine < a.n_groups && above < a.keep * part;
     *mask = (unsigned)(__ballot(kept) >> (threadIdx.x & 48)) & 0xffffu;
     if (sizeof(V) == 8 || a.keep == a.n_groups) return false;
     // the worst kept against the best other
@@ -377,7 +405,7 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
 #pragma unroll 1
         for (int i = 0; i < a.E; i += ROUTE_LANES) {
             const float zi = i + lane < a.E ? logit(i + lane) : -INFINITY;
-            sum += available(zi) ? exp_below<double>(zi, m) : 0.0;
+            sum += exp_below<double>(zi, m);
         }
         sum = lanes_sum(sum);
     }
@@ -418,12 +446,10 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
     at.capacity = a.capacity;
     const int first = lane * PER;
     float z[PER], b[PER];
+    if (a.bias) load_floats<VEC>(a.bias, a.E, first, b);
     load_logits<VEC>(reinterpret_cast<const L *>(a.logits) + t * a.stride, a.E, first, z);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const float v = a.bias && first + i < a.E ? a.bias[first + i] : 0.f;
-        b[i] = v == v ? v : -INFINITY;
-    }
+    for (int i = 0; i < PER; ++i) b[i] = !a.bias ? 0.f : b[i] == b[i] ? b[i] : -INFINITY;
     float m = z[0];
 #pragma unroll
     for (int i = 1; i < PER; ++i) m = fmaxf(m, z[i]);
@@ -438,46 +464,44 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
         if (!SIGMOID) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                s[i] = available(z[i]) ? exp_below<float>(z[i], m) : 0.f;
+                s[i] = exp_below<float>(z[i], m);
                 sum += s[i];
             }
             sum = lanes_sum(sum);
         } else {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) s[i] = available(z[i]) ? sigmoid<float>(z[i]) : 0.f;
+            for (int i = 0; i < PER; ++i) s[i] = sigmoid<float>(z[i]);
         }
         if (a.scores) {
+            if (!SIGMOID) {
+                const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (first + i < a.E) a.scores[t * a.E + first + i] = SIGMOID ? s[i] : (sum > 0.f ? s[i] / sum : 0.f);
+                for (int i = 0; i < PER; ++i) s[i] *= inv;
+            }
+            store_row<VEC>(a.scores + t * a.E, a.E, first, s);
         }
     }
-    // Weights, lane j the j-th.  Renormalised ones are taken relative to the largest selected logit, so that neither sum nor quotient
-    // underflows where all of them are small: sigmoid(z) = exp(min(z, 0)) / (1 + exp(-|z|)).
-    float top = -INFINITY, total = 0.f;
-    if (a.renorm) {
-        for (int j = lane; j < a.k; j += ROUTE_LANES) {
-            const float zj = logit_at<L>(a, t, chosen[j]);
-            if (available(zj)) top = fmaxf(top, SIGMOID ? fminf(zj, 0.f) : zj);
-        }
-        top = lanes_max(top);
-    }
+    // Weights, lane j the j-th (and 16 + j-th ..).  Renormalised ones are taken relative to the largest selected logit, so that neither
+    // sum nor quotient underflows where all of them are small: sigmoid(z) = exp(min(z, 0)) / (1 + exp(-|z|)).
+    auto chosen_logit = [&](int j) { return j < a.k ? logit_at<L>(a, t, chosen[j]) : -INFINITY; };
+    const float z0 = chosen_logit(lane);
+    float top = SIGMOID ? fminf(z0, 0.f) : z0, total = 0.f;
     auto part = [&](float zj) {
-        if (!available(zj)) return 0.f;
-        if (SIGMOID) return exp_below<float>(fminf(zj, 0.f), top) / (1.f + exp_of(-fabsf(zj)));
+        if (SIGMOID) return exp_below<float>(fminf(zj, 0.f), top) * inverse_of(1.f + exp_of(-fabsf(zj)));
         return exp_below<float>(zj, top);
     };
     if (a.renorm) {
-        for (int j = lane; j < a.k; j += ROUTE_LANES) total += part(logit_at<L>(a, t, chosen[j]));
+        for (int j = lane + ROUTE_LANES; j < a.k; j += ROUTE_LANES) top = fmaxf(top, SIGMOID ? fminf(chosen_logit(j), 0.f) : chosen_logit(j));
+        top = lanes_max(top);
+        total = part(z0);
+        for (int j = lane + ROUTE_LANES; j < a.k; j += ROUTE_LANES) total += part(chosen_logit(j));
         total = lanes_sum(total);
     }
     for (int j = lane; j < a.k; j += ROUTE_LANES) {
-        const int e = chosen[j];
-        const float zj = logit_at<L>(a, t, e);
-        float w = 0.f;
-        if (available(zj)) w = a.renorm ? part(zj) / total : SIGMOID ? sigmoid<float>(zj) : exp_below<float>(zj, m) / sum;
-        a.idx[t * a.k + j] = e;
-        a.weight[t * a.k + j] = a.scale * w;
+        const float zj = j == lane ? z0 : chosen_logit(j);
+        const float w = a.renorm ? part(zj) / total : SIGMOID ? sigmoid<float>(zj) : exp_below<float>(zj, m) / sum;
+        a.idx[t * a.k + j] = chosen[j];
+        a.weight[t * a.k + j] = available(zj) ? a.scale * w : 0.f;
     }
 }
 
@@ -521,7 +545,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_backward_kernel(co
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            s[i] = !available(z[i]) ? 0.f : SIGMOID ? sigmoid<float>(z[i]) : exp_below<float>(z[i], m);
+            s[i] = SIGMOID ? sigmoid<float>(z[i]) : exp_below<float>(z[i], m);
             sum += s[i];
         }
         if (!SIGMOID) {
@@ -539,8 +563,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_backward_kernel(co
         return available(zj) ? zj : -INFINITY;
     };
     auto ratio = [&](float zj) {  // s_j, up to a factor common to the token's
-        if (!available(zj)) return 0.f;
-        if (SIGMOID) return exp_below<float>(fminf(zj, 0.f), top) / (1.f + exp_of(-fabsf(zj)));
+        if (SIGMOID) return exp_below<float>(fminf(zj, 0.f), top) * inverse_of(1.f + exp_of(-fabsf(zj)));
         return exp_below<float>(zj, top);
     };
     int e;
@@ -585,26 +608,10 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_backward_kernel(co
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         d[i] = part[first + i];
-        if (every && s[i] > 0.f) d[i] += SIGMOID ? s[i] * sigmoid<float>(-z[i]) * ds[i] : s[i] * (ds[i] - common);
+        const float more = SIGMOID ? s[i] * sigmoid<float>(-z[i]) * ds[i] : s[i] * (ds[i] - common);
+        d[i] = every && s[i] > 0.f ? d[i] + more : d[i];
     }
-    L *out = reinterpret_cast<L *>(a.d_logits) + t * a.d_stride + first;
-    if (VEC) {
-        constexpr int N = PER * sizeof(L) > 16 ? 16 / sizeof(L) : PER;
-        typedef L Lx __attribute__((ext_vector_type(N)));
-        if (first < a.E) {
-#pragma unroll
-            for (int i = 0; i < PER; i += N) {
-                Lx v;
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[j] = (L)d[i + j];
-                *reinterpret_cast<Lx *>(out + i) = v;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (first + i < a.E) out[i] = (L)d[i];
-    }
+    store_row<VEC>(reinterpret_cast<L *>(a.d_logits) + t * a.d_stride, a.E, first, d);
 }
 
 static int check_router(const pgmoe_router *r, const char *fn) {
@@ -700,7 +707,7 @@ int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_s
     // sixteen tokens a workgroup, four where that would take more than 40 KiB of LDS: four workgroups a CU either way
     const int threads = ROUTE_TOKENS * a.lds > 40 * 1024 ? 64 : ROUTE_THREADS, tokens = threads / ROUTE_LANES;
     const size_t lds = (size_t)tokens * a.lds;
-    const bool vec = route_vec(router, logits, logits_stride);
+    const bool vec = route_vec(router, logits, logits_stride) && aligned(bias, 16) && aligned(scores_out, 16);
     const dim3 grid((T + tokens - 1) / tokens), block(threads);
     ROUTE_LAUNCH(route_logits_kernel, router, vec, grid, block, lds, (hipStream_t)stream, a);
     return launched(fn);
