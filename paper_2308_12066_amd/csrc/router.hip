@@ -196,20 +196,20 @@ __device__ inline void store_row(L *row, int E, int first, const float (&v)[PER]
 }
 
 // Scores of this lane's experts from its logits; m: the token's largest logit.
-template <typename V, bool SIGMOID, int PER>
-__device__ inline void scores_of(const float (&z)[PER], float m, V (&s)[PER]) {
+template <bool SIGMOID, int PER>
+__device__ inline void scores_of(const float (&z)[PER], float m, float (&s)[PER]) {
     if (SIGMOID) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) s[i] = sigmoid<V>(z[i]);
+        for (int i = 0; i < PER; ++i) s[i] = sigmoid<float>(z[i]);
     } else {
-        V sum = 0;
+        float sum = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            s[i] = exp_below<V>(z[i], m);
+            s[i] = exp_below<float>(z[i], m);
             sum += s[i];
         }
         sum = lanes_sum(sum);
-        const V inv = sum > V(0) ? inverse_of(sum) : V(0);
+        const float inv = sum > 0.f ? inverse_of(sum) : 0.f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) s[i] *= inv;
     }
@@ -220,50 +220,43 @@ __device__ inline void scores_of(const float (&z)[PER], float m, V (&s)[PER]) {
 struct RoutePlaces {
     int32_t *chosen, *keys;  // [capacity]
     double *exact;           // [capacity]
-    double *values;          // [n_experts]
+    float *values;           // [n_experts]
     int capacity;
 };
 constexpr int ROUTE_MORE = 32;  // candidates beyond the k that are looked at before all experts are
 
-// Which groups are kept, as a bit for each in the first of its lanes.  Returns whether 32 bits may have decided it (V = float only).
-template <typename V, int PER>
-__device__ bool keep_groups(const RouteArgs &a, const float (&z)[PER], const V (&v)[PER], int first, int lane, V *values, int part, unsigned *mask) {
-    typedef typename Keys<V>::T Key;
-    constexpr Key low = Keys<V>::lowest;
-    // The worth of a group: `part` lanes, the largest power of two there are for each, look for the two largest of a part of it each.
-    const int size = a.E / a.n_groups, mine = lane / part;
+// The two largest of what it is shown.
+template <typename V>
+struct TwoLargest {
     V one = -(V)INFINITY, two = -(V)INFINITY;
-    auto take = [&](V x) {
+    __device__ void take(V x) {
         const V low_one = x > one ? one : x;
         one = x > one ? x : one;
         two = low_one > two ? low_one : two;
-    };
-    if (size == part * PER) {  // which are this lane's own
-#pragma unroll
-        for (int i = 0; i < PER; ++i) take(available(z[i]) ? v[i] : -(V)INFINITY);
-    } else {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (first + i < a.E) values[first + i] = available(z[i]) ? v[i] : -(V)INFINITY;
-        wave_sync();
-        if (mine < a.n_groups) {
-            const int from = size * (lane - mine * part) / part, to = size * (lane - mine * part + 1) / part;
-            for (int j = from; j < to; ++j) take(values[mine * size + j]);
-        }
-        wave_sync();
     }
-    auto join = [&](V other_one, V other_two) {
-        take(other_one);
-        take(other_two);
-    };
-    if (part > 1) join(row_moved<0xB1>(one), row_moved<0xB1>(two));      // quad_perm 1 0 3 2
-    if (part > 2) join(row_moved<0x4E>(one), row_moved<0x4E>(two));      // quad_perm 2 3 0 1
-    if (part > 4) join(row_moved<0x141>(one), row_moved<0x141>(two));    // row_half_mirror: quads are of one mind
-    if (part > 8) join(row_moved<0x140>(one), row_moved<0x140>(two));    // row_mirror
+    template <int CTRL>
+    __device__ void join() {  // with another lane's
+        const V o = row_moved<CTRL>(one), t = row_moved<CTRL>(two);
+        take(o);
+        take(t);
+    }
+};
+
+// Which groups are kept, as a bit for each in the first of its `part` lanes, from what each of these has seen of the group.  Returns whether
+// 32 bits may have decided it (V = float only).
+template <typename V>
+__device__ bool keep_groups(const RouteArgs &a, TwoLargest<V> best, int lane, int part, unsigned *mask) {
+    typedef typename Keys<V>::T Key;
+    constexpr Key low = Keys<V>::lowest;
+    const int mine = lane / part;
+    if (part > 1) best.template join<0xB1>();   // quad_perm 1 0 3 2
+    if (part > 2) best.template join<0x4E>();   // quad_perm 2 3 0 1
+    if (part > 4) best.template join<0x141>();  // row_half_mirror: quads are of one mind
+    if (part > 8) best.template join<0x140>();  // row_mirror
     Key worth = low;
     V value = -(V)INFINITY;
     if (mine < a.n_groups) {
-        value = two > -(V)INFINITY ? one + two : one;
+        value = best.two > -(V)INFINITY ? best.one + best.two : best.one;
         worth = value > -(V)INFINITY ? Keys<V>::of(value) : low;
     }
     // kept: fewer than `keep` groups are worthier, or as worthy and lower.  All lanes of a group say the same, so each group counts `part` times.
@@ -284,10 +277,9 @@ __device__ bool keep_groups(const RouteArgs &a, const float (&z)[PER], const V (
 }
 
 // Takes the expert of the largest key: the lowest of those that have it.
-template <typename Key, int PER>
-__device__ inline int take_largest(Key (&key)[PER], int first, Key *top) {
-    constexpr Key lowest = sizeof(Key) == 4 ? (Key)Keys<float>::lowest : (Key)Keys<double>::lowest;
-    Key best = key[0];
+template <int PER>
+__device__ inline int take_largest(int32_t (&key)[PER], int first, int32_t *top) {
+    int32_t best = key[0];
 #pragma unroll
     for (int i = 1; i < PER; ++i) best = key[i] > best ? key[i] : best;
     best = lanes_max(best);
@@ -296,7 +288,7 @@ __device__ inline int take_largest(Key (&key)[PER], int first, Key *top) {
     for (int i = PER - 1; i >= 0; --i) won = key[i] == best ? first + i : won;
     won = lanes_min(won);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) key[i] = first + i == won ? lowest + KEY_TAKEN : key[i];
+    for (int i = 0; i < PER; ++i) key[i] = first + i == won ? INT_MIN + KEY_TAKEN : key[i];
     *top = best;
     return won;
 }
@@ -305,43 +297,67 @@ __device__ inline int take_largest(Key (&key)[PER], int first, Key *top) {
 template <bool SIGMOID, int PER, typename F>
 __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PER], const float (&b)[PER], int first, int lane, float m, const RoutePlaces &at, F logit) {
     int32_t key[PER];
-    unsigned outside = 0;  // of the kept groups, a bit an expert
+    unsigned gone = 0;  // of this lane's experts: outside the kept groups, later also taken
+    // In 64 bits, one expert at a time: there are few such tokens, and what they run is short code rather than fast.
+    double sum = 0.0;
+    auto exact_sum = [&]() {
+        if (SIGMOID || sum > 0.0) return;
+#pragma unroll 1
+        for (int e = lane; e < a.E; e += ROUTE_LANES) sum += exp_below<double>(logit(e), m);
+        sum = lanes_sum(sum);
+    };
+    auto exact_value = [&](int e) {
+        const float ze = logit(e), be = a.bias ? a.bias[e] : 0.f;
+        const double v = (SIGMOID ? sigmoid<double>(ze) : exp_below<double>(ze, m) / sum) + (double)be;
+        return available(ze) && be > -INFINITY ? v : -(double)INFINITY;
+    };
     {
         float v[PER];
         if (a.bias || a.n_groups > 1) {
-            scores_of<float, SIGMOID, PER>(z, m, v);
+            scores_of<SIGMOID, PER>(z, m, v);
 #pragma unroll
             for (int i = 0; i < PER; ++i) v[i] += b[i];
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             // without a bias by the logit: scores rise with it, and it is exact
-            const int32_t of = Keys<float>::of(a.bias ? v[i] : z[i]);
-            key[i] = first + i >= a.E ? INT_MIN + KEY_TAKEN : available(z[i]) ? of : INT_MIN + KEY_UNAVAILABLE;
+            const int32_t of = Keys<float>::of(a.bias ? v[i] : z[i]), there = available(z[i]) ? of : INT_MIN + KEY_UNAVAILABLE;
+            key[i] = first + i >= a.E ? INT_MIN + KEY_TAKEN : there;
         }
         if (a.n_groups > 1) {
+            // `part` lanes, the largest power of two there are for each, look for the two largest of a part of a group each
             int part = 1;
             while (part * 2 * a.n_groups <= ROUTE_LANES) part *= 2;
-            unsigned mask;
-            if (keep_groups<float, PER>(a, z, v, first, lane, reinterpret_cast<float *>(at.values), part, &mask)) {
-                double exact[PER];
-                scores_of<double, SIGMOID, PER>(z, m, exact);
+            const int size = a.E / a.n_groups, mine = lane / part;
+            const int from = size * (lane - mine * part) / part, to = mine < a.n_groups ? size * (lane - mine * part + 1) / part : from;
+            TwoLargest<float> best;
+            if (!a.straddle) {  // these are the lane's own
 #pragma unroll
-                for (int i = 0; i < PER; ++i) exact[i] += (double)b[i];
-                keep_groups<double, PER>(a, z, exact, first, lane, at.values, part, &mask);
+                for (int i = 0; i < PER; ++i) best.take(available(z[i]) ? v[i] : -INFINITY);
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (first + i < a.E) at.values[first + i] = available(z[i]) ? v[i] : -INFINITY;
+                wave_sync();
+                for (int j = from; j < to; ++j) best.take(at.values[mine * size + j]);
             }
-            const int size = a.E / a.n_groups;
+            unsigned mask;
+            if (keep_groups(a, best, lane, part, &mask)) {
+                exact_sum();
+                TwoLargest<double> exact;
+#pragma unroll 1
+                for (int j = from; j < to; ++j) exact.take(exact_value(mine * size + j));
+                keep_groups(a, exact, lane, part, &mask);
+            }
             int g = first / size, in_group = first - g * size;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                if (first + i < a.E && !((mask >> (g * part)) & 1)) {
-                    key[i] = INT_MIN + KEY_OUTSIDE;
-                    outside |= 1u << i;
-                }
-                if (++in_group == size) {
-                    in_group = 0;
-                    ++g;
-                }
+                const bool out = !((mask >> (g * part)) & 1);
+                gone |= out ? 1u << i : 0u;
+                key[i] = out && first + i < a.E ? INT_MIN + KEY_OUTSIDE : key[i];
+                const bool next = ++in_group == size;
+                in_group = next ? 0 : in_group;
+                g += next ? 1 : 0;
             }
         }
     }
@@ -383,38 +399,27 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
         ++n;
     }
     wave_sync();
+    exact_sum();
     if (all) {  // too many: all experts again, in 64 bits
-        double v[PER];
-        int64_t wide[PER], unused;
-        scores_of<double, SIGMOID, PER>(z, m, v);
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            wide[i] = first + i >= a.E       ? Keys<double>::lowest + KEY_TAKEN
-                      : (outside >> i) & 1   ? Keys<double>::lowest + KEY_OUTSIDE
-                      : available(z[i])      ? Keys<double>::of(v[i] + (double)b[i])
-                                             : Keys<double>::lowest + KEY_UNAVAILABLE;
         for (int j = 0; j < a.k; ++j) {
-            const int won = take_largest(wide, first, &unused);
+            int64_t top = LLONG_MIN;
+            int won = INT_MAX;
+#pragma unroll 1
+            for (int i = 0; i < PER; ++i) {
+                const int e = first + i;
+                if (e >= a.E || (gone >> i) & 1) continue;
+                const int64_t k = available(logit(e)) ? Keys<double>::of(exact_value(e)) : Keys<double>::lowest + KEY_UNAVAILABLE;
+                won = k > top ? e : won;
+                top = k > top ? k : top;
+            }
+            const int64_t best = lanes_max(top);
+            won = lanes_min(top == best ? won : INT_MAX);
+            if (won >= first && won < first + PER) gone |= 1u << (won - first);
             if (lane == 0) at.chosen[j] = won;
         }
         return at.chosen;
     }
-    double sum = 1.0;
-    if (!SIGMOID) {
-        sum = 0.0;
-#pragma unroll 1
-        for (int i = 0; i < a.E; i += ROUTE_LANES) {
-            const float zi = i + lane < a.E ? logit(i + lane) : -INFINITY;
-            sum += exp_below<double>(zi, m);
-        }
-        sum = lanes_sum(sum);
-    }
-    auto value = [&](int e) {
-        const float ze = logit(e), be = a.bias[e];
-        if (!available(ze) || !(be > -INFINITY)) return -(double)INFINITY;
-        return (SIGMOID ? sigmoid<double>(ze) : exp_below<double>(ze, m) / sum) + (double)be;
-    };
-    for (int j = lane; j < n; j += ROUTE_LANES) at.exact[j] = value(at.chosen[j]);
+    for (int j = lane; j < n; j += ROUTE_LANES) at.exact[j] = exact_value(at.chosen[j]);
     wave_sync();
     for (int j = lane; j < n; j += ROUTE_LANES) {
         const double x = at.exact[j];
@@ -440,9 +445,9 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
     // per token: with a bias `capacity` experts, keys and values, without k experts; n_experts values where groups straddle lanes
     RoutePlaces at;
     at.exact = reinterpret_cast<double *>(lds + (size_t)token * a.lds);
-    at.values = at.exact + (a.bias ? a.capacity : 0);
-    at.chosen = reinterpret_cast<int32_t *>(at.values + (a.straddle ? a.E : 0));
-    at.keys = at.chosen + a.capacity;
+    at.chosen = reinterpret_cast<int32_t *>(at.exact + (a.bias ? a.capacity : 0));
+    at.keys = at.chosen + (a.bias ? a.capacity : a.k);
+    at.values = reinterpret_cast<float *>(at.keys + (a.bias ? a.capacity : 0));
     at.capacity = a.capacity;
     const int first = lane * PER;
     float z[PER], b[PER];
@@ -703,7 +708,7 @@ int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_s
     while (part * 2 * groups <= ROUTE_LANES) part *= 2;
     a.straddle = groups > 1 && a.E / groups != part * route_per(a.E);
     a.capacity = std::min(a.E, a.k + ROUTE_MORE);
-    a.lds = ((bias ? 16 * a.capacity : 4 * a.k) + (a.straddle ? 8 * a.E : 0) + 15) & ~15;
+    a.lds = ((bias ? 16 * a.capacity : 4 * a.k) + (a.straddle ? 4 * a.E : 0) + 15) & ~15;
     // sixteen tokens a workgroup, four where that would take more than 40 KiB of LDS: four workgroups a CU either way
     const int threads = ROUTE_TOKENS * a.lds > 40 * 1024 ? 64 : ROUTE_THREADS, tokens = threads / ROUTE_LANES;
     const size_t lds = (size_t)tokens * a.lds;
