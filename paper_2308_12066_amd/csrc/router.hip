@@ -5,10 +5,11 @@
 // every lane and four exchanges, for four tokens at once, and the lowest lane that holds it has the lowest index.
 //
 // Selection.  Every expert's value becomes an integer key that orders as the value does, with places below all values for
-// an expert that is unavailable, outside the kept groups, or taken.  What is compared are 32-bit results, whose last bits
-// depend on how exp and the sums were rounded; so the chosen neighbours (and the two groups at the border) are looked at
-// once more, and a token where two of them lie closer than CLOSE is selected again with everything in 64 bits.
-// Values that are equal because logit and bias are equal are no such case: both ways the lowest index wins.
+// an expert that is unavailable, outside the kept groups, or taken.  The last four bits of a key are the expert's place in its lane
+// (15 the first), so that a lane's largest key names its expert, the first of equal ones.  What is compared are so 32-bit results
+// without their last four bits; hence the chosen neighbours (and the two groups at the border) are looked at once more, and a token where two of them
+// lie closer than CLOSE is decided in 64 bits.  Values that are equal because logit and bias are equal are no such case: either
+// way the lowest index wins.  16-bit logits without a bias have those bits to spare.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -26,7 +27,8 @@ struct RouteArgs {
     float scale;
     int32_t *idx;
     float *weight, *scores;
-    int straddle;  // groups that are not whole lanes
+    int size, shift;  // experts of a group, lanes of one as a power of two
+    int straddle;     // groups that are not whole lanes
     int capacity;
     int lds;       // bytes of a token
 };
@@ -34,17 +36,18 @@ struct RouteArgs {
 constexpr int ROUTE_LANES = 16;                                // of one token
 constexpr int ROUTE_THREADS = 256, ROUTE_TOKENS = ROUTE_THREADS / ROUTE_LANES;
 // Two selection values closer than this, relative to the larger of them and 2^-24, are compared in 64 bits: the scores carry
-// a few units of 2^-24 (exp, a sum of up to 256 terms in pairs, a division), the bias and the sum of a group's two one each.
-constexpr float CLOSE = 4e-6f;
+// a few units of 2^-24 (exp, a sum of up to 256 terms in pairs, a division), the bias and the sum of a group's two one each, 4e-6 in all;
+// a key leaves out 2^-19.
+constexpr float CLOSE = 6e-6f;
 
-// Keys of values: integers in the order of the values, -0 as 0 and NaN as -infinity.
+// Keys of values, which are not NaN: integers in the order of the values, -0 as 0.
 template <typename V>
 struct Keys;
 template <>
 struct Keys<float> {
     typedef int32_t T;
     __device__ static T of(float v) {
-        const int32_t b = __float_as_int(v == v ? v + 0.f : -INFINITY);
+        const int32_t b = __float_as_int(v + 0.f);
         return b ^ ((b >> 31) & INT_MAX);
     }
     __device__ static float value(T k) { return __int_as_float(k ^ ((k >> 31) & INT_MAX)); }
@@ -54,13 +57,13 @@ template <>
 struct Keys<double> {
     typedef int64_t T;
     __device__ static T of(double v) {
-        const int64_t b = __double_as_longlong(v == v ? v + 0.0 : -(double)INFINITY);
+        const int64_t b = __double_as_longlong(v + 0.0);
         return b ^ ((b >> 63) & LLONG_MAX);
     }
     static constexpr T lowest = LLONG_MIN;
 };
-// below every value: taken, outside the kept groups, unavailable (in rising order, from Keys::lowest)
-enum { KEY_TAKEN = 0, KEY_OUTSIDE = 1, KEY_UNAVAILABLE = 2 };
+// below every value, in rising order; the last two with the place in the lane added
+constexpr int32_t KEY_TAKEN = INT_MIN, KEY_OUTSIDE = INT_MIN + 16, KEY_UNAVAILABLE = INT_MIN + 32, KEY_VALUES = INT_MIN + 48;
 
 // Reductions over the 16 lanes of a token (a row of the wavefront): rotations by 8, 4, 2 and 1 inside the row, which the vector unit
 // does on the way (a shuffle through LDS takes some hundred clocks, and a selection is a chain of them).
@@ -242,17 +245,17 @@ struct TwoLargest {
     }
 };
 
-// Which groups are kept, as a bit for each in the first of its `part` lanes, from what each of these has seen of the group.  Returns whether
-// 32 bits may have decided it (V = float only).
+// Which groups are kept, as a bit for each in the first of its `part` lanes, from what each of these has seen of the group.  part = 2^shift.  Returns
+// whether 32 bits may have decided it (V = float only).
 template <typename V>
-__device__ bool keep_groups(const RouteArgs &a, TwoLargest<V> best, int lane, int part, unsigned *mask) {
+__device__ bool keep_groups(const RouteArgs &a, TwoLargest<V> best, int lane, int shift, unsigned *mask) {
     typedef typename Keys<V>::T Key;
     constexpr Key low = Keys<V>::lowest;
-    const int mine = lane / part;
-    if (part > 1) best.template join<0xB1>();   // quad_perm 1 0 3 2
-    if (part > 2) best.template join<0x4E>();   // quad_perm 2 3 0 1
-    if (part > 4) best.template join<0x141>();  // row_half_mirror: quads are of one mind
-    if (part > 8) best.template join<0x140>();  // row_mirror
+    const int mine = lane >> shift;
+    if (shift > 0) best.template join<0xB1>();   // quad_perm 1 0 3 2
+    if (shift > 1) best.template join<0x4E>();   // quad_perm 2 3 0 1
+    if (shift > 2) best.template join<0x141>();  // row_half_mirror: quads are of one mind
+    if (shift > 3) best.template join<0x140>();  // row_mirror
     Key worth = low;
     V value = -(V)INFINITY;
     if (mine < a.n_groups) {
@@ -264,10 +267,10 @@ __device__ bool keep_groups(const RouteArgs &a, TwoLargest<V> best, int lane, in
     static_for<ROUTE_LANES - 1>([&](auto r_) {
         constexpr int R = decltype(r_)::value + 1;
         const Key o = row_moved<0x120 + R>(worth);
-        const int theirs = ((lane - R) & (ROUTE_LANES - 1)) / part;  // row_ror:R brings what is R lanes below
+        const int theirs = ((lane - R) & (ROUTE_LANES - 1)) >> shift;  // row_ror:R brings what is R lanes below
         above += theirs < a.n_groups && (o > worth || (o == worth && theirs < mine)) ? 1 : 0;
     });
-    const bool kept = mine < a.n_groups && above < a.keep * part;
+    const bool kept = mine < a.n_groups && above < a.keep << shift;
     *mask = (unsigned)(__ballot(kept) >> (threadIdx.x & 48)) & 0xffffu;
     if (sizeof(V) == 8 || a.keep == a.n_groups) return false;
     // the worst kept against the best other
@@ -282,19 +285,16 @@ __device__ inline int take_largest(int32_t (&key)[PER], int first, int32_t *top)
     int32_t best = key[0];
 #pragma unroll
     for (int i = 1; i < PER; ++i) best = key[i] > best ? key[i] : best;
-    best = lanes_max(best);
-    int won = INT_MAX;
+    *top = lanes_max(best & ~15);
+    const int candidate = (best & ~15) == *top ? first + 15 - (best & 15) : INT_MAX, won = lanes_min(candidate);
+    const int32_t mine = candidate == won ? best : KEY_TAKEN;
 #pragma unroll
-    for (int i = PER - 1; i >= 0; --i) won = key[i] == best ? first + i : won;
-    won = lanes_min(won);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) key[i] = first + i == won ? INT_MIN + KEY_TAKEN : key[i];
-    *top = best;
+    for (int i = 0; i < PER; ++i) key[i] = key[i] == mine ? KEY_TAKEN : key[i];
     return won;
 }
 
-// Selects the k experts of one token; returns where they are: at.chosen or at.keys.  logit(e): a logit of this token.
-template <bool SIGMOID, int PER, typename F>
+// Selects the k experts of one token; returns where they are: at.chosen or at.keys.  logit(e): a logit of this token.  FULL: logits have 32 bits.
+template <bool SIGMOID, bool FULL, int PER, typename F>
 __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PER], const float (&b)[PER], int first, int lane, float m, const RoutePlaces &at, F logit) {
     int32_t key[PER];
     unsigned gone = 0;  // of this lane's experts: outside the kept groups, later also taken
@@ -321,15 +321,13 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             // without a bias by the logit: scores rise with it, and it is exact
-            const int32_t of = Keys<float>::of(a.bias ? v[i] : z[i]), there = available(z[i]) ? of : INT_MIN + KEY_UNAVAILABLE;
-            key[i] = first + i >= a.E ? INT_MIN + KEY_TAKEN : there;
+            const int32_t of = Keys<float>::of(a.bias ? v[i] : z[i]) & ~15, there = available(z[i]) ? of : KEY_UNAVAILABLE;
+            key[i] = first + i >= a.E ? KEY_TAKEN : there | (15 - i);
         }
         if (a.n_groups > 1) {
-            // `part` lanes, the largest power of two there are for each, look for the two largest of a part of a group each
-            int part = 1;
-            while (part * 2 * a.n_groups <= ROUTE_LANES) part *= 2;
-            const int size = a.E / a.n_groups, mine = lane / part;
-            const int from = size * (lane - mine * part) / part, to = mine < a.n_groups ? size * (lane - mine * part + 1) / part : from;
+            // 2^shift lanes a group, as many as there are, look for the two largest of a part of it each
+            const int shift = a.shift, size = a.size, mine = lane >> shift, in_part = lane - (mine << shift);
+            const int from = size * in_part >> shift, to = mine < a.n_groups ? size * (in_part + 1) >> shift : from;
             TwoLargest<float> best;
             if (!a.straddle) {  // these are the lane's own
 #pragma unroll
@@ -342,46 +340,56 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
                 for (int j = from; j < to; ++j) best.take(at.values[mine * size + j]);
             }
             unsigned mask;
-            if (keep_groups(a, best, lane, part, &mask)) {
+            if (keep_groups(a, best, lane, shift, &mask)) {
                 exact_sum();
                 TwoLargest<double> exact;
 #pragma unroll 1
                 for (int j = from; j < to; ++j) exact.take(exact_value(mine * size + j));
-                keep_groups(a, exact, lane, part, &mask);
+                keep_groups(a, exact, lane, shift, &mask);
             }
-            int g = first / size, in_group = first - g * size;
+            if (!a.straddle) {
+                const bool out = !((mask >> (mine << shift)) & 1) && mine < a.n_groups;
+                gone = out ? ~0u : 0u;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const bool out = !((mask >> (g * part)) & 1);
-                gone |= out ? 1u << i : 0u;
-                key[i] = out && first + i < a.E ? INT_MIN + KEY_OUTSIDE : key[i];
-                const bool next = ++in_group == size;
-                in_group = next ? 0 : in_group;
-                g += next ? 1 : 0;
+                for (int i = 0; i < PER; ++i) key[i] = out ? KEY_OUTSIDE | (15 - i) : key[i];
+            } else {
+                int g = first / size, in_group = first - g * size;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const bool out = !((mask >> (g << shift)) & 1);
+                    gone |= out ? 1u << i : 0u;
+                    key[i] = out && first + i < a.E ? KEY_OUTSIDE | (15 - i) : key[i];
+                    const bool next = ++in_group == size;
+                    in_group = next ? 0 : in_group;
+                    g += next ? 1 : 0;
+                }
             }
         }
     }
-    // with a bias one further than asked for, to compare the last chosen with the first that is not
-    int n = a.bias ? min(a.k + 1, a.E) : a.k;
+    // where keys do not decide, one further than asked for: to compare the last chosen with the first that is not
+    const bool look = a.bias || FULL;
+    int n = look ? min(a.k + 1, a.E) : a.k;
     int32_t top = 0;
     for (int j = 0; j < n; ++j) {
         const int won = take_largest(key, first, &top);
         if (lane == 0) {
             at.chosen[j] = won;
-            if (a.bias) at.keys[j] = top;
+            if (look) at.keys[j] = top;
         }
     }
-    if (!a.bias) return at.chosen;
+    if (!look) return at.chosen;
     wave_sync();
     auto near = [&](int32_t upper, int32_t lower) {  // might the order be another in 64 bits?
         const float hi = Keys<float>::value(upper), lo = Keys<float>::value(lower);
-        return lower > INT_MIN + KEY_UNAVAILABLE && lo > -INFINITY && !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f));
+        const bool unsure = a.bias ? lo > -INFINITY && !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f)) : upper == lower;
+        return lower >= KEY_VALUES && unsure;
     };
     bool close = false;
     for (int j = lane; j + 1 < n; j += ROUTE_LANES)
         if (near(at.keys[j], at.keys[j + 1])) {
             const int e = at.chosen[j], f = at.chosen[j + 1];
-            close |= logit(e) != logit(f) || !(a.bias[e] == a.bias[f]);
+            // (behind the last chosen there may be more: beside an equal one also a larger one)
+            close |= j + 1 == a.k || logit(e) != logit(f) || (a.bias && !(a.bias[e] == a.bias[f]));
         }
     if (!lanes_max(close ? 1 : 0)) return at.chosen;
 
@@ -399,7 +407,8 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
         ++n;
     }
     wave_sync();
-    exact_sum();
+    if (a.bias) exact_sum();
+    auto rank_value = [&](int e) { return a.bias ? exact_value(e) : (double)logit(e); };
     if (all) {  // too many: all experts again, in 64 bits
         for (int j = 0; j < a.k; ++j) {
             int64_t top = LLONG_MIN;
@@ -408,7 +417,7 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
             for (int i = 0; i < PER; ++i) {
                 const int e = first + i;
                 if (e >= a.E || (gone >> i) & 1) continue;
-                const int64_t k = available(logit(e)) ? Keys<double>::of(exact_value(e)) : Keys<double>::lowest + KEY_UNAVAILABLE;
+                const int64_t k = available(logit(e)) ? Keys<double>::of(rank_value(e)) : Keys<double>::lowest + 1;
                 won = k > top ? e : won;
                 top = k > top ? k : top;
             }
@@ -419,7 +428,7 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
         }
         return at.chosen;
     }
-    for (int j = lane; j < n; j += ROUTE_LANES) at.exact[j] = exact_value(at.chosen[j]);
+    for (int j = lane; j < n; j += ROUTE_LANES) at.exact[j] = rank_value(at.chosen[j]);
     wave_sync();
     for (int j = lane; j < n; j += ROUTE_LANES) {
         const double x = at.exact[j];
@@ -442,12 +451,13 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
     const int lane = threadIdx.x & (ROUTE_LANES - 1), token = threadIdx.x / ROUTE_LANES;
     const size_t t = (size_t)blockIdx.x * (blockDim.x / ROUTE_LANES) + token;
     if (t >= (size_t)a.T) return;  // whole rows of 16 lanes; no workgroup barrier below
-    // per token: with a bias `capacity` experts, keys and values, without k experts; n_experts values where groups straddle lanes
+    const bool look = a.bias || sizeof(L) == 4;
+    // per token: where keys do not decide `capacity` experts, keys and values, without k experts; n_experts values where groups straddle lanes
     RoutePlaces at;
     at.exact = reinterpret_cast<double *>(lds + (size_t)token * a.lds);
-    at.chosen = reinterpret_cast<int32_t *>(at.exact + (a.bias ? a.capacity : 0));
-    at.keys = at.chosen + (a.bias ? a.capacity : a.k);
-    at.values = reinterpret_cast<float *>(at.keys + (a.bias ? a.capacity : 0));
+    at.chosen = reinterpret_cast<int32_t *>(at.exact + (look ? a.capacity : 0));
+    at.keys = at.chosen + (look ? a.capacity : a.k);
+    at.values = reinterpret_cast<float *>(at.keys + (look ? a.capacity : 0));
     at.capacity = a.capacity;
     const int first = lane * PER;
     float z[PER], b[PER];
@@ -460,7 +470,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
     for (int i = 1; i < PER; ++i) m = fmaxf(m, z[i]);
     m = lanes_max(m);
 
-    const int32_t *chosen = select_experts<SIGMOID, PER>(a, z, b, first, lane, m, at, [&](int e) { return logit_at<L>(a, t, e); });
+    const int32_t *chosen = select_experts<SIGMOID, sizeof(L) == 4>(a, z, b, first, lane, m, at, [&](int e) { return logit_at<L>(a, t, e); });
     wave_sync();
 
     float sum = 0.f;  // of exp(z - m) over all experts
@@ -703,12 +713,11 @@ int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_s
     OPT_PTR(nullptr, fn, scores_out, 4);
     const int groups = router->n_groups ? router->n_groups : 1, keep = router->topk_groups ? router->topk_groups : groups;
     RouteArgs a = {logits, (size_t)logits_stride, bias, T, router->n_experts, router->top_k, groups, keep, router->renormalize,
-                   router->scale, topk_idx, topk_weight, scores_out, 0, 0, 0};
-    int part = 1;
-    while (part * 2 * groups <= ROUTE_LANES) part *= 2;
-    a.straddle = groups > 1 && a.E / groups != part * route_per(a.E);
+                   router->scale, topk_idx, topk_weight, scores_out, router->n_experts / groups, 0, 0, 0, 0};
+    while (groups << (a.shift + 1) <= ROUTE_LANES) ++a.shift;
+    a.straddle = groups > 1 && a.size != route_per(a.E) << a.shift;
     a.capacity = std::min(a.E, a.k + ROUTE_MORE);
-    a.lds = ((bias ? 16 * a.capacity : 4 * a.k) + (a.straddle ? 4 * a.E : 0) + 15) & ~15;
+    a.lds = ((bias || router->logits_dtype == PGMOE_F32 ? 16 * a.capacity : 4 * a.k) + (a.straddle ? 4 * a.E : 0) + 15) & ~15;
     // sixteen tokens a workgroup, four where that would take more than 40 KiB of LDS: four workgroups a CU either way
     const int threads = ROUTE_TOKENS * a.lds > 40 * 1024 ? 64 : ROUTE_THREADS, tokens = threads / ROUTE_LANES;
     const size_t lds = (size_t)tokens * a.lds;
