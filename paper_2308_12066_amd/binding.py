@@ -205,38 +205,43 @@ def unique_experts(idx, n_experts: int):
     return out[:rc].copy()
 
 
-# ---- routing and 8-bit experts: no context; tensors carry their sizes, types and strides
-_DTYPES = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16, "torch.float8_e4m3fn": E4M3, "torch.float8_e5m2": E5M2}
+# ---- routing and 8-bit experts: no context; tensors carry their sizes, types and strides.  A call takes a few
+# microseconds on the GPU, so what is checked here is checked on the tensors' own attributes.
+try:
+    import torch as _torch
+    _DTYPES = {_torch.float32: F32, _torch.bfloat16: BF16, _torch.float16: F16, _torch.float8_e4m3fn: E4M3, _torch.float8_e5m2: E5M2}
+    _f32, _i32 = _torch.float32, _torch.int32
+except ImportError:  # the calls below take torch tensors
+    _DTYPES, _f32, _i32 = {}, None, None
 
 
-def _dtype(t) -> int:
-    code = _DTYPES.get(str(t.dtype))
+def _dtype(t, name) -> int:
+    code = _DTYPES.get(t.dtype)
     if code is None:
-        raise TypeError(f"no operator of the library takes {t.dtype}")
+        raise TypeError(f"{name} has dtype {t.dtype}: no operator of the library takes it")
     return code
 
 
-def _expect(t, name, shape, dtype, strides=True):
-    """The checks only the tensor allows: the library sees addresses."""
-    if tuple(t.shape) != tuple(shape):
+def _expect(t, name, shape, dtype):
+    """The checks only the tensor allows: the library sees addresses.  -> its address"""
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if str(t.dtype) not in ((dtype,) if isinstance(dtype, str) else dtype):
+    if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
-    if strides and not t.is_contiguous():
+    if not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
+    return t.data_ptr()
 
 
 def _row_stride(t, name) -> int:
     """Elements from one row of a matrix to the next; within a row they lie side by side."""
-    if t.dim() != 2:
-        raise ValueError(f"{name} has {t.dim()} dimensions, not 2")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} has {len(shape)} dimensions, not 2")
+    row, col = t.stride()
+    if col != 1 and shape[1] > 1:
         raise ValueError(f"the elements of a row of {name} do not lie side by side")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-_FLOATS = ("torch.float32", "torch.bfloat16", "torch.float16")
-_FP8 = ("torch.float8_e4m3fn", "torch.float8_e5m2")
+    return row if shape[0] > 1 else max(row, shape[1])
 
 
 def fp8_blocks(n: int) -> int:
@@ -245,13 +250,15 @@ def fp8_blocks(n: int) -> int:
 
 def _fp8_rows(q, scale, cols, name) -> FP8Rows:
     """q [rows, >= 128 * blocks] codes, scale [blocks, >= rows] float32."""
-    rows = q.shape[0]
-    if str(q.dtype) not in _FP8:
-        raise TypeError(f"{name} has dtype {q.dtype}, not one of {_FP8}")
-    if q.shape[1] < FP8_BLOCK * fp8_blocks(cols):
-        raise ValueError(f"{name} has {q.shape[1]} columns, fewer than the {FP8_BLOCK * fp8_blocks(cols)} of whole blocks")
-    _expect(scale, name + "'s scale", (fp8_blocks(cols), rows), "torch.float32", strides=False)
-    return FP8Rows(q.data_ptr(), _row_stride(q, name), scale.data_ptr(), _row_stride(scale, name + "'s scale"), rows, cols, _dtype(q))
+    code = _DTYPES.get(q.dtype)
+    if code != E4M3 and code != E5M2:
+        raise TypeError(f"{name} has dtype {q.dtype}, not an 8-bit one")
+    stride, (rows, width), blocks = _row_stride(q, name), q.shape, (cols + FP8_BLOCK - 1) // FP8_BLOCK
+    if width < FP8_BLOCK * blocks:
+        raise ValueError(f"{name} has {width} columns, fewer than the {FP8_BLOCK * blocks} of whole blocks")
+    if scale.shape != (blocks, rows) or scale.dtype != _f32:
+        raise ValueError(f"{name}'s scale is {scale.dtype} {tuple(scale.shape)}, not float32 {(blocks, rows)}")
+    return FP8Rows(q.data_ptr(), stride, scale.data_ptr(), _row_stride(scale, "a scale"), rows, cols, code)
 
 
 def fp8_weight_shapes(n_experts: int, n_in: int, n_out: int):
@@ -260,10 +267,11 @@ def fp8_weight_shapes(n_experts: int, n_in: int, n_out: int):
 
 
 def _fp8_weights(q, scale, n_in, n_out, name) -> FP8Weights:
-    shape, scale_shape = fp8_weight_shapes(q.shape[0], n_in, n_out)
-    _expect(q, name, shape, "torch.float8_e4m3fn")
-    _expect(scale, name + "'s scale", scale_shape, "torch.float32")
-    return FP8Weights(q.data_ptr(), scale.data_ptr(), q.shape[0], n_in, n_out)
+    n = q.shape[0]
+    shape, scale_shape = fp8_weight_shapes(n, n_in, n_out)
+    if _DTYPES.get(q.dtype) != E4M3:
+        raise TypeError(f"{name} has dtype {q.dtype}, not torch.float8_e4m3fn")
+    return FP8Weights(_expect(q, name, shape, q.dtype), _expect(scale, "a scale", scale_shape, _f32), n, n_in, n_out)
 
 
 class Router:
@@ -271,46 +279,40 @@ class Router:
 
     def __init__(self, n_experts, top_k, score=SCORE_SOFTMAX, n_groups=1, topk_groups=0, renormalize=False, scale=1.0):
         self.cfg = RouterConfig(n_experts, top_k, n_groups, topk_groups, score, 1 if renormalize else 0, scale, F32)
+        self._shape = n_experts, top_k
 
     def _outer(self, logits):
-        T, E = logits.shape
-        if E != self.cfg.n_experts:
-            raise ValueError(f"logits of {E} experts, the router has {self.cfg.n_experts}")
-        self.cfg.logits_dtype = _dtype(logits)
-        return T, E
+        stride, (T, E) = _row_stride(logits, "logits"), logits.shape
+        if E != self._shape[0]:
+            raise ValueError(f"logits of {E} experts, the router has {self._shape[0]}")
+        self.cfg.logits_dtype = _dtype(logits, "logits")
+        return T, E, self._shape[1], stride
 
     def route(self, logits, bias, topk_idx, topk_weight, scores_out=None, stream=None):
-        T, E = self._outer(logits)
-        if bias is not None:
-            _expect(bias, "bias", (E,), "torch.float32")
-        _expect(topk_idx, "topk_idx", (T, self.cfg.top_k), "torch.int32")
-        _expect(topk_weight, "topk_weight", (T, self.cfg.top_k), "torch.float32")
-        if scores_out is not None:
-            _expect(scores_out, "scores_out", (T, E), "torch.float32")
-        rc = lib.pgmoe_route(byref(self.cfg), _ptr(logits), _row_stride(logits, "logits"), _ptr(bias), T, _ptr(topk_idx), _ptr(topk_weight),
-                             _ptr(scores_out), _stream(stream))
+        T, E, k, stride = self._outer(logits)
+        rc = lib.pgmoe_route(byref(self.cfg), logits.data_ptr(), stride, None if bias is None else _expect(bias, "bias", (E,), _f32), T,
+                             _expect(topk_idx, "topk_idx", (T, k), _i32), _expect(topk_weight, "topk_weight", (T, k), _f32),
+                             None if scores_out is None else _expect(scores_out, "scores_out", (T, E), _f32), _stream(stream))
         if rc:
             raise PgmoeError(rc, last_error())
 
     def route_backward(self, logits, topk_idx, d_weight, d_scores, d_logits, stream=None):
-        T, E = self._outer(logits)
-        _expect(topk_idx, "topk_idx", (T, self.cfg.top_k), "torch.int32")
-        _expect(d_weight, "d_weight", (T, self.cfg.top_k), "torch.float32")
-        if d_scores is not None:
-            _expect(d_scores, "d_scores", (T, E), "torch.float32")
-        _expect(d_logits, "d_logits", (T, E), str(logits.dtype), strides=False)
-        rc = lib.pgmoe_route_backward(byref(self.cfg), _ptr(logits), _row_stride(logits, "logits"), _ptr(topk_idx), _ptr(d_weight), _ptr(d_scores), T,
-                                      _ptr(d_logits), _row_stride(d_logits, "d_logits"), _stream(stream))
+        T, E, k, stride = self._outer(logits)
+        if d_logits.shape != (T, E) or d_logits.dtype != logits.dtype:
+            raise ValueError(f"d_logits is {d_logits.dtype} {tuple(d_logits.shape)}, logits are {logits.dtype} {(T, E)}")
+        rc = lib.pgmoe_route_backward(byref(self.cfg), logits.data_ptr(), stride, _expect(topk_idx, "topk_idx", (T, k), _i32),
+                                      _expect(d_weight, "d_weight", (T, k), _f32), None if d_scores is None else _expect(d_scores, "d_scores", (T, E), _f32), T,
+                                      d_logits.data_ptr(), _row_stride(d_logits, "d_logits"), _stream(stream))
         if rc:
             raise PgmoeError(rc, last_error())
 
 
 def quantize_rows(x, q, scale, row_of=None, copies=1, stream=None) -> None:
     """x [T, cols] -> codes q [rows, 128 * blocks] and scales [blocks, rows]; row_of [T * copies] deals the rows out."""
-    out = _fp8_rows(q, scale, x.shape[1], "q")
-    if row_of is not None:
-        _expect(row_of, "row_of", (x.shape[0] * copies,), "torch.int32")
-    rc = lib.pgmoe_quantize_rows(_ptr(x), _row_stride(x, "x"), _dtype(x), x.shape[0], _ptr(row_of), copies, byref(out), _stream(stream))
+    stride, (T, cols) = _row_stride(x, "x"), x.shape
+    out = _fp8_rows(q, scale, cols, "q")
+    rc = lib.pgmoe_quantize_rows(x.data_ptr(), stride, _dtype(x, "x"), T, None if row_of is None else _expect(row_of, "row_of", (T * copies,), _i32), copies,
+                                 byref(out), _stream(stream))
     if rc:
         raise PgmoeError(rc, last_error())
 
@@ -318,13 +320,13 @@ def quantize_rows(x, q, scale, row_of=None, copies=1, stream=None) -> None:
 def quantize_weights(w, forward_q, forward_scale, backward_q=None, backward_scale=None, stream=None) -> None:
     """w [E, n_in, n_out] -> the operand tiles and scales (fp8_weight_shapes) of x . W and, if given, of dy . W^T."""
     E, n_in, n_out = w.shape
-    _expect(w, "w", (E, n_in, n_out), _FLOATS)
     fwd = None if forward_q is None else _fp8_weights(forward_q, forward_scale, n_in, n_out, "forward_q")
     bwd = None if backward_q is None else _fp8_weights(backward_q, backward_scale, n_out, n_in, "backward_q")
     for f in (fwd, bwd):
         if f is not None and f.n_experts != E:
             raise ValueError(f"codes of {f.n_experts} experts for {E}")
-    rc = lib.pgmoe_quantize_weights(_ptr(w), _dtype(w), None if fwd is None else byref(fwd), None if bwd is None else byref(bwd), _stream(stream))
+    rc = lib.pgmoe_quantize_weights(_expect(w, "w", (E, n_in, n_out), w.dtype), _dtype(w, "w"), None if fwd is None else byref(fwd),
+                                    None if bwd is None else byref(bwd), _stream(stream))
     if rc:
         raise PgmoeError(rc, last_error())
 
@@ -333,14 +335,14 @@ def expert_matmul(x_q, x_scale, w_q, w_scale, expert_offsets, n_in, n_out, y, y_
     """y[rows] = act(x[rows] . W_e) for the rows of every expert e; y [rows, n_out], or codes with y_scale."""
     x = _fp8_rows(x_q, x_scale, n_in, "x_q")
     w = _fp8_weights(w_q, w_scale, n_in, n_out, "w_q")
-    _expect(expert_offsets, "expert_offsets", (w.n_experts + 1,), "torch.int32")
-    out = None
+    offsets = _expect(expert_offsets, "expert_offsets", (w.n_experts + 1,), _i32)
     if y_scale is not None:
         out = _fp8_rows(y, y_scale, n_out, "y")
+        rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, None, 0, out.dtype, byref(out), _stream(stream))
     else:
-        _expect(y, "y", (x.rows, n_out), _FLOATS, strides=False)
-    rc = lib.pgmoe_expert_matmul(byref(x), byref(w), _ptr(expert_offsets), 1 if relu else 0, None if out is not None else _ptr(y),
-                                 0 if out is not None else _row_stride(y, "y"), _dtype(y), None if out is None else byref(out), _stream(stream))
+        if y.shape != (x.rows, n_out):
+            raise ValueError(f"y has shape {tuple(y.shape)}, not {(x.rows, n_out)}")
+        rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, y.data_ptr(), _row_stride(y, "y"), _dtype(y, "y"), None, _stream(stream))
     if rc:
         raise PgmoeError(rc, last_error())
 
