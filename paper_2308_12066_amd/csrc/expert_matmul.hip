@@ -196,10 +196,14 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 // 4 RUN (4 a / RUN) + RUN (i / 4) + 4 a % RUN + i % 4 of the wavefront's 128 (a lane's four results of a product are rows 4 (lane / 16) ..).
 // With 64 bytes a lane in a row, stores of 16 bytes went to 64 places at once: an item ended 5 us later.
 constexpr int MATMUL_W_TILE = FP8_TILE + 64;
-template <int TM>
-struct MatmulRing {
-    static constexpr int W = 16 * MATMUL_W_TILE, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
-    static constexpr int NS = TM == 4 ? 2 : 3, TABLE = NS * STAGE, BYTES = TABLE + 4 * PGMOE_MAX_EXPERTS * 4, LOADS = 4 + TM + 1;
+// The shape of an item: up to TM * 64 rows and WN blocks of 128 outputs; its wavefronts as WN x WM.
+template <int WN_, int TM_>
+struct MatmulShape {
+    static constexpr int WN = WN_, TM = TM_, WM = 8 / WN, MC = TM * 4 / WM;  // MC: most row tiles of a wavefront
+    static constexpr int W = WN * 8 * MATMUL_W_TILE, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S, TABLE = 4 * PGMOE_MAX_EXPERTS * 4;
+    static constexpr int NS = (160 * 1024 - TABLE) / STAGE < 4 ? (160 * 1024 - TABLE) / STAGE : 4, BYTES = NS * STAGE + TABLE;
+    static constexpr int LOADS = 2 * WN + TM + 1;
+    static_assert(NS >= 2 && TM * 4 % WM == 0, "a ring, and as many row tiles for every wavefront");
 };
 constexpr int TILE_THREADS = 512, TILE_GROUPS = 256;  // workgroups: one per CU
 
@@ -219,8 +223,9 @@ struct MatmulItem {
     int expert, row0, nrows, nb;  // nrows == 0: there are no more
 };
 constexpr int MATMUL_COST = 1;
-template <int TM>
+template <typename R>
 struct MatmulItems {
+    static constexpr int TM = R::TM;
     const int *table;
     int cols, total;  // column blocks; chunks
     __device__ static int each_of(int n, int chunks) { return (((n + chunks - 1) / chunks) + 15) & ~15; }
@@ -239,19 +244,19 @@ struct MatmulItems {
             lo[q] = max(0, min(lo[q], a.rows));
             n[q] = max(lo[q], min(n[q], a.rows)) - lo[q];
         }
-        cols = (a.NB + 1) / 2;
+        cols = (a.NB + R::WN - 1) / R::WN;
         int most = TM * 64;
-        if (TM > 1) {
+        if (R::MC > 1) {
             float best = INFINITY;
-            static_for<TM>([&](auto u_) {
-                constexpr int MOST = 64 * (TM - decltype(u_)::value);
+            static_for<R::MC>([&](auto u_) {
+                constexpr int UNIT = 16 * R::WM, MOST = UNIT * (R::MC - decltype(u_)::value);
                 int sum = 0;
                 float cost = 0.f;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = (n[q] + MOST - 1) / MOST;
                     sum += c;
-                    cost += c ? (float)c * (float)(MATMUL_COST + ((each_of(n[q], c) + 63) >> 6)) : 0.f;
+                    cost += c ? (float)c * (float)(MATMUL_COST + (each_of(n[q], c) + UNIT - 1) / UNIT) : 0.f;
                 }
                 const int chunks = __builtin_amdgcn_readlane(wave_incl_scan(sum), 63);
 #pragma unroll
@@ -290,14 +295,14 @@ struct MatmulItems {
         const int before = e ? __builtin_amdgcn_readfirstlane(table[e - 1]) : 0, first = __builtin_amdgcn_readfirstlane(table[PGMOE_MAX_EXPERTS + e]);
         const int rows = __builtin_amdgcn_readfirstlane(table[2 * PGMOE_MAX_EXPERTS + e]), each = __builtin_amdgcn_readfirstlane(table[3 * PGMOE_MAX_EXPERTS + e]);
         const int k = chunk - before;
-        return {e, first + k * each, max(1, min(each, rows - k * each)), (turn - group * cols) * 2};
+        return {e, first + k * each, max(1, min(each, rows - k * each)), (turn - group * cols) * R::WN};
     }
 };
 
 // What a wavefront requests: the blocks of its workgroup's items one after the other.
-template <int TM>
+template <typename R>
 struct MatmulRequests {
-    typedef MatmulRing<TM> R;
+    static constexpr int TM = R::TM;
     const uint8_t *w_src, *x_src;
     const float *s_src;
     unsigned w_second, lds, stage;  // bytes to the wavefront's second weight tile; LDS address of the ring
@@ -310,7 +315,7 @@ struct MatmulRequests {
         left = ahead = 0;
         stage = 0;
     }
-    __device__ void next(const MatmulArgs &a, const MatmulItems<TM> &items, int wave) {
+    __device__ void next(const MatmulArgs &a, const MatmulItems<R> &items, int wave) {
         const int lane = lane_again();
         if (left == 0) {  // uniform
             const MatmulItem it = items.at(item);
@@ -318,8 +323,8 @@ struct MatmulRequests {
             item += gridDim.x;
             left = a.KB;
             const size_t block = (size_t)it.expert * a.NB + it.nb;
-            const int last = it.nb + 1 < a.NB ? 15 : 7;  // an odd last block of outputs has no neighbour
-            w_src = a.w + (block * 8 + min(wave * 2, last)) * a.KB * FP8_TILE;
+            const int last = it.nb + R::WN <= a.NB ? R::WN * 8 - 1 : 7;  // an odd last block of outputs has no neighbour
+            w_src = a.w + (block * 8 + min(wave * R::WN, last)) * a.KB * FP8_TILE;
             w_second = wave * 2 < last ? (unsigned)a.KB * FP8_TILE : 0;
             x_src = a.x + (size_t)it.row0 * a.x_stride;
             x_last = it.nrows - 1;
@@ -330,8 +335,8 @@ struct MatmulRequests {
             s_last = wave < 4 ? it.nrows - 1 : (last == 15 ? 1 : 0);
         }
         const unsigned to = lds + stage;
-        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * 2 * MATMUL_W_TILE);
-        load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
+        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * R::WN * MATMUL_W_TILE);
+        if (R::WN == 2) load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
         w_src += FP8_TILE;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -348,32 +353,27 @@ struct MatmulRequests {
     }
 };
 
-// Waits until, at most, the loads of one more request (two) and the stores of `tiles` row tiles are outstanding: operations complete in order.
-template <int LOADS, int STORES>
-__device__ inline void wait_for_loads(bool two, int tiles) {  // uniform
-#define PG_WAIT(T_)                                                                                              \
-    case T_:                                                                                                     \
-        if (two) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS + T_ * STORES < 63 ? LOADS + T_ * STORES : 63) : "memory"); \
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T_ * STORES < 63 ? T_ * STORES : 63) : "memory");          \
-        return;
-    switch (tiles) {
-        PG_WAIT(0) PG_WAIT(1) PG_WAIT(2) PG_WAIT(3) PG_WAIT(4)
-    }
-#undef PG_WAIT
+// Waits until, at most, the loads of `later` more requests and the stores of `tiles` row tiles are outstanding: operations complete in order.
+template <int LATER, int LOADS, int STORES>
+__device__ inline void wait_for_loads(int later, int tiles) {  // uniform; later 0 .. LATER, tiles 0 .. 4
+    static_for<LATER + 1>([&](auto l_) {
+        static_for<5>([&](auto t_) {
+            constexpr int l = decltype(l_)::value, t = decltype(t_)::value, n = l * LOADS + t * STORES;
+            if (later == l && tiles == t) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n < 63 ? n : 63) : "memory");
+        });
+    });
 }
 
 // The products of one item.  stored: row tiles whose results the wavefront stored behind the requests that are outstanding.
-template <int XQ, int TM, int MC, int RUN, int STORES>
-__device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const char *ring, unsigned &stage, int wave, int stored,
+template <int XQ, typename R, int MC, int RUN, int STORES>
+__device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<R> &items, MatmulRequests<R> &rq, const char *ring, unsigned &stage, int wave, int stored,
                                      floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
-    typedef MatmulRing<TM> R;
-    const int wn = wave & 1, wm = wave >> 1;
+    const int wn = wave & (R::WN - 1), wm = wave / R::WN;
     constexpr int PER = RUN / 4;  // products of a run
     auto place = [](int t) { return t / PER * PER * MATMUL_W_TILE + t % PER * 64; };
     for (int kb = 0; kb < a.KB; ++kb) {
         // This block's loads have landed: those of the later ones, and stores behind them all, may be outstanding.
-        const bool two = R::NS > 2 && rq.ahead > 1;
-        wait_for_loads<(R::NS > 2 ? R::LOADS : 0), STORES>(two, kb < (two ? 2 : 1) ? stored : 0);
+        wait_for_loads<R::NS - 2, R::LOADS, STORES>(min(rq.ahead - 1, R::NS - 2), kb <= R::NS - 2 ? stored : 0);
         // Behind the barrier they have for everyone, and everyone has read the block before, whose stage the next request takes.
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         rq.next(a, items, wave);
@@ -390,14 +390,64 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> 
             const float sw = *reinterpret_cast<const float *>(s_at + stage + 4 * 256 + wn * 4);
 #pragma unroll
             for (int m = 0; m < MC; ++m) {
-                const char *r = x_at + stage + m * 64 * FP8_BLOCK;
+                const char *r = x_at + stage + m * 16 * R::WM * FP8_BLOCK;
                 x[m] = operand<XQ>(*reinterpret_cast<const intx4 *>(r + x_low), *reinterpret_cast<const intx4 *>(r + x_high));
-                s[m] = sw * *reinterpret_cast<const float *>(s_at + stage + ((wm + 4 * m) * 16 + i16) * 4);
+                s[m] = sw * *reinterpret_cast<const float *>(s_at + stage + ((wm + R::WM * m) * 16 + i16) * 4);
             }
-            // Half a step is the products of one output tile and two row tiles.  Beside them run what the half before left to do (its sums into the
-            // accumulators) and half of the next output tile's conversion, dealt out behind the products one by one: the vector
-            // unit's work fits under the matrix cores' then, in a wavefront by itself.
-            constexpr int HALVES = MC > 2 ? 2 : 1, HM = MC > 1 ? 2 : 1;
+            // A step is two chains of products.  Beside them run what the step before left to do (its sums into the accumulators) and the
+            // conversion of weights that come next, dealt out behind the products one by one: the vector unit's work fits under the
+            // matrix cores' then, in a wavefront by itself.
+            if constexpr (MC == 1) {  // one row tile: the chains are two output tiles
+                auto codes = [&](int t, intx4(&to)[2]) {
+                    to[0] = *reinterpret_cast<const intx4 *>(w_at + stage + place(t));
+                    to[1] = *reinterpret_cast<const intx4 *>(w_at + stage + place(t) + 1024);
+                };
+                intx4 next[2][2];
+                codes(0, next[0]);
+                codes(1, next[1]);
+                Operand w[2] = {operand<PGMOE_E4M3>(next[0][0], next[0][1]), operand<PGMOE_E4M3>(next[1][0], next[1][1])}, w_next[2];
+                codes(2, next[0]);
+                codes(3, next[1]);
+                floatx4 before[2];
+                static_for<4>([&](auto step_) {
+                    constexpr int step = decltype(step_)::value;
+                    __builtin_amdgcn_sched_barrier(0);
+                    floatx4 p[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j].part[i], x[0].part[i], p[j], 0, 0, 0);
+                    if constexpr (step > 0) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[2 * step - 2 + j][0][v] = fmaf(s[0], before[j][v], acc[2 * step - 2 + j][0][v]);
+                    }
+                    if constexpr (step < 3) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            w_next[j] = operand<PGMOE_E4M3>(next[j][0], next[j][1]);
+                            if constexpr (step < 2) codes(2 * step + 4 + j, next[j]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        before[j] = p[j];
+                        w[j] = w_next[j];
+                    }
+                });
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[6 + j][0][v] = fmaf(s[0], before[j][v], acc[6 + j][0][v]);
+            } else {
+            constexpr int HALVES = MC > 2 ? 2 : 1, HM = 2;  // row tiles: the chains are two of them
             Operand w = operand<PGMOE_E4M3>(*reinterpret_cast<const intx4 *>(w_at + stage), *reinterpret_cast<const intx4 *>(w_at + stage + 1024)), w_next;
             intx4 low = *reinterpret_cast<const intx4 *>(w_at + stage + place(1)), high;
             floatx4 before[HM];
@@ -449,6 +499,7 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<TM> 
 #pragma unroll
                     for (int v = 0; v < 4; ++v) acc[7][2 * (HALVES - 1) + j][v] = fmaf(s[2 * (HALVES - 1) + j], before[j][v], acc[7][2 * (HALVES - 1) + j][v]);
                 }
+            }
         }
         stage = stage + R::STAGE == R::NS * R::STAGE ? 0 : stage + R::STAGE;
     }
@@ -466,8 +517,8 @@ constexpr int run_of() {  // results in 16 bytes
     else return 16 / sizeof(Y);
 }
 
-template <int XQ, typename Y, int YQ, bool VEC, int TM, int MC>
-__device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<TM> &items, MatmulRequests<TM> &rq, const MatmulItem &it, char *ring, unsigned &stage, int wave,
+template <int XQ, typename Y, int YQ, bool VEC, typename R, int MC>
+__device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<R> &items, MatmulRequests<R> &rq, const MatmulItem &it, char *ring, unsigned &stage, int wave,
                                   int stored) {
     constexpr int STORES = tile_stores<Y, VEC>(), RUN = run_of<Y>();
     floatx4 acc[8][MC > 0 ? MC : 1];
@@ -475,13 +526,13 @@ __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<TM> &it
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int m = 0; m < MC; ++m) acc[i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-    matmul_k_loop<XQ, TM, MC, RUN, STORES>(a, items, rq, ring, stage, wave, stored, acc);
-    const int lane = lane_again(), wn = wave & 1, wm = wave >> 1;
+    matmul_k_loop<XQ, R, MC, RUN, STORES>(a, items, rq, ring, stage, wave, stored, acc);
+    const int lane = lane_again(), wn = wave & (R::WN - 1), wm = wave / R::WN;
     const int block = it.nb + wn, o = block * FP8_BLOCK + RUN * (lane >> 4);  // run r of the lane begins at o + 4 RUN r
     if (block >= a.NB) return 0;
 #pragma unroll
     for (int m = 0; m < MC; ++m) {
-        const int in_chunk = (wm + 4 * m) * 16 + (lane & 15), row = it.row0 + in_chunk;
+        const int in_chunk = (wm + R::WM * m) * 16 + (lane & 15), row = it.row0 + in_chunk;
         const bool live = in_chunk < it.nrows;
         if (a.relu) {
 #pragma unroll
@@ -537,27 +588,27 @@ __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<TM> &it
     return (block + 1) * FP8_BLOCK <= a.n_out ? MC : 0;  // every row tile has a live row: STORES were issued for each
 }
 
-template <int XQ, typename Y, int YQ, bool VEC, int TM>
+template <int XQ, typename Y, int YQ, bool VEC, typename R>
 __global__ __launch_bounds__(TILE_THREADS, 2) void matmul_tiles_kernel(const MatmulArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char ring[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    MatmulItems<TM> items;
-    items.build(a, reinterpret_cast<int *>(ring + MatmulRing<TM>::TABLE));
+    MatmulItems<R> items;
+    items.build(a, reinterpret_cast<int *>(ring + R::NS * R::STAGE));
     __syncthreads();
-    MatmulRequests<TM> rq;
+    MatmulRequests<R> rq;
     rq.start(ring, blockIdx.x);
 #pragma unroll
-    for (int st = 0; st < MatmulRing<TM>::NS - 1; ++st) rq.next(a, items, wave);
+    for (int st = 0; st < R::NS - 1; ++st) rq.next(a, items, wave);
     unsigned stage = 0;
     int stored = 0;
     for (int i = blockIdx.x;; i += gridDim.x) {
         const MatmulItem it = items.at(i);
         if (it.nrows == 0) break;  // uniform over the workgroup; every request has been waited for
-        const int rt = (it.nrows + 15) >> 4, own = max(0, (rt - (wave >> 1) + 3) >> 2);
+        const int rt = (it.nrows + 15) >> 4, own = max(0, (rt - wave / R::WN + R::WM - 1) / R::WM);
         switch (own) {  // uniform over the wavefront
 #define PG_BODY(MC_)                                                                                                                        \
     case MC_:                                                                                                                               \
-        if constexpr (MC_ <= TM) stored = matmul_item<XQ, Y, YQ, VEC, TM, MC_>(a, items, rq, it, ring, stage, wave, stored);                 \
+        if constexpr (MC_ <= R::MC) stored = matmul_item<XQ, Y, YQ, VEC, R, MC_>(a, items, rq, it, ring, stage, wave, stored);               \
         asm volatile("; %0 row tiles" ::"n"(MC_)); /* keeps the bodies' stores apart */                                                      \
         break;
             PG_BODY(0) PG_BODY(1) PG_BODY(2) PG_BODY(3) PG_BODY(4)
@@ -568,34 +619,41 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void matmul_tiles_kernel(const Mat
 
 constexpr int64_t TILE_STRIDE_MAX = 1 << 23;  // bytes: offsets within a chunk of 256 rows have 31 bits
 
-template <int XQ, typename Y, int YQ, bool VEC, int TM>
+template <int XQ, typename Y, int YQ, bool VEC, typename R>
 static int launch_tiles(const MatmulArgs &a, hipStream_t s) {
     // more than 48 KiB of LDS: the kernel's limit is raised once per device
     static std::atomic<uint64_t> raised{0};
     int device = 0;
     if (const hipError_t e = hipGetDevice(&device)) return e == hipErrorNoDevice ? fail(nullptr, PGMOE_ENODEVICE, "pgmoe_expert_matmul: no HIP device is visible") : hip_fail(nullptr, e, "hipGetDevice");
     if (!(raised.load(std::memory_order_relaxed) >> (device & 63) & 1)) {
-        const void *kernel = reinterpret_cast<const void *>(&matmul_tiles_kernel<XQ, Y, YQ, VEC, TM>);
-        PG_HIP(nullptr, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, MatmulRing<TM>::BYTES));
+        const void *kernel = reinterpret_cast<const void *>(&matmul_tiles_kernel<XQ, Y, YQ, VEC, R>);
+        PG_HIP(nullptr, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, R::BYTES));
         raised.fetch_or(1ull << (device & 63), std::memory_order_relaxed);
     }
-    // chunks: sum over the experts of ceil(rows / (TM * 64)), in whole eights
-    const int64_t chunks = ((a.rows + (int64_t)(TM * 64 - 1) * std::min(a.E, a.rows)) / (TM * 64) + 7) & ~(int64_t)7;
-    const unsigned groups = (unsigned)std::min<int64_t>(TILE_GROUPS, chunks * ((a.NB + 1) / 2));
-    hipLaunchKernelGGL((matmul_tiles_kernel<XQ, Y, YQ, VEC, TM>), dim3(groups), dim3(TILE_THREADS), MatmulRing<TM>::BYTES, s, a);
+    // chunks: at most the sum over the experts of ceil(rows / the smallest the kernel may choose), in whole eights
+    constexpr int UNIT = 16 * R::WM;
+    const int64_t chunks = ((a.rows + (int64_t)(UNIT - 1) * std::min(a.E, a.rows)) / UNIT + 7) & ~(int64_t)7;
+    const unsigned groups = (unsigned)std::min<int64_t>(TILE_GROUPS, chunks * ((a.NB + R::WN - 1) / R::WN));
+    hipLaunchKernelGGL((matmul_tiles_kernel<XQ, Y, YQ, VEC, R>), dim3(groups), dim3(TILE_THREADS), R::BYTES, s, a);
     return PGMOE_OK;
 }
 template <int XQ, typename Y, int YQ, bool VEC>
 static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
-    const int mean = a.rows / std::min(a.E, a.rows);  // rows an expert
-    if (mean > 16 && (int64_t)a.x_stride < TILE_STRIDE_MAX) {
-        if (mean > 128) return launch_tiles<XQ, Y, YQ, VEC, 4>(a, s);
-        if (mean > 64) return launch_tiles<XQ, Y, YQ, VEC, 2>(a, s);
-        return launch_tiles<XQ, Y, YQ, VEC, 1>(a, s);
+    // Which kernel, by rows an expert (on the mean) and by what there is to deal out; both sides in us a launch, bf16 results:
+    //  * few rows, to 8 an expert: the tiles would be empty mostly (64 experts of 1024 x 4096: 4 rows each 50.0, in tiles of 64 rows 51.0; 8 rows
+    //    52.5 / 51.8, 16 rows 64.8 / 53.1); also launches of at most one workgroup a CU in 16-row chunks (32 rows for each of 8 experts of
+    //    4096 x 1024 20.7 / 47.5, 64 for one 20.2 / 46.6; not 512 for one of 1024 x 4096 22.0 / 17.0), and rows too far apart for the tiles;
+    //  * tiles of 64 rows, three stages in flight, to 48 rows an expert (32 for each of 64 59.9, in tiles of 256 rows 65.8; 64 rows 86 / 77) and where
+    //    tiles of 256 leave half the CUs without an item (512 for each of 8 experts of 2048 x 768 31.7 / 34.9; not 128 for each of 8 of
+    //    1024 x 4096 30.5 / 25.7);
+    //  * tiles of up to 256 rows for the others.
+    const int active = std::min(a.E, a.rows), mean = a.rows / active;
+    const int64_t chunks16 = (a.rows + (int64_t)15 * active) / 16, items256 = (active + (int64_t)a.rows / 256) * ((a.NB + 1) / 2);
+    if (mean > 8 && chunks16 * a.NB > TILE_GROUPS && (int64_t)a.x_stride < TILE_STRIDE_MAX) {
+        if (mean <= 48 || items256 < TILE_GROUPS / 2) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<2, 1>>(a, s);
+        return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<2, 4>>(a, s);
     }
-    // chunks: sum over the experts of ceil(rows / 16)
-    const int64_t chunks = (a.rows + (int64_t)15 * std::min(a.E, a.rows)) / 16;
-    hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC>), dim3((unsigned)(chunks * a.NB)), dim3(FEW_THREADS), 0, s, a);
+    hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC>), dim3((unsigned)(chunks16 * a.NB)), dim3(FEW_THREADS), 0, s, a);
     return PGMOE_OK;
 }
 template <int XQ, typename Y>
