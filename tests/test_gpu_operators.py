@@ -647,3 +647,58 @@ def test_block_with_8_bit_experts_replays_from_a_captured_graph(B):
             assert torch.equal(b["y"], y) and torch.equal(dl, d_logits), rep
     del graph
     ctx.close()
+
+
+@pytest.fixture(scope="module")
+def example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "fp8_experts.py")
+    spec = importlib.util.spec_from_file_location("fp8_experts", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@pytest.mark.parametrize("T,d,f,E,k", [(1, 256, 512, 8, 2), (200, 256, 1000, 16, 2)])
+def test_example_of_a_block_with_8_bit_experts(example, T, d, f, E, k):
+    """examples/fp8_experts.py as it is run: replays of the captured forward give the eager bits; the result is near that of unquantised
+    experts: three roundings to e4m3 (half a step 2^-4 of a value at most, on the mean a good third of it) of terms of sums."""
+    say("example", T, d, f, E, k)
+    errors, us, same = example.run(T, d, f, E, k, replays=3)
+    assert same and us > 0
+    assert errors["y"] < 2.0 ** -4 and all(np.isfinite(v) for v in errors.values()), errors
+
+
+@pytest.mark.parametrize("T,d,f,E,k", [(1, 256, 512, 8, 2), (60, 128, 300, 16, 3)])
+def test_backward_of_the_example(example, B, T, d, f, E, k):
+    """Its backward against the same chain in 64 bits, from what the forward left: codes, experts, weights, results of the experts."""
+    say("example backward", T, d, f, E, k)
+    g = np.random.default_rng(T)
+    w1, w2 = ((0.05 * g.standard_normal(s)).astype(np.float32) for s in ((E, d, f), (E, f, d)))
+    x, z, dy = dev(g.standard_normal((T, d)), "bf16"), dev(g.standard_normal((T, E))), g.standard_normal((T, d)).astype(np.float32)
+    block = example.Block(dev(w1), dev(w2), None, k, T, renormalize=True)
+    block.forward(x, z)
+    d_x, d_logits = block.backward(z, dev(dy))
+    torch.cuda.synchronize()
+    idx, wt, row_of, offs = block.idx.cpu().numpy(), f64(block.weight), block.row_of.cpu().numpy(), block.offsets.cpu().numpy()
+    q1, s1 = O.quantize_weights(w1)
+    q2, s2 = O.quantize_weights(w2)
+    turn = lambda q, s: (q.transpose(0, 2, 1), s.transpose(0, 2, 1))  # noqa: E731
+    d_rows = np.zeros((T * k, d), np.float32)
+    d_rows[row_of] = (np.float32(wt)[:, :, None] * dy[:, None]).reshape(T * k, d)
+    qv, qs = O.quantize_rows(d_rows, "e5m2")
+    d_h, _ = O.expert_matmul(qv[:, :d], qs, *turn(q2, s2), offs)
+    d_h = np.where(f64(block.h_q[0])[:, :f] != 0, d_h, 0)
+    qv, qs = O.quantize_rows(d_h.astype(np.float32), "e5m2")
+    d_rows, _ = O.expert_matmul(qv[:, :f], qs, *turn(q1, s1), offs)
+    want = d_rows[row_of].reshape(T, k, d).sum(1)
+    # two roundings to bfloat16 of at most 2^-8; now and then a code of e5m2 on a border, a part in a million of them
+    assert np.linalg.norm(f64(d_x) - want) < 2.0 ** -8 * np.linalg.norm(want)
+    d_weight = (f64(block.y_rows)[row_of].reshape(T, k, d) * dy[:, None].astype(np.float64)).sum(2)
+    mag_w = (np.abs(f64(block.y_rows))[row_of].reshape(T, k, d) * np.abs(dy)[:, None]).sum(2)
+    want, mag = O.route_loss_gradient(f64(z), idx, "softmax", d_weight, None, True)
+    _, mag_w = O.route_loss_gradient(f64(z), idx, "softmax", mag_w, None, True)
+    # the gradient of the weights is a float32 sum of d products (counted d + 2 roundings), then the gradient's own tolerance
+    assert np.all(np.abs(f64(d_logits) - want) <= (d + 2) * H * mag_w + 2 * (spread(f64(z)) + 64) * H * mag + 2.0 ** -130)
+    block.close()
