@@ -218,8 +218,9 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 // Many rows an expert.  An item is up to TM * 64 rows of one expert and 256 outputs; a workgroup, one per CU, takes every
 // gridDim-th of them.  Both operands go straight from memory into a ring of NS stages in LDS, a stage being one block of 128
 // inputs, its scales among them; the requests run ahead of the products without regard to where an item ends, so the first
-// stages of an item arrive, and the results of the one before leave, under products.  Eight wavefronts as 2 x 4: wavefront
-// (wn, wm) has 128 outputs (one scale) and the row tiles wm, wm + 4, ..
+// stages of an item arrive, and the results of the one before leave, under products.  Items of up
+// to 256 rows: eight wavefronts as 2 x 4, wavefront (wn, wm) with 128 outputs (one scale) and the row tiles wm, wm + 4, ..; of up to 64 rows:
+// 8 x 1, 32 outputs and all row tiles each (4 + 4 of 16 conversions a block of inputs, where 2 x 4 would take 8 + 1).
 //
 // LDS, a stage: 16 weight tiles of 2 KiB, 64 bytes more behind each; rows of 128 bytes whose 16-byte pieces are
 // exchanged among themselves, piece c of row r at place c ^ (r / 2 % 8); 256 bytes of scales from each wavefront (rows: the
@@ -228,16 +229,18 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 // The outputs are dealt to the matrix instruction's 16 rows so that what a lane stores at once is 16 bytes, and what the four lanes of
 // a row store is 64 bytes side by side: with RUN = 16 / bytes of a result, row i of the a-th product is output
 // 4 RUN (4 a / RUN) + RUN (i / 4) + 4 a % RUN + i % 4 of the wavefront's 128 (a lane's four results of a product are rows 4 (lane / 16) ..).
+// (Of 32 outputs a lane has 8 codes at most.)
 // With 64 bytes a lane in a row, stores of 16 bytes went to 64 places at once: an item ended 5 us later.
 constexpr int MATMUL_W_TILE = FP8_TILE + 64;
-// The shape of an item: up to TM * 64 rows and WN blocks of 128 outputs; its wavefronts as WN x WM.
-template <int WN_, int TM_>
+// The shape of an item: up to TM * 64 rows and 256 outputs; a wavefront has OT tiles of 16 outputs and every WM-th row tile.
+template <int TM_, int OT_>
 struct MatmulShape {
-    static constexpr int WN = WN_, TM = TM_, WM = 8 / WN, MC = TM * 4 / WM;  // MC: most row tiles of a wavefront
-    static constexpr int W = WN * 8 * MATMUL_W_TILE, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S, TABLE = 4 * PGMOE_MAX_EXPERTS * 4;
-    static constexpr int NS = (160 * 1024 - TABLE) / STAGE < 4 ? (160 * 1024 - TABLE) / STAGE : 4, BYTES = NS * STAGE + TABLE;
-    static constexpr int LOADS = 2 * WN + TM + 1;
-    static_assert(NS >= 2 && TM * 4 % WM == 0, "a ring, and as many row tiles for every wavefront");
+    static constexpr int TM = TM_, OT = OT_, COLS = 16 / OT, WM = 8 / COLS, MC = TM * 4 / WM;  // MC: most row tiles of a wavefront
+    static constexpr int W = 16 * MATMUL_W_TILE, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
+    static constexpr int TABLE = 4 * PGMOE_MAX_EXPERTS * 4, MAXIMA = OT < 8 ? 8 * 64 * 4 : 0;
+    static constexpr int NS = (160 * 1024 - TABLE - MAXIMA) / STAGE, BYTES = NS * STAGE + TABLE + MAXIMA;
+    static constexpr int LOADS = 4 + TM + 1;
+    static_assert(NS >= 2 && MC <= 4 && (OT == 8 || (OT == 2 && WM == 1)), "a ring; one of the two wavefront shapes below");
 };
 constexpr int TILE_THREADS = 512, TILE_GROUPS = 256;  // workgroups: one per CU
 
@@ -278,9 +281,9 @@ struct MatmulItems {
             lo[q] = max(0, min(lo[q], a.rows));
             n[q] = max(lo[q], min(n[q], a.rows)) - lo[q];
         }
-        cols = (a.NB + R::WN - 1) / R::WN;
+        cols = (a.NB + 1) / 2;
         int most = TM * 64;
-        if (R::MC > 1) {
+        if (R::OT == 8) {
             float best = INFINITY;
             static_for<R::MC>([&](auto u_) {
                 constexpr int UNIT = 16 * R::WM, MOST = UNIT * (R::MC - decltype(u_)::value);
@@ -329,7 +332,7 @@ struct MatmulItems {
         const int before = e ? __builtin_amdgcn_readfirstlane(table[e - 1]) : 0, first = __builtin_amdgcn_readfirstlane(table[PGMOE_MAX_EXPERTS + e]);
         const int rows = __builtin_amdgcn_readfirstlane(table[2 * PGMOE_MAX_EXPERTS + e]), each = __builtin_amdgcn_readfirstlane(table[3 * PGMOE_MAX_EXPERTS + e]);
         const int k = chunk - before;
-        return {e, first + k * each, max(1, min(each, rows - k * each)), (turn - group * cols) * R::WN};
+        return {e, first + k * each, max(1, min(each, rows - k * each)), (turn - group * cols) * 2};
     }
 };
 
@@ -357,8 +360,8 @@ struct MatmulRequests {
             item += gridDim.x;
             left = a.KB;
             const size_t block = (size_t)it.expert * a.NB + it.nb;
-            const int last = it.nb + R::WN <= a.NB ? R::WN * 8 - 1 : 7;  // an odd last block of outputs has no neighbour
-            w_src = a.w + (block * 8 + min(wave * R::WN, last)) * a.KB * FP8_TILE;
+            const int last = it.nb + 1 < a.NB ? 15 : 7;  // an odd last block of outputs has no neighbour
+            w_src = a.w + (block * 8 + min(wave * 2, last)) * a.KB * FP8_TILE;
             w_second = wave * 2 < last ? (unsigned)a.KB * FP8_TILE : 0;
             x_src = a.x + (size_t)it.row0 * a.x_stride;
             x_last = it.nrows - 1;
@@ -369,8 +372,8 @@ struct MatmulRequests {
             s_last = wave < 4 ? it.nrows - 1 : (last == 15 ? 1 : 0);
         }
         const unsigned to = lds + stage;
-        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * R::WN * MATMUL_W_TILE);
-        if (R::WN == 2) load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
+        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * 2 * MATMUL_W_TILE);
+        load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
         w_src += FP8_TILE;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -401,8 +404,8 @@ __device__ inline void wait_for_loads(int later, int tiles) {  // uniform; later
 // The products of one item.  stored: row tiles whose results the wavefront stored behind the requests that are outstanding.
 template <int XQ, typename R, int MC, int RUN, int STORES>
 __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<R> &items, MatmulRequests<R> &rq, const char *ring, unsigned &stage, int wave, int stored,
-                                     floatx4 (&acc)[8][MC > 0 ? MC : 1]) {
-    const int wn = wave & (R::WN - 1), wm = wave / R::WN;
+                                     floatx4 (&acc)[R::OT][MC > 0 ? MC : 1]) {
+    const int wn = wave % R::COLS, wm = wave / R::COLS;
     constexpr int PER = RUN / 4;  // products of a run
     auto place = [](int t) { return t / PER * PER * MATMUL_W_TILE + t % PER * 64; };
     for (int kb = 0; kb < a.KB; ++kb) {
@@ -415,27 +418,79 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<R> &
         if (MC > 0) {
             const int lane = lane_again(), g = lane >> 4, i16 = lane & 15;
             const int o0 = RUN * (i16 >> 2) + (i16 & 3);  // this lane's output of product 0
-            const char *w_at = ring + (wn * 8 + (o0 >> 4)) * MATMUL_W_TILE + (o0 & 15) * 16 + g * 256;
+            const char *w_at = ring + (wn * R::OT + (o0 >> 4)) * MATMUL_W_TILE + (o0 & 15) * 16 + g * 256;
             const char *x_at = ring + R::W + (wm * 16 + i16) * FP8_BLOCK;
             const int x_low = (g ^ (i16 >> 1)) << 4, x_high = ((4 + g) ^ (i16 >> 1)) << 4;
             const char *s_at = ring + R::W + R::X;
-            Operand x[MC > 0 ? MC : 1];
             float s[MC > 0 ? MC : 1];
-            const float sw = *reinterpret_cast<const float *>(s_at + stage + 4 * 256 + wn * 4);
+            const float sw = *reinterpret_cast<const float *>(s_at + stage + 4 * 256 + wn * R::OT / 8 * 4);
 #pragma unroll
-            for (int m = 0; m < MC; ++m) {
+            for (int m = 0; m < MC; ++m) s[m] = sw * *reinterpret_cast<const float *>(s_at + stage + ((wm + R::WM * m) * 16 + i16) * 4);
+            auto row_codes = [&](int m, intx4(&to)[2]) {
                 const char *r = x_at + stage + m * 16 * R::WM * FP8_BLOCK;
-                x[m] = operand<XQ>(*reinterpret_cast<const intx4 *>(r + x_low), *reinterpret_cast<const intx4 *>(r + x_high));
-                s[m] = sw * *reinterpret_cast<const float *>(s_at + stage + ((wm + R::WM * m) * 16 + i16) * 4);
+                to[0] = *reinterpret_cast<const intx4 *>(r + x_low);
+                to[1] = *reinterpret_cast<const intx4 *>(r + x_high);
+            };
+            auto codes = [&](int t, intx4(&to)[2]) {
+                to[0] = *reinterpret_cast<const intx4 *>(w_at + stage + place(t));
+                to[1] = *reinterpret_cast<const intx4 *>(w_at + stage + place(t) + 1024);
+            };
+            Operand x[R::OT == 8 && MC > 0 ? MC : 1];
+            if constexpr (R::OT == 8) {
+#pragma unroll
+                for (int m = 0; m < MC; ++m) {
+                    intx4 raw[2];
+                    row_codes(m, raw);
+                    x[m] = operand<XQ>(raw[0], raw[1]);
+                }
             }
             // A step is two chains of products.  Beside them run what the step before left to do (its sums into the accumulators) and the
             // conversion of weights that come next, dealt out behind the products one by one: the vector unit's work fits under the
             // matrix cores' then, in a wavefront by itself.
-            if constexpr (MC == 1) {  // one row tile: the chains are two output tiles
-                auto codes = [&](int t, intx4(&to)[2]) {
-                    to[0] = *reinterpret_cast<const intx4 *>(w_at + stage + place(t));
-                    to[1] = *reinterpret_cast<const intx4 *>(w_at + stage + place(t) + 1024);
-                };
+            if constexpr (R::OT == 2) {  // the chains are the two output tiles; rows come one tile after the other
+                intx4 raw[2];
+                codes(0, raw);
+                Operand w[2], x_next;
+                w[0] = operand<PGMOE_E4M3>(raw[0], raw[1]);
+                codes(1, raw);
+                w[1] = operand<PGMOE_E4M3>(raw[0], raw[1]);
+                row_codes(0, raw);
+                x[0] = operand<XQ>(raw[0], raw[1]);
+                if (MC > 1) row_codes(1, raw);
+                floatx4 before[2];
+                static_for<MC>([&](auto m_) {
+                    constexpr int m = decltype(m_)::value;
+                    __builtin_amdgcn_sched_barrier(0);
+                    floatx4 p[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j].part[i], x[0].part[i], p[j], 0, 0, 0);
+                    if constexpr (m > 0) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[j][m - 1][v] = fmaf(s[m - 1], before[j][v], acc[j][m - 1][v]);
+                    }
+                    if constexpr (m + 1 < MC) {
+                        x_next = operand<XQ>(raw[0], raw[1]);
+                        if constexpr (m + 2 < MC) row_codes(m + 2, raw);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) before[j] = p[j];
+                    x[0] = x_next;
+                });
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[j][MC - 1][v] = fmaf(s[MC - 1], before[j][v], acc[j][MC - 1][v]);
+            } else if constexpr (MC == 1) {  // one row tile: the chains are two output tiles
                 intx4 next[2][2];
                 codes(0, next[0]);
                 codes(1, next[1]);
@@ -540,72 +595,107 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<R> &
 }
 
 // Stores of one row tile of a wavefront whose 128 outputs are all there.
-template <typename Y, bool VEC>
+template <typename Y, bool VEC, int OT>
 constexpr int tile_stores() {
-    if constexpr (std::is_void<Y>::value) return 3;
-    else return VEC ? (sizeof(Y) == 4 ? 8 : 4) : 32;
+    if constexpr (std::is_void<Y>::value) return OT == 8 ? 3 : 1;
+    else return VEC ? (sizeof(Y) == 4 ? OT : OT / 2) : 4 * OT;
 }
-template <typename Y>
-constexpr int run_of() {  // results in 16 bytes
-    if constexpr (std::is_void<Y>::value) return 16;
+template <typename Y, int OT>
+constexpr int run_of() {  // results in 16 bytes, as far as a wavefront's outputs go
+    if constexpr (std::is_void<Y>::value) return OT == 8 ? 16 : 8;
     else return 16 / sizeof(Y);
 }
 
 template <int XQ, typename Y, int YQ, bool VEC, typename R, int MC>
 __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<R> &items, MatmulRequests<R> &rq, const MatmulItem &it, char *ring, unsigned &stage, int wave,
                                   int stored) {
-    constexpr int STORES = tile_stores<Y, VEC>(), RUN = run_of<Y>();
-    floatx4 acc[8][MC > 0 ? MC : 1];
+    constexpr int RUN = run_of<Y, R::OT>(), STORES = tile_stores<Y, VEC, R::OT>(), OT = R::OT;
+    floatx4 acc[OT][MC > 0 ? MC : 1];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < OT; ++i)
 #pragma unroll
         for (int m = 0; m < MC; ++m) acc[i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
     matmul_k_loop<XQ, R, MC, RUN, STORES>(a, items, rq, ring, stage, wave, stored, acc);
-    const int lane = lane_again(), wn = wave & (R::WN - 1), wm = wave / R::WN;
-    const int block = it.nb + wn, o = block * FP8_BLOCK + RUN * (lane >> 4);  // run r of the lane begins at o + 4 RUN r
+    const int lane = lane_again(), wn = wave % R::COLS, wm = wave / R::COLS;
+    const int block = it.nb + wn * OT / 8, o = it.nb * FP8_BLOCK + wn * OT * 16 + RUN * (lane >> 4);  // run r of the lane begins at o + 4 RUN r
+    if (OT == 8 && block >= a.NB) return 0;
+    if (a.relu) {
+#pragma unroll
+        for (int m = 0; m < MC; ++m)
+#pragma unroll
+            for (int i = 0; i < OT; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][m][v] = relu_of(acc[i][m][v]);
+    }
+    float amax[MC > 0 ? MC : 1];  // of a row's block, where that is quantised
+    bool unusual = false;
+    if constexpr (std::is_void<Y>::value) {
+        auto largest = [&](auto of) {
+#pragma unroll
+            for (int m = 0; m < MC; ++m) {
+                float l = 0.f;
+#pragma unroll
+                for (int i = 0; i < OT; ++i)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) l = maximum(l, of(acc[i][m][v]));
+                l = maximum(l, __shfl_xor(l, 16));
+                amax[m] = maximum(l, __shfl_xor(l, 32));
+            }
+            if constexpr (OT < 8) {  // four wavefronts have a block's outputs.  (No barrier of the compiler's: it would wait for the requests.)
+                float *maxima = reinterpret_cast<float *>(ring + R::NS * R::STAGE + R::TABLE);
+#pragma unroll
+                for (int m = 0; m < MC; ++m)
+                    if (lane < 16) maxima[wave * 64 + m * 16 + lane] = amax[m];
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+                for (int m = 0; m < MC; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) amax[m] = maximum(amax[m], maxima[((wave & 4) + i) * 64 + m * 16 + (lane & 15)]);
+            }
+        };
+        largest([](float v) { return fabsf(v); });
+#pragma unroll
+        for (int m = 0; m < MC; ++m) {
+            unusual |= fp8_unusual<YQ>(amax[m]);
+            if constexpr (OT < 8) {  // the other block's rows too: if one wavefront looks again all do, they meet at barriers there
+                const float *others = reinterpret_cast<const float *>(ring + R::NS * R::STAGE + R::TABLE) + (4 - (wave & 4)) * 64 + m * 16 + (lane & 15);
+                unusual |= fp8_unusual<YQ>(maximum(maximum(others[0], others[64]), maximum(others[128], others[192])));
+            }
+        }
+        if (unusual) {
+            if (OT < 8) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            largest(finite_magnitude);
+        }
+    }
     if (block >= a.NB) return 0;
 #pragma unroll
     for (int m = 0; m < MC; ++m) {
         const int in_chunk = (wm + R::WM * m) * 16 + (lane & 15), row = it.row0 + in_chunk;
         const bool live = in_chunk < it.nrows;
-        if (a.relu) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][m][v] = relu_of(acc[i][m][v]);
-        }
         if constexpr (std::is_void<Y>::value) {
-            auto largest = [&](auto of) {
-                float l = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) l = maximum(l, of(acc[i][m][v]));
-                l = maximum(l, __shfl_xor(l, 16));
-                return maximum(l, __shfl_xor(l, 32));
-            };
-            float amax = largest([](float v) { return fabsf(v); });
-            const bool unusual = fp8_unusual<YQ>(amax);
-            if (unusual) amax = largest(finite_magnitude);
-            const float scale = fp8_scale<YQ>(amax);
-            uint32_t codes[8];
+            const float scale = fp8_scale<YQ>(amax[m]);
+            uint32_t codes[OT];
             auto quantise = [&](auto by) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) codes[i] = fp8_pack<YQ>(by(acc[i][m][0]), by(acc[i][m][1]), by(acc[i][m][2]), by(acc[i][m][3]));
+                for (int i = 0; i < OT; ++i) codes[i] = fp8_pack<YQ>(by(acc[i][m][0]), by(acc[i][m][1]), by(acc[i][m][2]), by(acc[i][m][3]));
             };
             if (unusual) quantise(Fp8CarefulDivisor(scale));
             else quantise(Fp8Divisor(scale));
             if (live) {
-                uint4 *q = reinterpret_cast<uint4 *>(a.y_q + (size_t)row * a.y_q_stride + o);
-                q[0] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
-                q[4] = make_uint4(codes[4], codes[5], codes[6], codes[7]);
-                if (lane < 16) a.y_scale[(size_t)block * a.y_scale_stride + row] = scale;
+                uint8_t *q = a.y_q + (size_t)row * a.y_q_stride + o;
+                if constexpr (OT == 8) {
+                    reinterpret_cast<uint4 *>(q)[0] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+                    reinterpret_cast<uint4 *>(q)[4] = make_uint4(codes[4], codes[5], codes[6], codes[7]);
+                } else {
+                    *reinterpret_cast<uint2 *>(q) = make_uint2(codes[0], codes[1]);
+                }
+                if (lane < 16 && (OT == 8 || (wave & 3) == 0)) a.y_scale[(size_t)block * a.y_scale_stride + row] = scale;
             }
         } else if (live) {
             if constexpr (VEC && sizeof(Y) == 2) {
                 typedef Y Yx8 __attribute__((ext_vector_type(8), aligned(8)));
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
+                for (int i = 0; i < OT; i += 2) {
                     const int at = o + 16 * i;
                     const floatx4 u = acc[i][m], v = acc[i + 1][m];
                     if (at + 4 < a.n_out)
@@ -615,7 +705,7 @@ __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<R> &ite
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) store_four<Y, VEC>(a, row, o + 4 * RUN * (4 * i / RUN) + 4 * i % RUN, acc[i][m]);
+                for (int i = 0; i < OT; ++i) store_four<Y, VEC>(a, row, o + 4 * RUN * (4 * i / RUN) + 4 * i % RUN, acc[i][m]);
             }
         }
     }
@@ -638,7 +728,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void matmul_tiles_kernel(const Mat
     for (int i = blockIdx.x;; i += gridDim.x) {
         const MatmulItem it = items.at(i);
         if (it.nrows == 0) break;  // uniform over the workgroup; every request has been waited for
-        const int rt = (it.nrows + 15) >> 4, own = max(0, (rt - wave / R::WN + R::WM - 1) / R::WM);
+        const int rt = (it.nrows + 15) >> 4, own = max(0, (rt - wave / R::COLS + R::WM - 1) / R::WM);
         switch (own) {  // uniform over the wavefront
 #define PG_BODY(MC_)                                                                                                                        \
     case MC_:                                                                                                                               \
@@ -665,9 +755,9 @@ static int launch_tiles(const MatmulArgs &a, hipStream_t s) {
         raised.fetch_or(1ull << (device & 63), std::memory_order_relaxed);
     }
     // chunks: at most the sum over the experts of ceil(rows / the smallest the kernel may choose), in whole eights
-    constexpr int UNIT = 16 * R::WM;
+    constexpr int UNIT = R::OT == 8 ? 16 * R::WM : R::TM * 64;
     const int64_t chunks = ((a.rows + (int64_t)(UNIT - 1) * std::min(a.E, a.rows)) / UNIT + 7) & ~(int64_t)7;
-    const unsigned groups = (unsigned)std::min<int64_t>(TILE_GROUPS, chunks * ((a.NB + R::WN - 1) / R::WN));
+    const unsigned groups = (unsigned)std::min<int64_t>(TILE_GROUPS, chunks * ((a.NB + 1) / 2));
     hipLaunchKernelGGL((matmul_tiles_kernel<XQ, Y, YQ, VEC, R>), dim3(groups), dim3(TILE_THREADS), R::BYTES, s, a);
     return PGMOE_OK;
 }
@@ -684,8 +774,8 @@ static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
     const int active = std::min(a.E, a.rows), mean = a.rows / active;
     const int64_t chunks16 = (a.rows + (int64_t)15 * active) / 16, items256 = (active + (int64_t)a.rows / 256) * ((a.NB + 1) / 2);
     if (mean > 8 && chunks16 * a.NB > TILE_GROUPS && (int64_t)a.x_stride < TILE_STRIDE_MAX) {
-        if (mean <= 48 || items256 < TILE_GROUPS / 2) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<2, 1>>(a, s);
-        return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<2, 4>>(a, s);
+        if (mean <= 48 || items256 < TILE_GROUPS / 2) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<1, 2>>(a, s);
+        return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<4, 8>>(a, s);
     }
     auto few = [&](auto ks_) {
         constexpr int KS = decltype(ks_)::value;
