@@ -237,7 +237,7 @@ template <int TM_, int OT_>
 struct MatmulShape {
     static constexpr int TM = TM_, OT = OT_, COLS = 16 / OT, WM = 8 / COLS, MC = TM * 4 / WM;  // MC: most row tiles of a wavefront
     static constexpr int W = 16 * MATMUL_W_TILE, X = TM * 64 * FP8_BLOCK, S = 8 * 256, STAGE = W + X + S;
-    static constexpr int TABLE = 4 * PGMOE_MAX_EXPERTS * 4, MAXIMA = OT < 8 ? 8 * 64 * 4 : 0;
+    static constexpr int TABLE = 3 * PGMOE_MAX_EXPERTS * 4, MAXIMA = OT < 8 ? 8 * 64 * 4 : 0;
     static constexpr int NS = (160 * 1024 - TABLE - MAXIMA) / STAGE, BYTES = NS * STAGE + TABLE + MAXIMA;
     static constexpr int LOADS = 4 + TM + 1;
     static_assert(NS >= 2 && MC <= 4 && (OT == 8 || (OT == 2 && WM == 1)), "a ring; one of the two wavefront shapes below");
@@ -252,10 +252,11 @@ __device__ inline int lane_again() {
     return lane;
 }
 
-// The items of a launch, looked up in a table of the experts in LDS: chunks up to and with the expert, its first row, its rows, rows of a chunk.
-// The chunks of an expert are its rows dealt evenly, in whole 16s, to as few chunks of at most 64 u rows as hold them.  u is the one
-// of 1 .. TM for which the launch should end first: rounds of one item a workgroup, times what a block of inputs costs an
-// item of u units on the mean, which is MATMUL_COST + u.
+// The items of a launch, looked up in a table of the experts in LDS: chunks up to and with the expert, its first row, its rows.
+// An expert's chunks are full ones of `most` rows and what is left over: of 270 rows 256 and 14, which take 4 + 1 units of work where two of 135
+// would take 3 + 3 (4096 rows of one expert of 1024 x 4096 37.9 -> 36.7 us, 32768 over 128 as long either way).  `most` is that of 1 .. MC units (16 WM rows)
+// for which the launch should end first: rounds of one item a workgroup, times what a block of inputs costs an item on the mean,
+// which is MATMUL_COST + its units.
 struct MatmulItem {
     int expert, row0, nrows, nb;  // nrows == 0: there are no more
 };
@@ -264,8 +265,7 @@ template <typename R>
 struct MatmulItems {
     static constexpr int TM = R::TM;
     const int *table;
-    int cols, total;  // column blocks; chunks
-    __device__ static int each_of(int n, int chunks) { return (((n + chunks - 1) / chunks) + 15) & ~15; }
+    int cols, total, most;  // column blocks; chunks; rows of one
     // Offsets are clamped to the rows there are, whatever they say.
     __device__ void build(const MatmulArgs &a, int *to) {
         const int lane = threadIdx.x & 63;
@@ -282,7 +282,7 @@ struct MatmulItems {
             n[q] = max(lo[q], min(n[q], a.rows)) - lo[q];
         }
         cols = (a.NB + 1) / 2;
-        int most = TM * 64;
+        most = TM * 64;
         if (R::OT == 8) {
             float best = INFINITY;
             static_for<R::MC>([&](auto u_) {
@@ -293,7 +293,7 @@ struct MatmulItems {
                 for (int q = 0; q < 4; ++q) {
                     const int c = (n[q] + MOST - 1) / MOST;
                     sum += c;
-                    cost += c ? (float)c * (float)(MATMUL_COST + (each_of(n[q], c) + UNIT - 1) / UNIT) : 0.f;
+                    cost += (float)(c * MATMUL_COST + (n[q] + UNIT - 1) / UNIT);
                 }
                 const int chunks = __builtin_amdgcn_readlane(wave_incl_scan(sum), 63);
 #pragma unroll
@@ -305,6 +305,7 @@ struct MatmulItems {
                 }
             });
         }
+        most = __builtin_amdgcn_readfirstlane(most);
         int before = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -315,7 +316,6 @@ struct MatmulItems {
                 to[e] = c_incl;
                 to[PGMOE_MAX_EXPERTS + e] = lo[q];
                 to[2 * PGMOE_MAX_EXPERTS + e] = n[q];
-                to[3 * PGMOE_MAX_EXPERTS + e] = c ? each_of(n[q], c) : 0;
             }
         }
         table = to;
@@ -330,9 +330,8 @@ struct MatmulItems {
 #pragma unroll
         for (int q = 0; q < 4; ++q) e += __popcll(__ballot(c[q] <= chunk));
         const int before = e ? __builtin_amdgcn_readfirstlane(table[e - 1]) : 0, first = __builtin_amdgcn_readfirstlane(table[PGMOE_MAX_EXPERTS + e]);
-        const int rows = __builtin_amdgcn_readfirstlane(table[2 * PGMOE_MAX_EXPERTS + e]), each = __builtin_amdgcn_readfirstlane(table[3 * PGMOE_MAX_EXPERTS + e]);
-        const int k = chunk - before;
-        return {e, first + k * each, max(1, min(each, rows - k * each)), (turn - group * cols) * 2};
+        const int rows = __builtin_amdgcn_readfirstlane(table[2 * PGMOE_MAX_EXPERTS + e]), from = (chunk - before) * most;
+        return {e, first + from, max(1, min(most, rows - from)), (turn - group * cols) * 2};
     }
 };
 
