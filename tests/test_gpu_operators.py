@@ -308,6 +308,18 @@ def test_quantize_rows_reads_strided_rows_and_passes_32_bits(B):
     assert np.array_equal(f64(far_q.contiguous()), want_q) and np.array_equal(f64(scale), want_s)
 
 
+def test_quantize_rows_of_more_rows_than_a_grid_has_places(B):
+    say("quantize rows many")
+    T = 16 * 65535 + 2345
+    x = torch.randn(T, 24, device="cuda", generator=torch.Generator("cuda").manual_seed(5))
+    q, scale = torch.full((T, 128), 1.0, device="cuda").to(torch.float8_e4m3fn), torch.zeros(1, T, device="cuda")
+    B.quantize_rows(x, q, scale)
+    for rows in (slice(0, 40), slice(T // 2, T // 2 + 40), slice(T - 40, T)):
+        want_q, want_s = O.quantize_rows(f64(x[rows]).astype(np.float32), "e4m3")
+        assert np.array_equal(f64(q[rows]), want_q) and np.array_equal(f64(scale[:, rows]), want_s)
+    assert bool((scale > 0).all()) and not bool(q[:, 24:].view(torch.uint8).any())
+
+
 @pytest.mark.parametrize("E,n_in,n_out,dtype", [(1, 1, 1, "f32"), (2, 128, 128, "bf16"), (3, 200, 300, "f32"), (1, 129, 257, "bf16"), (2, 384, 136, "f16"), (5, 64, 520, "bf16")])
 def test_quantize_weights(B, E, n_in, n_out, dtype):
     say("quantize weights", E, n_in, n_out, dtype)
@@ -520,6 +532,94 @@ def test_expert_matmul_passes_on_what_is_not_finite(B):
     p.run(q, s, relu=True)
     got = f64(q)
     assert np.isnan(got[5, :260]).all() and np.isfinite(f64(s)).all() and not np.isnan(np.delete(got, [5, 9], 0)).any()
+
+
+# Enough rows for the tiled kernels, of 64 rows and of up to 256: experts without rows, with one, with a few more than a whole chunk.
+TILED = {64: [20, 0, 65, 3, 64, 17, 1, 40] * 6, 256: [60, 1, 0, 17, 130, 64, 257, 31] * 5}
+
+
+@pytest.mark.parametrize("tile", TILED)
+@pytest.mark.parametrize("n_in,n_out", [(200, 517), (640, 640), (517, 644), (1, 1100), (129, 520)])
+def test_expert_matmul_in_tiles(B, tile, n_in, n_out):
+    say("matmul tiles", tile, n_in, n_out)
+    p = Product(B, TILED[tile], n_in, n_out, "e5m2" if n_in % 2 else "e4m3")
+    for out in ("f32", "bf16", "f16", "e4m3", "e5m2"):
+        p.check(out, relu=out in ("f32", "e4m3"))
+
+
+@pytest.mark.parametrize("tile", TILED)
+def test_expert_matmul_in_tiles_of_rows_and_results_with_strides(B, tile):
+    say("matmul tiles strides", tile)
+    n_out = 516
+    p = Product(B, TILED[tile], 200, n_out)
+    want, mag = p.want(False)
+    wide = torch.zeros(p.R, 384 + 16, device="cuda").to(torch.float8_e4m3fn)
+    wide[:, 16:16 + 256] = p.x_q
+    p.x_q = wide[:, 16:16 + 256]
+    scale = torch.full((2, p.R + 9), float("nan"), device="cuda")
+    scale[:, 4:4 + p.R] = p.x_scale
+    p.x_scale = scale[:, 4:4 + p.R]
+    for lead, width in ((0, 520), (1, 524), (4, 524), (2, 521)):
+        for out in ("f32", "bf16"):
+            y = torch.full((p.R, width), 7.0, dtype=TORCH[out], device="cuda")
+            p.run(y[:, lead:lead + n_out])
+            got = f64(y)
+            assert np.all(np.abs(got[:, lead:lead + n_out] - want) <= p.err(mag) + HALF[out] * (np.abs(want) + p.err(mag)) + TINY[out])
+            assert np.all(got[:, :lead] == 7.0) and np.all(got[:, lead + n_out:] == 7.0)
+
+
+@pytest.mark.parametrize("tile", TILED)
+def test_expert_matmul_in_tiles_with_offsets_that_are_none(B, tile):
+    say("matmul tiles offsets", tile)
+    p = Product(B, TILED[tile], 130, 600)
+    want, mag = p.want(False)
+    live = int(p.offs[-2]) - 5
+    for offs in (np.minimum(p.offs, live), np.where(np.arange(p.E + 1) == p.E, 1 << 30, p.offs)):
+        p.offsets = torch.from_numpy(offs.astype(np.int32)).cuda()
+        rows = min(int(offs[-1]), p.R)
+        y = torch.full((p.R + 300, 600), 7.0, device="cuda")
+        p.run(y[:p.R])
+        got = f64(y)
+        assert np.all(np.abs(got[:rows] - want[:rows]) <= p.err(mag[:rows]) + H * np.abs(want[:rows])) and np.all(got[rows:] == 7.0)
+    g = np.random.default_rng(9)
+    for offs in (g.integers(-(1 << 31), 1 << 31, p.E + 1), g.integers(-50, p.R + 50, p.E + 1), p.offs[::-1].copy()):
+        p.offsets = torch.from_numpy(offs.astype(np.int32)).cuda()
+        y = torch.full((p.R + 300, 600), 7.0, device="cuda")
+        p.run(y[:p.R])
+        assert np.all(f64(y)[p.R:] == 7.0)
+
+
+@pytest.mark.parametrize("tile", TILED)
+@pytest.mark.parametrize("column", [100, 200, 517])
+def test_expert_matmul_in_tiles_passes_on_what_is_not_finite(B, tile, column):
+    """A weight that is NaN, a row with a NaN code and a row of zeros: nothing else changes, neither result nor scale."""
+    say("matmul tiles not finite", tile, column)
+    p = Product(B, TILED[tile], 300, 520)
+    e = p.E - 4
+    rows = slice(int(p.offs[e]), int(p.offs[e + 1]))
+    zero, odd = int(p.offs[4]) + 3, int(p.offs[4]) + 4        # rows of another expert
+    flat = p.w_q.view(torch.uint8).reshape(p.E, -1)
+    at = O.tile_positions(300, 520)[:, column]
+
+    def run(nan):
+        flat[e, torch.from_numpy(at).cuda()] = 0
+        p.x_q.view(torch.uint8)[[zero, odd]] = 0
+        if nan:
+            flat[e, int(at[17])] = 0x7F
+            p.x_q.view(torch.uint8)[odd, 7] = 0x7F
+        q, s, y = torch.zeros(p.R, 640, device="cuda").to(torch.float8_e4m3fn), torch.zeros(5, p.R, device="cuda"), torch.zeros(p.R, 520, device="cuda")
+        p.run(q, s)
+        p.run(y)
+        return f64(q)[:, :520], f64(s), f64(y)
+
+    q0, s0, y0 = run(False)
+    q1, s1, y1 = run(True)
+    bad = np.zeros((p.R, 520), bool)
+    bad[rows, column] = True
+    bad[odd] = True
+    assert np.array_equal(np.isnan(y1), bad) and np.array_equal(y1[~bad], y0[~bad])
+    assert np.array_equal(np.isnan(q1), bad) and np.array_equal(q1[~bad], q0[~bad]) and np.array_equal(s1, s0)
+    assert np.all(q1[zero] == 0) and np.all(s1[:, [zero, odd]] == 2.0 ** -126) and (np.delete(s1, [zero, odd], 1) > 1e-6).all()
 
 
 def test_gradient_of_rows_through_the_transposed_weights(B):

@@ -103,6 +103,8 @@ def test_bad_arguments_of_quantising_and_of_products_are_refused():
     refused(L.pgmoe_quantize_rows(P, 199, B.F32, 8, None, 1, r, None), "x_stride")
     refused(L.pgmoe_quantize_rows(None, 200, B.F32, 8, None, 1, r, None), "x is NULL")
     refused(L.pgmoe_quantize_rows(P + 2, 200, B.F32, 8, None, 1, r, None), "aligned")
+    big = byref(rows(rows=8, cols=1 << 22, q_stride=1 << 22))
+    refused(L.pgmoe_quantize_rows(P, 1 << 22, B.F32, (1 << 31) - 1, P, 1, big, None), "launch")
     refused(L.pgmoe_quantize_weights(P, B.F32, None, None, None), "both")
     refused(L.pgmoe_quantize_weights(None, B.F32, w, None, None), "w is NULL")
     refused(L.pgmoe_quantize_weights(P, B.E5M2, w, None, None), "w_dtype")
