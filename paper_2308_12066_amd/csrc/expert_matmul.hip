@@ -122,17 +122,16 @@ __device__ inline void store_four(const MatmulArgs &a, int r, int o, floatx4 v) 
     }
 }
 
-// Few rows an expert: the stream of weights.  Operands straight from memory into registers, the next blocks of inputs requested before those at
-// hand are multiplied.  A workgroup takes 16 rows and 8 / KS tiles of 16 outputs, a wavefront one of them and one KS-th of the inputs; the
-// parts are added up in LDS, in order.  KS > 1, and four blocks at once, where launches have too few tiles to keep the memory busy
-// (2 rows, 1024 x 4096: 5.9 us with KS = 1, 4.4 with 4; 4096 x 1024: 13.2, 5.9, with 8 4.5).  With many tiles one block at a time and more
-// wavefronts: 5.0 to 5.7 TB/s of weights (128 rows over some fifty experts of 4096 x 1024 39.5 us, with four blocks at once 42.4; a plain read 6.2).
-// Y = void: quantised again, YQ, which takes a whole block of 128 outputs, KS = 1.
+// Few rows an expert: the stream of weights.  Operands straight from memory into registers, the next block of inputs requested before the one
+// at hand is multiplied.  A workgroup takes 16 rows and 8 / KS tiles of 16 outputs, a wavefront one of them and one KS-th of the inputs; the
+// parts are added up in LDS, in order.  One workgroup's stream is bound by its CU: 512 KB in 10.2 us (2 rows, 4096 x 1024, KS = 1), so few
+// tiles go to more CUs (KS = 8: 4.1), and long sums to more wavefronts (512 rows over 64 experts of 4096 x 1024 56.1 us with KS = 1, 51.0 with 8:
+// 5.3 TB/s of weights, a plain read on this chip 6.2).  Two and four blocks requested at once were no faster where KS suits the launch.
+// Y = void: quantised again, YQ, which takes a whole block of 128 outputs, KS = 1 (twice the wavefronts for half the inputs each: no faster).
 constexpr int FEW_THREADS = 512;
 template <int XQ, typename Y, int YQ, bool VEC, int KS>
 __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const MatmulArgs a) {
-    constexpr int TILES = 8 / KS;             // of a workgroup
-    constexpr int FEW_BATCH = KS > 1 ? 4 : 1;  // blocks of inputs requested at once
+    constexpr int TILES = 8 / KS;  // of a workgroup
     __shared__ float amax_of[8][16];
     __shared__ floatx4 parts[KS > 1 ? 8 : 1][64];
     const int part = blockIdx.x % KS, item = blockIdx.x / KS, chunk = item / a.NB, nb = item - chunk * a.NB;
@@ -143,36 +142,29 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
     const uint8_t *x = a.x + (size_t)row * a.x_stride + (lane >> 4) * 16;
     const uint8_t *w = a.w + (((size_t)ci.expert * a.NB + nb) * 8 + tile) * a.KB * FP8_TILE + lane * 16;
     const float *sx = a.x_scale + row, *sw = a.w_scale + ((size_t)ci.expert * a.NB + nb) * a.KB;
-    struct Batch {
-        intx4 w[FEW_BATCH][2], x[FEW_BATCH][2];
-        float s[FEW_BATCH], t[FEW_BATCH];
+    struct Block {
+        intx4 w[2], x[2];
+        float s, t;
     };
-    auto load = [&](Batch &b, int kb) {  // past the end the last block again, which nobody uses: no conditions in front of loads
-#pragma unroll
-        for (int i = 0; i < FEW_BATCH; ++i) {
-            const int k = min(kb + i, a.KB - 1);
-            const uint8_t *wk = w + (size_t)k * FP8_TILE, *xk = x + (size_t)k * FP8_BLOCK;
-            b.w[i][0] = *reinterpret_cast<const intx4 *>(wk);
-            b.w[i][1] = *reinterpret_cast<const intx4 *>(wk + 1024);
-            b.x[i][0] = *reinterpret_cast<const intx4 *>(xk);
-            b.x[i][1] = *reinterpret_cast<const intx4 *>(xk + 64);
-            b.s[i] = sx[(size_t)k * a.x_scale_stride];
-            b.t[i] = sw[k];
-        }
+    auto load = [&](Block &b, int kb) {
+        const int k = min(kb, a.KB - 1);  // past the end the last block again, which nobody uses: no conditions in front of loads
+        const uint8_t *wk = w + (size_t)k * FP8_TILE, *xk = x + (size_t)k * FP8_BLOCK;
+        b.w[0] = *reinterpret_cast<const intx4 *>(wk);
+        b.w[1] = *reinterpret_cast<const intx4 *>(wk + 1024);
+        b.x[0] = *reinterpret_cast<const intx4 *>(xk);
+        b.x[1] = *reinterpret_cast<const intx4 *>(xk + 64);
+        b.s = sx[(size_t)k * a.x_scale_stride];
+        b.t = sw[k];
     };
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    Batch at, next;
+    Block at, next;
     load(at, first);
-    for (int kb = first; kb < last; kb += FEW_BATCH) {
-        load(next, kb + FEW_BATCH);
+    for (int kb = first; kb < last; ++kb) {
+        load(next, kb + 1);
+        const floatx4 p = product(operand<PGMOE_E4M3>(at.w[0], at.w[1]), operand<XQ>(at.x[0], at.x[1]));
+        const float s = at.s * at.t;
 #pragma unroll
-        for (int i = 0; i < FEW_BATCH; ++i) {
-            if (kb + i >= last) break;  // uniform
-            const floatx4 p = product(operand<PGMOE_E4M3>(at.w[i][0], at.w[i][1]), operand<XQ>(at.x[i][0], at.x[i][1]));
-            const float s = at.s[i] * at.t[i];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] = fmaf(s, p[v], acc[v]);
-        }
+        for (int v = 0; v < 4; ++v) acc[v] = fmaf(s, p[v], acc[v]);
         at = next;
     }
     if constexpr (KS > 1) {
@@ -762,36 +754,35 @@ static int launch_tiles(const MatmulArgs &a, hipStream_t s) {
 }
 template <int XQ, typename Y, int YQ, bool VEC>
 static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
-    // Which kernel, by rows an expert (on the mean) and by what there is to deal out; both sides in us a launch, bf16 results:
-    //  * few rows, to 8 an expert: the tiles would be empty mostly (64 experts of 1024 x 4096: 4 rows each 50.0, in tiles of 64 rows 51.0; 8 rows
-    //    52.5 / 51.8, 16 rows 64.8 / 53.1); also launches of at most one workgroup a CU in 16-row chunks (32 rows for each of 8 experts of
-    //    4096 x 1024 20.7 / 47.5, 64 for one 20.2 / 46.6; not 512 for one of 1024 x 4096 22.0 / 17.0), and rows too far apart for the tiles;
-    //  * tiles of 64 rows, three stages in flight, to 48 rows an expert (32 for each of 64 59.9, in tiles of 256 rows 65.8; 64 rows 86 / 77) and where
-    //    tiles of 256 leave half the CUs without an item (512 for each of 8 experts of 2048 x 768 31.7 / 34.9; not 128 for each of 8 of
-    //    1024 x 4096 30.5 / 25.7);
-    //  * tiles of up to 256 rows for the others.
-    const int active = std::min(a.E, a.rows), mean = a.rows / active;
-    const int64_t chunks16 = (a.rows + (int64_t)15 * active) / 16, items256 = (active + (int64_t)a.rows / 256) * ((a.NB + 1) / 2);
-    if (mean > 8 && chunks16 * a.NB > TILE_GROUPS && (int64_t)a.x_stride < TILE_STRIDE_MAX) {
-        if (mean <= 48 || items256 < TILE_GROUPS / 2) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<1, 2>>(a, s);
+    // Which kernel, by what there is to deal out; both sides in us a launch, bf16 results, rows dealt to the experts at random:
+    //  * few rows, to 8 an expert: the tiles would be empty mostly (64 experts of 1024 x 4096, 8 rows each 50.4, in tiles of 64 rows 52.1; 12 rows
+    //    54.7 / 52.4); also launches of at most two items of 16 rows a CU (64 rows for each of 8 experts of 4096 x 1024 23.3 / 44.2, 128 41.0 / 43.8,
+    //    256 for one of 1024 x 4096 11.8 / 15.0; not 512 21.3 / 15.1, 48 for each of 8 19.5 / 14.9), and rows too far apart for the tiles;
+    //  * tiles of 64 rows or of up to 256, by rounds of one item a workgroup, of which the larger take 4 / 3 as long (32 for each of 64 experts of
+    //    1024 x 4096 55.9 / 63.6, 64 rows 79.7 / 75.8; 512 for each of 8 of 2048 x 768 26.5 / 31.0, 1024 46.3 / 39.4; 96 for each of 8 of
+    //    1024 x 4096 17.0 / 20.4, 128 27.1 / 24.4).  An expert has half a chunk more than its rows fill, on the mean.
+    // The inputs of few rows are split so that a wavefront has three blocks at least, further while workgroups are no more than two a CU: KS = 1 / 2 / 4 / 8
+    // take 33.9 / 33.2 / 32.3 / 43.0 for one row for each of 64 experts of 1024 x 4096 (eight blocks), 6.8 / 5.0 / 5.1 / 5.0 for 64 rows of one, 6.6 / 4.8 / 3.8 / 3.0
+    // for 16, 20.5 / 21.1 / 21.6 / 21.6 for 512 rows of one of 4096 x 1024, 38.2 / 31.5 / 25.5 / 23.7 for 64 for each of eight.
+    const int64_t active = std::min(a.E, a.rows), mean = a.rows / active, cols = (a.NB + 1) / 2;
+    const int64_t chunks16 = (a.rows + 15 * active) / 16, items16 = chunks16 * a.NB;
+    if (mean > 8 && items16 > 2 * TILE_GROUPS && (int64_t)a.x_stride < TILE_STRIDE_MAX) {
+        const auto rounds = [&](int most) { return (std::max(active, a.rows / most + active / 2) * cols + TILE_GROUPS - 1) / TILE_GROUPS; };
+        if (3 * rounds(64) <= 4 * rounds(256)) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<1, 2>>(a, s);
         return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<4, 8>>(a, s);
     }
     auto few = [&](auto ks_) {
         constexpr int KS = decltype(ks_)::value;
-        hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS>), dim3((unsigned)(chunks16 * a.NB * KS)), dim3(FEW_THREADS), 0, s, a);
+        hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS>), dim3((unsigned)(items16 * KS)), dim3(FEW_THREADS), 0, s, a);
+        return PGMOE_OK;
     };
-    if constexpr (!std::is_void<Y>::value) {  // the inputs split where items (16 rows, 128 outputs) are few
-        if (chunks16 * a.NB <= TILE_GROUPS / 8) {
-            few(std::integral_constant<int, 8>());
-            return PGMOE_OK;
-        }
-        if (chunks16 * a.NB <= TILE_GROUPS) {
-            few(std::integral_constant<int, 4>());
-            return PGMOE_OK;
-        }
+    if constexpr (!std::is_void<Y>::value) {
+        const auto split = [&](int ks) { return 3 * ks <= a.KB || (ks <= a.KB && ks * items16 <= 2 * TILE_GROUPS); };
+        if (split(8)) return few(std::integral_constant<int, 8>());
+        if (split(4)) return few(std::integral_constant<int, 4>());
+        if (split(2)) return few(std::integral_constant<int, 2>());
     }
-    few(std::integral_constant<int, 1>());
-    return PGMOE_OK;
+    return few(std::integral_constant<int, 1>());
 }
 template <int XQ, typename Y>
 static int launch_matmul_to(const MatmulArgs &a, hipStream_t s) {

@@ -534,6 +534,15 @@ def test_expert_matmul_passes_on_what_is_not_finite(B):
     assert np.isnan(got[5, :260]).all() and np.isfinite(f64(s)).all() and not np.isnan(np.delete(got, [5, 9], 0)).any()
 
 
+@pytest.mark.parametrize("counts", [[1, 0, 3], [17, 1] * 10, [9] * 40, [130]])
+@pytest.mark.parametrize("n_in,n_out", [(256, 100), (384, 700), (1000, 520), (1025, 132), (2048, 130), (3100, 65)])
+def test_expert_matmul_of_few_rows_with_its_inputs_split(B, counts, n_in, n_out):
+    say("matmul split", counts[:3], n_in, n_out)
+    p = Product(B, counts, n_in, n_out, "e5m2" if n_in % 2 else "e4m3")
+    for out in ("f32", "bf16", "e4m3"):
+        p.check(out, relu=out == "bf16")
+
+
 # Enough rows for the tiled kernels, of 64 rows and of up to 256: experts without rows, with one, with a few more than a whole chunk.
 TILED = {64: [20, 0, 65, 3, 64, 17, 1, 40] * 6, 256: [60, 1, 0, 17, 130, 64, 257, 31] * 5}
 
