@@ -68,7 +68,8 @@ struct QuantizeWeightsArgs {
 // One workgroup takes one 128 x 128 block of one expert and keeps it in registers: a thread has two patches of four inputs by
 // eight outputs, so that four inputs of an output are one dword of the forward tiles, and eight outputs of an input two of the
 // backward ones.  Both go out through LDS as whole tiles.  The forward image has 16 bytes more behind each tile: the 64 dwords a
-// wavefront writes at once are then on 64 banks.
+// wavefront writes at once are then on 64 banks.  128 experts of 1024 x 4096 bfloat16 in both orientations take 417 us, 5.15 TB/s read and
+// written, either order of the blocks; 8 of 512 x 2048 float32 in one 9.1.
 constexpr int QW_THREADS = 256;
 constexpr int QW_TILE = FP8_TILE + 16;
 template <typename L, bool VEC>

@@ -10,6 +10,10 @@
 // without their last four bits; hence the chosen neighbours (and the two groups at the border) are looked at once more, and a token where two of them
 // lie closer than CLOSE is decided in 64 bits.  Values that are equal because logit and bias are equal are no such case: either
 // way the lowest index wins.  16-bit logits without a bias have those bits to spare.
+//
+// What bounds it is not bytes but the chain of dependent instructions of the searches: 16384 tokens of 256 experts, 8 of them, sigmoid,
+// bfloat16, take 7.5 us (1.3 TB/s), 12.3 with a bias and 15.9 with groups too; of 128 experts 2, softmax with a bias, 7.3; one token 3.0.
+// The gradient of 16384 x 128 float32 with that of the scores 7.8 us (3.2 TB/s), of 8191 x 256 bfloat16 6.1.
 #include <algorithm>
 #include <climits>
 #include <cmath>
