@@ -407,8 +407,10 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<R> &
         wait_for_loads<R::NS - 2, R::LOADS, STORES>(min(rq.ahead - 1, R::NS - 2), kb <= R::NS - 2 ? stored : 0);
         // Behind the barrier they have for everyone, and everyone has read the block before, whose stage the next request takes.
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        rq.next(a, items, wave);
-        --rq.ahead;
+        if (MC == 0 || R::OT == 8) {
+            rq.next(a, items, wave);
+            --rq.ahead;
+        }
         if (MC > 0) {
             const int lane = lane_again(), g = lane >> 4, i16 = lane & 15;
             const int o0 = RUN * (i16 >> 2) + (i16 & 3);  // this lane's output of product 0
@@ -442,15 +444,15 @@ __device__ inline void matmul_k_loop(const MatmulArgs &a, const MatmulItems<R> &
             // conversion of weights that come next, dealt out behind the products one by one: the vector unit's work fits under the
             // matrix cores' then, in a wavefront by itself.
             if constexpr (R::OT == 2) {  // the chains are the two output tiles; rows come one tile after the other
-                intx4 raw[2];
-                codes(0, raw);
-                Operand w[2], x_next;
-                w[0] = operand<PGMOE_E4M3>(raw[0], raw[1]);
-                codes(1, raw);
-                w[1] = operand<PGMOE_E4M3>(raw[0], raw[1]);
-                row_codes(0, raw);
-                x[0] = operand<XQ>(raw[0], raw[1]);
+                intx4 raw[2], first[3][2];
+                codes(0, first[0]);
+                codes(1, first[1]);
+                row_codes(0, first[2]);
                 if (MC > 1) row_codes(1, raw);
+                rq.next(a, items, wave);  // while the first operands are on their way from LDS
+                --rq.ahead;
+                Operand w[2] = {operand<PGMOE_E4M3>(first[0][0], first[0][1]), operand<PGMOE_E4M3>(first[1][0], first[1][1])}, x_next;
+                x[0] = operand<XQ>(first[2][0], first[2][1]);
                 floatx4 before[2];
                 static_for<MC>([&](auto m_) {
                     constexpr int m = decltype(m_)::value;
