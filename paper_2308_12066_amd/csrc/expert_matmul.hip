@@ -214,8 +214,8 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 // to 256 rows: eight wavefronts as 2 x 4, wavefront (wn, wm) with 128 outputs (one scale) and the row tiles wm, wm + 4, ..; of up to 64 rows:
 // 8 x 1, 32 outputs and all row tiles each (4 + 4 of 16 conversions a block of inputs, where 2 x 4 would take 8 + 1).
 // What bounds it are the conversions and scales beside the matrix cores' products: 32768 rows over 128 experts of 1024 x 4096 with
-// quantised results 330 us (0.83 PFLOP/s), 8192 rows of one of 4096 x 4096 1.28 PFLOP/s, 4099 over eight of 2048 x 768 (1.3 us a block, one item for
-// 204 of 256 CUs) 26.1 us.
+// quantised results 330 us (0.83 PFLOP/s), 8192 rows of one of 4096 x 4096 1.28 PFLOP/s, 4099 over eight of 2048 x 768 (1.2 us a block, one item for
+// 204 of 256 CUs) 25 to 26 us.
 //
 // LDS, a stage: 16 weight tiles of 2 KiB, 64 bytes more behind each; rows of 128 bytes whose 16-byte pieces are
 // exchanged among themselves, piece c of row r at place c ^ (r / 2 % 8); 256 bytes of scales from each wavefront (rows: the
@@ -766,7 +766,9 @@ static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
     //  * tiles of 64 rows or of up to 256, by rounds of one item a workgroup, of which the larger take 4 / 3 as long (32 for each of 64 experts of
     //    1024 x 4096 55.9 / 63.6, 64 rows 79.7 / 75.8; 512 for each of 8 of 2048 x 768 26.5 / 31.0, 1024 46.3 / 39.4; 96 for each of 8 of
     //    1024 x 4096 17.0 / 20.4, 128 27.1 / 24.4).  An expert has half a chunk more than its rows fill, on the mean.
-    // The inputs of few rows are split so that a wavefront has three blocks at least, further while workgroups are no more than two a CU: KS = 1 / 2 / 4 / 8
+    // The inputs of few rows are split so that a wavefront has three blocks at least and there are 24 workgroups a CU at most (experts without rows
+    // leave empty ones: 128 rows over 46 of 128 experts of 4096 x 1024, room for 1024 items, KS = 1 / 2 / 4 / 8 39.4 / 40.3 / 36.8 / 38.4, of 1024 x 4096 36.9 / 38.6 /
+    // 45.2 / 64.2), further while workgroups are no more than two a CU: KS = 1 / 2 / 4 / 8
     // take 33.9 / 33.2 / 32.3 / 43.0 for one row for each of 64 experts of 1024 x 4096 (eight blocks), 6.8 / 5.0 / 5.1 / 5.0 for 64 rows of one, 6.6 / 4.8 / 3.8 / 3.0
     // for 16, 20.5 / 21.1 / 21.6 / 21.6 for 512 rows of one of 4096 x 1024, 38.2 / 31.5 / 25.5 / 23.7 for 64 for each of eight.
     const int64_t active = std::min(a.E, a.rows), mean = a.rows / active, cols = (a.NB + 1) / 2;
@@ -782,7 +784,7 @@ static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
         return PGMOE_OK;
     };
     if constexpr (!std::is_void<Y>::value) {
-        const auto split = [&](int ks) { return 3 * ks <= a.KB || (ks <= a.KB && ks * items16 <= 2 * TILE_GROUPS); };
+        const auto split = [&](int ks) { return ks * items16 <= (3 * ks <= a.KB ? 24 : ks <= a.KB ? 2 : 0) * TILE_GROUPS; };
         if (split(8)) return few(std::integral_constant<int, 8>());
         if (split(4)) return few(std::integral_constant<int, 4>());
         if (split(2)) return few(std::integral_constant<int, 2>());
