@@ -465,7 +465,7 @@ typedef struct {
 /* Quantise x dev [T, out->cols] (PGMOE_F32, BF16 or F16, rows x_stride elements apart).  row_of NULL: token t becomes
  * row t (copies = 1, T <= out->rows).  row_of dev [T * copies]: token t becomes the rows row_of[t*copies + j] (what
  * pgmoe_permute and pgmoe_group_rows give: the dispatch to experts, quantised once and written `copies` times); an
- * entry outside [0, out->rows) is skipped. */
+ * entry outside [0, out->rows) is skipped.  T / 16 * ceil(cols/128) is below 2^31. */
 int pgmoe_quantize_rows(const void *x, int64_t x_stride, int x_dtype, int T, const int32_t *row_of, int copies,
                         const pgmoe_fp8_rows *out, void *stream);
 /* Quantise w dev [E, n_in, n_out] (PGMOE_F32, BF16 or F16; contiguous) into `forward` (y = x . W) and, if given, into
