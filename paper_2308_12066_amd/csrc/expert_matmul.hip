@@ -29,6 +29,7 @@ struct MatmulArgs {
     const float *w_scale;
     const int32_t *offsets;
     int relu;
+    bool once;  // the weights are passed by the caches
     void *y;
     size_t y_stride;
     uint8_t *y_q;
@@ -125,11 +126,11 @@ __device__ inline void store_four(const MatmulArgs &a, int r, int o, floatx4 v) 
 // Few rows an expert: the stream of weights.  Operands straight from memory into registers, the next block of inputs requested before the one
 // at hand is multiplied.  A workgroup takes 16 rows and 8 / KS tiles of 16 outputs, a wavefront one of them and one KS-th of the inputs; the
 // parts are added up in LDS, in order.  One workgroup's stream is bound by its CU: 512 KB in 10.2 us (2 rows, 4096 x 1024, KS = 1), so few
-// tiles go to more CUs (KS = 8: 4.1), and long sums to more wavefronts (512 rows over 64 experts of 4096 x 1024 56.1 us with KS = 1, 51.0 with 8:
-// 5.3 TB/s of weights, a plain read on this chip 6.2).  Two and four blocks requested at once were no faster where KS suits the launch.
+// tiles go to more CUs (KS = 8: 4.1), and long sums to more wavefronts (512 rows over 64 experts of 4096 x 1024 56.1 us with KS = 1, 51.0 with 8;
+// with ONCE, weights past the caches, 48.7, of 1024 x 4096 44.7: 5.6 and 6.1 TB/s, a plain read on this chip 6.2).  Two and four blocks requested at once were no faster where KS suits the launch.
 // Y = void: quantised again, YQ, which takes a whole block of 128 outputs, KS = 1 (twice the wavefronts for half the inputs each: no faster).
 constexpr int FEW_THREADS = 512;
-template <int XQ, typename Y, int YQ, bool VEC, int KS>
+template <int XQ, typename Y, int YQ, bool VEC, int KS, bool ONCE>
 __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const MatmulArgs a) {
     constexpr int TILES = 8 / KS;  // of a workgroup
     __shared__ float amax_of[8][16];
@@ -149,8 +150,8 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
     auto load = [&](Block &b, int kb) {
         const int k = min(kb, a.KB - 1);  // past the end the last block again, which nobody uses: no conditions in front of loads
         const uint8_t *wk = w + (size_t)k * FP8_TILE, *xk = x + (size_t)k * FP8_BLOCK;
-        b.w[0] = *reinterpret_cast<const intx4 *>(wk);
-        b.w[1] = *reinterpret_cast<const intx4 *>(wk + 1024);
+        b.w[0] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const intx4 *>(wk)) : *reinterpret_cast<const intx4 *>(wk);
+        b.w[1] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const intx4 *>(wk + 1024)) : *reinterpret_cast<const intx4 *>(wk + 1024);
         b.x[0] = *reinterpret_cast<const intx4 *>(xk);
         b.x[1] = *reinterpret_cast<const intx4 *>(xk + 64);
         b.s = sx[(size_t)k * a.x_scale_stride];
@@ -330,6 +331,11 @@ struct MatmulItems {
     }
 };
 
+__device__ inline void load_two_tiles_once(const char *src, unsigned lane_off, unsigned lds_tile) {  // load_two_tiles_to_lds, past the caches
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt\n\tglobal_load_lds_dwordx4 %0, %1 offset:1024 nt" ::"v"(lane_off), "s"(src), "s"(lds_tile)
+                 : "memory", "m0");
+}
+
 // What a wavefront requests: the blocks of its workgroup's items one after the other.
 template <typename R>
 struct MatmulRequests {
@@ -366,8 +372,13 @@ struct MatmulRequests {
             s_last = wave < 4 ? it.nrows - 1 : (last == 15 ? 1 : 0);
         }
         const unsigned to = lds + stage;
-        load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * 2 * MATMUL_W_TILE);
-        load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
+        if (a.once) {  // uniform; as many loads either way
+            load_two_tiles_once((const char *)w_src, lane * 16, to + wave * 2 * MATMUL_W_TILE);
+            load_two_tiles_once((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
+        } else {
+            load_two_tiles_to_lds((const char *)w_src, lane * 16, to + wave * 2 * MATMUL_W_TILE);
+            load_two_tiles_to_lds((const char *)w_src + w_second, lane * 16, to + (wave * 2 + 1) * MATMUL_W_TILE);
+        }
         w_src += FP8_TILE;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -759,7 +770,8 @@ static int launch_tiles(const MatmulArgs &a, hipStream_t s) {
 }
 template <int XQ, typename Y, int YQ, bool VEC>
 static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
-    // Which kernel, by what there is to deal out; both sides in us a launch, bf16 results, rows dealt to the experts at random:
+    // Which kernel, by what there is to deal out; both sides in us a launch, bf16 results, rows dealt to the experts at random,
+    // weights through the caches:
     //  * few rows, to 8 an expert: the tiles would be empty mostly (64 experts of 1024 x 4096, 8 rows each 50.4, in tiles of 64 rows 52.1; 12 rows
     //    54.7 / 52.4); also launches of at most two items of 16 rows a CU (64 rows for each of 8 experts of 4096 x 1024 23.3 / 44.2, 128 41.0 / 43.8,
     //    256 for one of 1024 x 4096 11.8 / 15.0; not 512 21.3 / 15.1, 48 for each of 8 19.5 / 14.9), and rows too far apart for the tiles;
@@ -780,7 +792,9 @@ static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
     }
     auto few = [&](auto ks_) {
         constexpr int KS = decltype(ks_)::value;
-        hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS>), dim3((unsigned)(items16 * KS)), dim3(FEW_THREADS), 0, s, a);
+        const dim3 grid((unsigned)(items16 * KS));
+        if (a.once) hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, true>), grid, dim3(FEW_THREADS), 0, s, a);
+        else hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, false>), grid, dim3(FEW_THREADS), 0, s, a);
         return PGMOE_OK;
     };
     if constexpr (!std::is_void<Y>::value) {
@@ -850,6 +864,11 @@ extern "C" int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weig
     a.w_scale = w->scale;
     a.offsets = expert_offsets;
     a.relu = relu;
+    // Weights that the last-level cache (256 MB) does not hold until the next call, and that an expert's rows read once, pass by the caches: 16 rows for
+    // each of 64 experts of 1024 x 4096 52.4 -> 47.4 us, 128 rows over 46 of 128 37.3 -> 35.0, 128 for each of 64 96.6 -> 94.0; not 32 for each of 128 of 1024 x 1024 (134 MB)
+    // 27.6 / 30.4, nor 256 for each of 64 of 1024 x 4096, half of which have two chunks, 181 / 187.
+    const int64_t active = std::min(a.E, a.rows);
+    a.once = active * a.KB * a.NB * (8 * FP8_TILE) >= 256000000 && a.rows / active <= 128;
     a.y = y;
     a.y_stride = (size_t)y_stride;
     if (y_q) {

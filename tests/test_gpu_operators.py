@@ -518,6 +518,27 @@ def test_expert_matmul_of_weights_and_rows_that_pass_32_bits(B):
     assert np.all(np.abs(got[:, :4096] - one) <= p.err(m1) + 64 * H * m1 + H * np.abs(one)) and np.all(got[:, 4096:] == 0)
 
 
+@pytest.mark.parametrize("counts", [[1, 0, 6, 2], [20, 0, 37, 23], [100, 57, 128, 115]], ids=lambda c: "x".join(map(str, c)))
+def test_expert_matmul_of_more_weights_than_the_cache_holds(B, counts):
+    """64 experts of 2048 x 2048, 268 MB: copies of two, so that the plain form is two matrices."""
+    say("matmul large", counts)
+    p = Product(B, [4, 4], 2048, 2048)
+    n = 64
+    counts = counts * (n // 4)
+    offs = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    R = int(offs[-1])
+    x_val, x_s = O.quantize_rows(np.random.default_rng(7).standard_normal((R, 2048)).astype(np.float32), "e4m3")
+    w_q, w_scale = p.w_q.view(torch.uint8).repeat(n // 2, *[1] * (p.w_q.dim() - 1)).view(torch.float8_e4m3fn), p.w_scale.repeat(n // 2, *[1] * (p.w_scale.dim() - 1))
+    y = torch.full((R, 2048), 7.0, device="cuda")
+    B.expert_matmul(dev(x_val).to(torch.float8_e4m3fn), dev(x_s), w_q, w_scale, torch.from_numpy(offs).cuda(), 2048, 2048, y)
+    torch.cuda.synchronize()
+    got = f64(y)
+    for base in (0, 1):
+        rows = np.concatenate([np.arange(offs[e], offs[e + 1]) for e in range(base, n, 2)]).astype(int)
+        want, mag = O.expert_matmul(x_val[rows], x_s[:, rows], p.w_val[base:base + 1], p.w_s[base:base + 1], [0, len(rows)])
+        assert np.all(np.abs(got[rows] - want) <= (128 + 4 * 16) * H * mag + H * np.abs(want))
+
+
 def test_expert_matmul_passes_on_what_is_not_finite(B):
     """A NaN code or scale reaches exactly the results that use it, also through ReLU and back into 8 bits."""
     say("matmul not finite")
