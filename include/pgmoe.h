@@ -395,7 +395,8 @@ int pgmoe_stack_step(pgmoe_ctx *ctx, const pgmoe_step_buffers *io, int T, void *
  * passed), allocate nothing and may be captured into a HIP graph.
  *
  * For every token: an expert whose logit z is NaN or -infinity is unavailable.
- *   scores     s = softmax(z) over the available experts, or 1 / (1 + exp(-z)); 0 for the others.
+ *   scores     s = softmax(z) over the available experts, or 1 / (1 + exp(-z)); 0 for the others. (Written or as a
+ *              weight, a score below 2^-126 may be 0.)
  *   selection  by v = s + bias (a balancing bias moves the selection, never a weight; a NaN bias counts
  *              as -infinity); without a bias by z itself.  With n_groups > 1 the experts are n_groups runs
  *              of n_experts / n_groups; a group is worth the sum of the two largest s + bias above

@@ -116,12 +116,12 @@ __device__ inline void wave_sync() {
 
 __device__ inline bool available(float z) { return z > -INFINITY; }  // false for NaN too
 
-// exp(x), x <= 0 or any finite: 2^t with the rest of the product by log2 e put back, three half-steps of 2^-24 from exact.
-// Results below 2^-126 may be 0.
+// exp(x): 2^t with the rest of the product by log2 e put back, three half-steps of 2^-24 from exact. Results below 2^-126 may be 0.
+// Nothing is put back where 2^t is infinite (from t = 128 on: infinity less a rest of it is NaN) or below 2^-128.
 __device__ inline float exp_of(float x) {
     const float t = x * 1.44269502f, rest = fmaf(x, 1.92596303e-8f, fmaf(x, 1.44269502f, -t));
     const float e = __builtin_amdgcn_exp2f(t);
-    return fabsf(t) < 200.f ? fmaf(e, rest * 0.693147182f, e) : e;  // beyond, 0 or infinity (and no infinity less infinity)
+    return fabsf(t) < 128.f ? fmaf(e, rest * 0.693147182f, e) : e;
 }
 __device__ inline float inverse_of(float x) { return __builtin_amdgcn_rcpf(x); }  // one step of 2^-24
 __device__ inline double exp_of(double x) { return exp(x); }

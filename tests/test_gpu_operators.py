@@ -144,6 +144,51 @@ def test_route_tells_apart_what_32_bits_do_not(B, kind):
     check_route(B, z, kind, 4, n_groups=16, topk_groups=3)
 
 
+# sigmoid(z) = 1 / (1 + exp(-z)) where exp passes what float32 holds, or 2^-126, but not yet in any way one would take: between about 88 and 139.
+FAR = (-138.5, -130.0, -120.0, -112.0, -110.0, -99.0, -95.0, -92.5, -90.25, -89.0, 89.0, 90.25, 92.5, 95.0, 99.0, 110.0, 112.0, 120.0, 130.0, 138.5)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("groups,keep", [(1, 1), (4, 2)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_route_with_logits_far_from_zero(B, kind, renormalize, groups, keep, dtype):
+    say("route far", kind, renormalize, groups, keep, dtype)
+    g = np.random.default_rng(12)
+    T, E, k = 60, 24, 6
+    z = np.where(g.random((T, E)) < 0.6, g.choice(FAR, (T, E)), 1.5 * g.standard_normal((T, E)))
+    z[:len(FAR)] = np.array(FAR)[:, None]                    # tokens of nothing else
+    z = f64(dev(z, dtype))
+    for bias in (None, (0.1 * g.standard_normal(E)).astype(np.float32)):
+        got = run_route(B, z, kind, k, dtype, bias, True, n_groups=groups, topk_groups=keep, renormalize=renormalize)
+        want = O.route(z, kind, k, None if bias is None else bias.astype(np.float64), groups, keep, renormalize)
+        assert np.array_equal(got[0], want[0]), np.argwhere(got[0] != want[0])[:5]
+        tol = (spread(z) + 64) * H                           # as in check_route; scores below the least normal number may be 0
+        assert np.all(np.abs(got[1] - want[1]) <= tol * np.abs(want[1]) + 2.0 ** -126)
+        assert np.all(np.abs(got[2] - want[2]) <= tol * want[2] + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("every", [False, True])
+@pytest.mark.parametrize("renormalize", [False, True])
+def test_route_backward_with_logits_far_from_zero(B, kind, every, renormalize):
+    say("route backward far", kind, every, renormalize)
+    g = np.random.default_rng(13)
+    T, E, k = 60, 24, 6
+    z = np.where(g.random((T, E)) < 0.6, g.choice(FAR, (T, E)), 1.5 * g.standard_normal((T, E)))
+    z[:len(FAR)] = np.array(FAR)[:, None]
+    z = f64(dev(z))
+    idx = np.stack([g.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
+    dw, ds = g.standard_normal((T, k)).astype(np.float32), g.standard_normal((T, E)).astype(np.float32) if every else None
+    r = B.Router(E, k, score=B.SCORE_SIGMOID if kind == "sigmoid" else B.SCORE_SOFTMAX, renormalize=renormalize)
+    d = torch.full((T, E), 7.0, device="cuda")
+    r.route_backward(dev(z), torch.from_numpy(idx).cuda(), dev(dw), None if ds is None else dev(ds), d)
+    torch.cuda.synchronize()
+    want, mag = O.route_loss_gradient(z, idx, kind, dw.astype(np.float64), ds, renormalize, 1.0)
+    # as in check_backward; of a score or of 1 - score below 2^-126, times gradients below 2^4, all may be missing
+    assert np.all(np.abs(f64(d) - want) <= 2 * (spread(z) + 64) * H * mag + H * np.abs(want) * (1 + 1e-3) + 2.0 ** -122)
+
+
 def test_route_reads_strided_logits_on_another_stream(B):
     say("route strided")
     g = np.random.default_rng(7)
