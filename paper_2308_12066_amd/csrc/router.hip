@@ -410,6 +410,8 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
         if (lane == 0) at.chosen[n] = won;
         ++n;
     }
+    // The first that lies apart is none of them.  (It may be of a group that is not kept, whatever its value.)
+    if (n > a.k && !near(before, last)) --n;
     wave_sync();
     if (a.bias) exact_sum();
     auto rank_value = [&](int e) { return a.bias ? exact_value(e) : (double)logit(e); };

@@ -144,6 +144,21 @@ def test_route_tells_apart_what_32_bits_do_not(B, kind):
     check_route(B, z, kind, 4, n_groups=16, topk_groups=3)
 
 
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("biased", [False, True])
+def test_route_takes_all_of_the_kept_groups_and_no_other(B, kind, biased):
+    """All experts of the kept groups are asked for, two of them as good as equal, and the best expert of all is of another group."""
+    say("route kept groups", kind, biased)
+    z = np.full((8, 16), -4.0, np.float32)
+    z[:, 0] = 3.0
+    for t in range(8):
+        z[t, 4 + t // 4 * 8:8 + t // 4 * 8] = 2.0, -1.0, -1.5, 2.0
+        z[t, 4 + t // 4 * 8 + t % 4] += np.float32(2.0 ** -21)       # close to another one, or to nothing
+    bias = np.full(16, 0.25, np.float32) if biased else None
+    check_route(B, z, kind, 4, bias=bias, n_groups=4, topk_groups=1)
+    check_route(B, z, kind, 3, bias=bias, n_groups=4, topk_groups=1)
+
+
 # sigmoid(z) = 1 / (1 + exp(-z)) where exp passes what float32 holds, or 2^-126, but not yet in any way one would take: between about 88 and 139.
 FAR = (-138.5, -130.0, -120.0, -112.0, -110.0, -99.0, -95.0, -92.5, -90.25, -89.0, 89.0, 90.25, 92.5, 95.0, 99.0, 110.0, 112.0, 120.0, 130.0, 138.5)
 
