@@ -39,9 +39,13 @@ struct RouteArgs {
 
 constexpr int ROUTE_LANES = 16;                                // of one token
 constexpr int ROUTE_THREADS = 256, ROUTE_TOKENS = ROUTE_THREADS / ROUTE_LANES;
-// Two selection values closer than this, relative to the larger of them and 2^-24, are compared in 64 bits: the scores carry
-// a few units of 2^-24 (exp, a sum of up to 256 terms in pairs, a division), the bias and the sum of a group's two one each, 4e-6 in all;
-// a key leaves out 2^-19.
+// Selection values closer than this, relative to what they are made of, are compared in 64 bits.  A score is off by some thirty half-steps of
+// 2^-24 (exp, a sum of 16 + 4 terms and their exp, an inverse), 1.8e-6 of itself, and by a third of a half-step of the largest score for exp's
+// argument: the two that are compared by 3.7e-6.  A key leaves out 2^-19 of the value, 1.9e-6, and the sum with the bias a half-step.
+// With a bias the value may be far smaller than the score in it, so the measure is the larger of the value and the token's largest score,
+// the same for all its experts: one further down with a larger score cannot pass by.  Two groups are compared by four scores, 8e-6 of the
+// largest, and four values and two sums of half a step each, 2.4e-7 of the largest sum of magnitudes.  Without a bias nothing
+// cancels, and a group's measure is its value.  No measure is below 2^-24.
 constexpr float CLOSE = 6e-6f;
 
 // Keys of values, which are not NaN: integers in the order of the values, -0 as 0.
@@ -202,12 +206,13 @@ __device__ inline void store_row(L *row, int E, int first, const float (&v)[PER]
     }
 }
 
-// Scores of this lane's experts from its logits; m: the token's largest logit.
+// Scores of this lane's experts from its logits; m: the token's largest logit.  Returns the token's largest score.
 template <bool SIGMOID, int PER>
-__device__ inline void scores_of(const float (&z)[PER], float m, float (&s)[PER]) {
+__device__ inline float scores_of(const float (&z)[PER], float m, float (&s)[PER]) {
     if (SIGMOID) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) s[i] = sigmoid<float>(z[i]);
+        return sigmoid<float>(m);
     } else {
         float sum = 0;
 #pragma unroll
@@ -219,6 +224,7 @@ __device__ inline void scores_of(const float (&z)[PER], float m, float (&s)[PER]
         const float inv = sum > 0.f ? inverse_of(sum) : 0.f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) s[i] *= inv;
+        return inv;  // the largest term is 1
     }
 }
 
@@ -250,9 +256,9 @@ struct TwoLargest {
 };
 
 // Which groups are kept, as a bit for each in the first of its `part` lanes, from what each of these has seen of the group.  part = 2^shift.  Returns
-// whether 32 bits may have decided it (V = float only).
+// whether 32 bits may not have decided it (V = float only; most: the token's largest score).
 template <typename V>
-__device__ bool keep_groups(const RouteArgs &a, TwoLargest<V> best, int lane, int shift, unsigned *mask) {
+__device__ bool keep_groups(const RouteArgs &a, TwoLargest<V> best, int lane, int shift, float most, unsigned *mask) {
     typedef typename Keys<V>::T Key;
     constexpr Key low = Keys<V>::lowest;
     const int mine = lane >> shift;
@@ -280,7 +286,12 @@ __device__ bool keep_groups(const RouteArgs &a, TwoLargest<V> best, int lane, in
     // the worst kept against the best other
     const float inside = -lanes_max(kept ? -(float)value : -INFINITY);
     const float outside = lanes_max(mine < a.n_groups && !kept && worth > low ? (float)value : -INFINITY);
-    return outside > -INFINITY && !(inside - outside > CLOSE * fmaxf(fabsf(inside), 6e-8f));
+    float terms = fabsf(inside);
+    if (a.bias) {
+        const float one = fabsf((float)best.one), two = fabsf((float)best.two);
+        terms = 4.f / 3 * most + 0.04f * lanes_max(worth > low ? (best.two > -(V)INFINITY ? one + two : one) : 0.f);
+    }
+    return outside > -INFINITY && !(inside - outside > CLOSE * fmaxf(terms, 6e-8f));
 }
 
 // Takes the expert of the largest key: the lowest of those that have it.
@@ -315,10 +326,11 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
         const double v = (SIGMOID ? sigmoid<double>(ze) : exp_below<double>(ze, m) / sum) + (double)be;
         return available(ze) && be > -INFINITY ? v : -(double)INFINITY;
     };
+    float most = 0.f;  // the largest score and at least 2^-24, where scores are compared
     {
         float v[PER];
         if (a.bias || a.n_groups > 1) {
-            scores_of<SIGMOID, PER>(z, m, v);
+            most = fmaxf(scores_of<SIGMOID, PER>(z, m, v), 6e-8f);
 #pragma unroll
             for (int i = 0; i < PER; ++i) v[i] += b[i];
         }
@@ -344,12 +356,12 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
                 for (int j = from; j < to; ++j) best.take(at.values[mine * size + j]);
             }
             unsigned mask;
-            if (keep_groups(a, best, lane, shift, &mask)) {
+            if (keep_groups(a, best, lane, shift, most, &mask)) {
                 exact_sum();
                 TwoLargest<double> exact;
 #pragma unroll 1
                 for (int j = from; j < to; ++j) exact.take(exact_value(mine * size + j));
-                keep_groups(a, exact, lane, shift, &mask);
+                keep_groups(a, exact, lane, shift, most, &mask);
             }
             if (!a.straddle) {
                 const bool out = !((mask >> (mine << shift)) & 1) && mine < a.n_groups;
@@ -385,7 +397,7 @@ __device__ const int32_t *select_experts(const RouteArgs &a, const float (&z)[PE
     wave_sync();
     auto near = [&](int32_t upper, int32_t lower) {  // might the order be another in 64 bits?
         const float hi = Keys<float>::value(upper), lo = Keys<float>::value(lower);
-        const bool unsure = a.bias ? lo > -INFINITY && !(hi - lo > CLOSE * fmaxf(fabsf(hi), 6e-8f)) : upper == lower;
+        const bool unsure = a.bias ? lo > -INFINITY && !(hi - lo > CLOSE * fmaxf(fabsf(hi), most)) : upper == lower;
         return lower >= KEY_VALUES && unsure;
     };
     bool close = false;

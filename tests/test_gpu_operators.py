@@ -145,6 +145,30 @@ def test_route_tells_apart_what_32_bits_do_not(B, kind):
 
 
 @pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_route_where_bias_and_score_cancel(B, kind):
+    """Selection values near 0 that are sums of a score and a bias which are not: the rounding of the score decides in 32 bits."""
+    say("route cancelling", kind)
+    z, bias = np.array([[0.44873318, -0.00598402]], np.float32), np.array([-0.6103381, -0.4985041], np.float32)
+    check_route(B, z, "sigmoid", 1, bias=bias)
+    g = np.random.default_rng(11)
+    T, E = 400, 64
+    z = (0.7 * g.standard_normal(E) + g.standard_normal((T, E)) * 10.0 ** g.uniform(-7.5, -3, (T, 1))).astype(np.float32)
+    bias = (-O.scores(z, kind).mean(0)).astype(np.float32)
+    check_route(B, z, kind, 1, bias=bias)
+    check_route(B, z, kind, 9, bias=bias)
+    check_route(B, z, kind, 4, bias=bias, n_groups=16, topk_groups=3)
+    # one candidate's value is exact, the other's carries the error of a large score
+    z = np.stack([np.full(T, -40.0), 0.4 + g.standard_normal(T) * 10.0 ** g.uniform(-7.5, -5, T)], 1).astype(np.float32)
+    bias = np.array([0.0, -O.scores(z, kind)[:, 1].mean()], np.float32)
+    check_route(B, z, kind, 1, bias=bias)
+    # groups of two whose values are a third and minus a third: their sums are near 0, they are not
+    z = (0.7 * g.standard_normal(32) + g.standard_normal((T, 32)) * 10.0 ** g.uniform(-7.5, -3, (T, 1))).astype(np.float32)
+    bias = (np.tile([0.34, -0.34], 16) - O.scores(z, kind).mean(0)).astype(np.float32)
+    for keep in (1, 7):
+        check_route(B, z, kind, 2, bias=bias, n_groups=16, topk_groups=keep)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("biased", [False, True])
 def test_route_takes_all_of_the_kept_groups_and_no_other(B, kind, biased):
     """All experts of the kept groups are asked for, two of them as good as equal, and the best expert of all is of another group."""
