@@ -420,7 +420,9 @@ typedef struct {
     int32_t logits_dtype; /* PGMOE_F32, PGMOE_BF16 or PGMOE_F16: logits and d_logits */
 } pgmoe_router;
 /*   logits dev [T, E], rows logits_stride >= E elements apart    bias dev [E] f32 | NULL
- *   topk_idx dev [T,k] int32 out    topk_weight dev [T,k] f32 out    scores_out dev [T,E] f32 out | NULL */
+ *   topk_idx dev [T,k] int32 out    topk_weight dev [T,k] f32 out    scores_out dev [T,E] f32 out | NULL
+ * scores_out may be the logits themselves (f32, rows n_experts apart).  Otherwise here and in the calls below no output
+ * may overlap an input. */
 int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_stride, const float *bias, int T,
                 int32_t *topk_idx, float *topk_weight, float *scores_out, void *stream);
 /* Gradient of the logits: d_weight dev [T,k] f32 is that of topk_weight, d_scores dev [T,E] f32 | NULL that of

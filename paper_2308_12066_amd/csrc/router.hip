@@ -491,9 +491,8 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
     const int32_t *chosen = select_experts<SIGMOID, sizeof(L) == 4>(a, z, b, first, lane, m, at, [&](int e) { return logit_at<L>(a, t, e); });
     wave_sync();
 
-    float sum = 0.f;  // of exp(z - m) over all experts
+    float s[PER], sum = 0.f;  // scores, softmax before the division; of exp(z - m) over all experts
     if (a.scores || (!SIGMOID && !a.renorm)) {
-        float s[PER];
         if (!SIGMOID) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
@@ -504,14 +503,6 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
         } else {
 #pragma unroll
             for (int i = 0; i < PER; ++i) s[i] = sigmoid<float>(z[i]);
-        }
-        if (a.scores) {
-            if (!SIGMOID) {
-                const float inv = sum > 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) s[i] *= inv;
-            }
-            store_row<VEC>(a.scores + t * a.E, a.E, first, s);
         }
     }
     // Weights, lane j the j-th (and 16 + j-th ..).  Renormalised ones are taken relative to the largest selected logit, so that neither
@@ -535,6 +526,14 @@ __global__ __launch_bounds__(ROUTE_THREADS) void route_logits_kernel(const Route
         const float w = a.renorm ? part(zj) / total : SIGMOID ? sigmoid<float>(zj) : exp_below<float>(zj, m) / sum;
         a.idx[t * a.k + j] = chosen[j];
         a.weight[t * a.k + j] = available(zj) ? a.scale * w : 0.f;
+    }
+    if (a.scores) {  // last: they may take the logits' place
+        if (!SIGMOID) {
+            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) s[i] *= inv;
+        }
+        store_row<VEC>(a.scores + t * a.E, a.E, first, s);
     }
 }
 

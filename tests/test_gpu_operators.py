@@ -228,6 +228,22 @@ def test_route_backward_with_logits_far_from_zero(B, kind, every, renormalize):
     assert np.all(np.abs(f64(d) - want) <= 2 * (spread(z) + 64) * H * mag + H * np.abs(want) * (1 + 1e-3) + 2.0 ** -122)
 
 
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("T,E,k", [(1, 8, 2), (50, 60, 6), (70, 129, 20), (100, 256, 8), (9, 256, 256)])
+def test_route_writes_scores_in_place_of_the_logits(B, kind, renormalize, T, E, k):
+    say("route in place", kind, renormalize, T, E, k)
+    g = np.random.default_rng(T + E)
+    z = 1.5 * g.standard_normal((T, E))
+    for bias in (None, g.standard_normal(E) * 0.05):
+        want = run_route(B, z, kind, k, bias=bias, renormalize=renormalize)
+        r = B.Router(E, k, score=B.SCORE_SIGMOID if kind == "sigmoid" else B.SCORE_SOFTMAX, renormalize=renormalize)
+        zt, idx, w = dev(z), torch.full((T, k), -7, dtype=torch.int32, device="cuda"), torch.full((T, k), 7.0, device="cuda")
+        r.route(zt, None if bias is None else dev(bias), idx, w, zt)
+        torch.cuda.synchronize()
+        assert np.array_equal(idx.cpu().numpy(), want[0]) and np.array_equal(f64(w), want[1]) and np.array_equal(f64(zt), want[2])
+
+
 def test_route_reads_strided_logits_on_another_stream(B):
     say("route strided")
     g = np.random.default_rng(7)
