@@ -431,7 +431,8 @@ int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_s
  *   d_s[e] = d_scores[e] + (e selected: c * d_weight, renormalised c * (d_weight - sum d_weight s / total) / total)
  *   softmax: d_z = s * (d_s - sum d_s s)      sigmoid: d_z = s * (1 - s) * d_s       unavailable experts: 0.
  * An index outside [0, E) contributes nothing.
- *   d_logits dev [T, E] in logits_dtype, rows d_logits_stride apart, out; d_logits may not overlap logits. */
+ *   d_logits dev [T, E] in logits_dtype, rows d_logits_stride apart, out; d_logits may not overlap logits (rows of both
+ * between each other, in one buffer, do not: strides are the same then). */
 int pgmoe_route_backward(const pgmoe_router *router, const void *logits, int64_t logits_stride, const int32_t *topk_idx,
                          const float *d_weight, const float *d_scores, int T, void *d_logits, int64_t d_logits_stride,
                          void *stream);

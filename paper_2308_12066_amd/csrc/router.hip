@@ -677,6 +677,15 @@ static bool route_vec(const pgmoe_router *r, const void *rows, int64_t stride) {
     return r->n_experts % per == 0 && aligned(rows, bytes) && stride * dtype_bytes(r->logits_dtype) % bytes == 0;
 }
 
+// Do two matrices of n rows of `bytes` bytes, at rows so many bytes apart, share any?  Rows as far apart as the others' may lie between them.
+static bool rows_overlap(const void *a, int64_t a_apart, const void *b, int64_t b_apart, int64_t bytes, int64_t n) {
+    const int64_t d = (const char *)b - (const char *)a;
+    if (d >= (n - 1) * a_apart + bytes || -d >= (n - 1) * b_apart + bytes) return false;
+    if (a_apart != b_apart) return true;
+    const int64_t phase = (d % a_apart + a_apart) % a_apart;
+    return phase < bytes || a_apart - phase < bytes;
+}
+
 // The instantiation for a type of logits, a score, a number of experts and the form of the loads: KERNEL<L, SIGMOID, PER, VEC>.
 #define ROUTE_LAUNCH_PER(KERNEL, L, SIG, PER, vec, ...)                                      \
     do {                                                                                     \
@@ -759,9 +768,7 @@ int pgmoe_route_backward(const pgmoe_router *router, const void *logits, int64_t
     NEED_PTR(nullptr, fn, d_weight, 4);
     OPT_PTR(nullptr, fn, d_scores, 4);
     NEED_PTR(nullptr, fn, d_logits, elem);
-    const char *a0 = (const char *)logits, *b0 = (const char *)d_logits;
-    const char *a1 = a0 + ((T - 1) * logits_stride + router->n_experts) * elem, *b1 = b0 + ((T - 1) * d_logits_stride + router->n_experts) * elem;
-    if (a0 < b1 && b0 < a1) return fail(nullptr, PGMOE_EINVAL, "%s: d_logits overlaps logits", fn);
+    if (rows_overlap(logits, logits_stride * elem, d_logits, d_logits_stride * elem, router->n_experts * elem, T)) return fail(nullptr, PGMOE_EINVAL, "%s: d_logits overlaps logits", fn);
     const RouteBackwardArgs a = {logits, (size_t)logits_stride, topk_idx, d_weight, d_scores, d_logits, (size_t)d_logits_stride,
                                  T, router->n_experts, router->top_k, router->renormalize, router->scale};
     const size_t lds = (size_t)ROUTE_THREADS * route_per(a.E) * 4;  // at most 16 KiB

@@ -69,6 +69,18 @@ def test_bad_arguments_of_routing_are_refused():
     refused(B.lib.pgmoe_route_backward(r, P, 64, P, P, None, 4, P + 128, 64, None), "overlaps")
 
 
+@needs_no_gpu
+def test_gradient_of_routing_beside_the_logits_in_one_buffer():
+    """Rows of logits and of their gradient that lie between each other share nothing; with one byte of a row in common they do."""
+    r = byref(router())                                                                  # rows of 64 bf16, 128 bytes
+    for stride, at in ((128, 64), (128, -64), (200, 64), (200, 136), (200, -64), (128, 64 + 128), (64, 256), (64, -256)):
+        a, b = P + 16384, P + 16384 + 2 * at
+        assert B.lib.pgmoe_route_backward(r, a, stride, P, P, None, 4, b, stride, None) == B.ENODEVICE, (stride, at)
+    for stride, d_stride, at in ((128, 128, 63), (128, 128, 65), (200, 200, 63), (200, 200, 137), (200, 200, -63), (64, 64, 255), (128, 136, 64), (128, 128, 0)):
+        a, b = P + 16384, P + 16384 + 2 * at
+        refused(B.lib.pgmoe_route_backward(r, a, stride, P, P, None, 4, b, d_stride, None), "overlaps")
+
+
 @pytest.mark.parametrize("bad,word", [
     (dict(dtype=B.F32), "dtype"), (dict(rows=-1), "rows"), (dict(cols=0), "columns"), (dict(cols=(1 << 22) + 1), "columns"),
     (dict(q_stride=240), "q_stride"), (dict(q_stride=264), "q_stride"), (dict(scale_stride=7), "scale_stride"), (dict(q=None), "NULL"),
