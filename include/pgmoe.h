@@ -421,7 +421,7 @@ typedef struct {
 } pgmoe_router;
 /*   logits dev [T, E], rows logits_stride >= E elements apart    bias dev [E] f32 | NULL
  *   topk_idx dev [T,k] int32 out    topk_weight dev [T,k] f32 out    scores_out dev [T,E] f32 out | NULL
- * scores_out may be the logits themselves (f32, rows n_experts apart).  Otherwise here and in the calls below no output
+ * T is at most 2^28 - 16.  scores_out may be the logits themselves (f32, rows n_experts apart).  Otherwise here and in the calls below no output
  * may overlap an input. */
 int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_stride, const float *bias, int T,
                 int32_t *topk_idx, float *topk_weight, float *scores_out, void *stream);
@@ -469,7 +469,7 @@ typedef struct {
 /* Quantise x dev [T, out->cols] (PGMOE_F32, BF16 or F16, rows x_stride elements apart).  row_of NULL: token t becomes
  * row t (copies = 1, T <= out->rows).  row_of dev [T * copies]: token t becomes the rows row_of[t*copies + j] (what
  * pgmoe_permute and pgmoe_group_rows give: the dispatch to experts, quantised once and written `copies` times); an
- * entry outside [0, out->rows) is skipped.  T / 16 * ceil(cols/128) is below 2^31. */
+ * entry outside [0, out->rows) is skipped.  One launch: ceil(T/128) * ceil(cols/128) is below 2^21. */
 int pgmoe_quantize_rows(const void *x, int64_t x_stride, int x_dtype, int T, const int32_t *row_of, int copies,
                         const pgmoe_fp8_rows *out, void *stream);
 /* Quantise w dev [E, n_in, n_out] (PGMOE_F32, BF16 or F16; contiguous) into `forward` (y = x . W) and, if given, into
@@ -482,7 +482,9 @@ int pgmoe_quantize_weights(const void *w, int w_dtype, const pgmoe_fp8_weights *
  *   x->cols == w->n_in; expert_offsets dev [E+1], rows past x->rows are not touched; relu 0 or 1.
  * Exactly one output: y dev [x->rows, n_out] (PGMOE_F32, BF16 or F16, rows y_stride >= n_out elements apart), or y_q
  * (rows = x->rows, cols = n_out): the float32 results quantised as by pgmoe_quantize_rows, the next product's operand.
- * Backward: the gradient of x is this call on d_y's codes with the `backward` weights. */
+ * Backward: the gradient of x is this call on d_y's codes with the `backward` weights.
+ * x->rows is at most 2^24.  Of up to 8 rows an expert on the mean, and of rows 2^23 bytes or more apart, one launch holds
+ * below 2^23 pieces of 16 rows and 128 outputs (at most rows / 16 + experts with rows, times ceil(n_out/128)). */
 int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, const int32_t *expert_offsets, int relu, void *y,
                         int64_t y_stride, int y_dtype, const pgmoe_fp8_rows *y_q, void *stream);
 

@@ -790,8 +790,11 @@ static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
         if (3 * rounds(64) <= 4 * rounds(256)) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<1, 2>>(a, s);
         return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<4, 8>>(a, s);
     }
-    auto few = [&](auto ks_) {
+    auto few = [&](auto ks_) -> int {
         constexpr int KS = decltype(ks_)::value;
+        if (items16 * KS * FEW_THREADS > GRID_THREADS_MAX)
+            return fail(nullptr, PGMOE_EINVAL, "pgmoe_expert_matmul: %d rows by n_out=%d are more than one launch holds (%lld items of 16 rows and 128 outputs)", a.rows, a.n_out,
+                        (long long)items16);
         const dim3 grid((unsigned)(items16 * KS));
         if (a.once) hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, true>), grid, dim3(FEW_THREADS), 0, s, a);
         else hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, false>), grid, dim3(FEW_THREADS), 0, s, a);

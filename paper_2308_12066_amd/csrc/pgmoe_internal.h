@@ -143,7 +143,8 @@ inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_
         if ((p) && !aligned(p, a)) return fail(ctx, PGMOE_EINVAL, "%s: %s is not %d-byte aligned", fn, #p, (int)(a)); \
     } while (0)
 
-// The context-free operators: bytes of an element, and the status of a launch.
+// The context-free operators: the most threads a grid has in a direction, bytes of an element, and the status of a launch.
+constexpr int64_t GRID_THREADS_MAX = ((int64_t)1 << 32) - 1;
 inline size_t dtype_bytes(int dtype) { return dtype == PGMOE_F32 ? 4 : (dtype == PGMOE_BF16 || dtype == PGMOE_F16 ? 2 : 1); }
 inline int launched(const char *fn) {
     const hipError_t e = hipGetLastError();

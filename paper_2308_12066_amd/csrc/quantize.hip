@@ -193,7 +193,7 @@ int pgmoe_quantize_rows(const void *x, int64_t x_stride, int x_dtype, int T, con
         return fail(nullptr, PGMOE_EINVAL, "%s: without row_of copies is 1 (got %d) and T at most out->rows (got %d of %d)", fn, copies, T, out->rows);
     if (x_stride < out->cols) return fail(nullptr, PGMOE_EINVAL, "%s: x_stride=%lld is less than out->cols=%d", fn, (long long)x_stride, out->cols);
     if (T == 0 || out->rows == 0) return PGMOE_OK;
-    if (quantize_rows_grid(T, out->cols) > 0x7fffffff)
+    if (quantize_rows_grid(T, out->cols) * QR_THREADS > GRID_THREADS_MAX)
         return fail(nullptr, PGMOE_EINVAL, "%s: T=%d rows of %d columns are more than one launch holds", fn, T, out->cols);
     NEED_PTR(nullptr, fn, x, dtype_bytes(x_dtype));
     OPT_PTR(nullptr, fn, row_of, 4);

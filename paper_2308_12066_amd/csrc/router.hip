@@ -664,6 +664,14 @@ static int check_router(const pgmoe_router *r, const char *fn) {
     return PGMOE_OK;
 }
 
+constexpr int ROUTE_TOKENS_MAX = (1 << 28) - ROUTE_TOKENS;  // whole workgroups of 16 lanes a token
+static_assert((int64_t)ROUTE_TOKENS_MAX * ROUTE_LANES <= GRID_THREADS_MAX && ROUTE_TOKENS_MAX % ROUTE_TOKENS == 0, "one launch");
+static int check_tokens(int T, const char *fn) {
+    if (T < 0) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d is negative", fn, T);
+    if (T > ROUTE_TOKENS_MAX) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d tokens are more than one launch holds, %d", fn, T, ROUTE_TOKENS_MAX);
+    return PGMOE_OK;
+}
+
 // Experts a lane holds.
 static int route_per(int E) {
     int per = 1;
@@ -728,7 +736,7 @@ int pgmoe_route(const pgmoe_router *router, const void *logits, int64_t logits_s
     const char *fn = "pgmoe_route";
     const int rc = check_router(router, fn);
     if (rc) return rc;
-    if (T < 0) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d is negative", fn, T);
+    if (const int bad = check_tokens(T, fn)) return bad;
     if (logits_stride < router->n_experts) return fail(nullptr, PGMOE_EINVAL, "%s: logits_stride=%lld is less than n_experts=%d", fn, (long long)logits_stride, router->n_experts);
     if (T == 0) return PGMOE_OK;
     const size_t elem = dtype_bytes(router->logits_dtype);
@@ -758,7 +766,7 @@ int pgmoe_route_backward(const pgmoe_router *router, const void *logits, int64_t
     const char *fn = "pgmoe_route_backward";
     const int rc = check_router(router, fn);
     if (rc) return rc;
-    if (T < 0) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d is negative", fn, T);
+    if (const int bad = check_tokens(T, fn)) return bad;
     if (logits_stride < router->n_experts || d_logits_stride < router->n_experts)
         return fail(nullptr, PGMOE_EINVAL, "%s: a stride (%lld, %lld) is less than n_experts=%d", fn, (long long)logits_stride, (long long)d_logits_stride, router->n_experts);
     if (T == 0) return PGMOE_OK;

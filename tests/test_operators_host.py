@@ -136,6 +136,28 @@ def test_bad_arguments_of_quantising_and_of_products_are_refused():
     refused(L.pgmoe_expert_matmul(big, byref(weights(n_out=1 << 22)), P, 0, P, 1 << 22, B.BF16, None, None), "launch")
 
 
+@needs_no_gpu
+def test_a_grid_has_less_than_2_to_the_32_threads():
+    """The largest sizes one launch holds get as far as the missing device, the next are refused."""
+    L, r = B.lib, byref(router())
+    for T, rc in (((1 << 28) - 16, B.ENODEVICE), ((1 << 28) - 15, B.EINVAL), ((1 << 31) - 1, B.EINVAL)):
+        for got in (L.pgmoe_route(r, P, 64, None, T, P, P, None, None), L.pgmoe_route_backward(r, P, 64, P, P, None, T, P + (1 << 40), 64, None)):
+            assert got == rc and (rc != B.EINVAL or "launch" in B.last_error()), T
+    # 8192 blocks of 128 columns, whole 128s of rows: 8 * 256 threads each
+    many = byref(rows(rows=40000, cols=1 << 20, q_stride=1 << 20, scale_stride=40000))
+    assert L.pgmoe_quantize_rows(P, 1 << 20, B.F32, 255 * 128, None, 1, many, None) == B.ENODEVICE
+    refused(L.pgmoe_quantize_rows(P, 1 << 20, B.F32, 255 * 128 + 1, None, 1, many, None), "launch")
+    # products of few rows, 512 threads for 16 rows and 128 outputs: eight rows for each of 256 experts, and rows far apart
+    for n, stride in ((256, 256), (1, 1 << 23)):
+        count = n * 8 if n > 1 else 65536 + 1
+        pieces = (count + 15 * n) // 16
+        blocks = ((1 << 23) - 1) // pieces
+        x = byref(rows(rows=count, q_stride=stride, scale_stride=count))
+        for nb, rc in ((blocks, B.ENODEVICE), (blocks + 1, B.EINVAL)):
+            got = L.pgmoe_expert_matmul(x, byref(weights(n_experts=n, n_out=nb * 128)), P, 0, P, nb * 128, B.BF16, None, None)
+            assert got == rc and (rc != B.EINVAL or "launch" in B.last_error()), (n, nb, got)
+
+
 def test_nothing_to_do_is_no_error():
     r = byref(router())
     assert B.lib.pgmoe_route(r, None, 64, None, 0, None, None, None, None) == B.OK
