@@ -29,7 +29,7 @@ struct Fp8Divisor {
     __device__ explicit Fp8Divisor(float s) : scale(s), inverse(1.f / s) {}
     __device__ float operator()(float x) const {
         const float q = x * inverse;
-        return fmaf(fmaf(-q, scale, x), inverse, q);
+        return fmaf(fmaf(q, scale, -x), -inverse, q);  // (the remainder's other sign would lose that of -0)
     }
 };
 struct Fp8CarefulDivisor {

@@ -376,6 +376,32 @@ def test_quantize_rows(B, kind, T, d, dtype, copies):
     assert np.all(got_q[untouched] == 1.0) and np.all(got_s[:, untouched] == 7.0) and np.all(got_q[:, blocks * 128:] == 1.0) and np.all(got_s[:, rows:] == 7.0)
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+def test_codes_keep_the_sign_of_zero(B, kind):
+    """-0 / scale is -0, in blocks of ordinary, tiny and infinite values and of zeros; of rows and of weights."""
+    say("quantize minus zero", kind)
+    x = np.random.default_rng(1).standard_normal((5, 256)).astype(np.float32)
+    x[1] *= np.float32(1e-38)
+    x[2, 3] = np.inf
+    x[4] = 0.0
+    x[:, ::7], x[:, 1::7] = -0.0, 0.0
+    x[3, ::5] = np.float32(-1e-30)                            # goes to -0 too
+    q, scale = torch.full((5, 256), 1.0, device="cuda").to(TORCH[kind]), torch.zeros(2, 5, device="cuda")
+    B.quantize_rows(dev(x), q, scale)
+    want, _ = O.quantize_rows(x, kind)
+    got = f64(q)
+    zero = want == 0
+    assert np.array_equal(got, want, equal_nan=True) and np.array_equal(np.signbit(got[zero]), np.signbit(x[zero]))
+    if kind == "e4m3":
+        w = np.concatenate([x[:4]] * 32)[None, :, :128].copy()
+        w[~np.isfinite(w)] = 1
+        sf, ssf = B.fp8_weight_shapes(1, 128, 128)
+        q, s = torch.zeros(sf, device="cuda").to(torch.float8_e4m3fn), torch.zeros(ssf, device="cuda")
+        B.quantize_weights(dev(w), q, s)
+        got, (want, _) = f64(q).reshape(-1)[O.tile_positions(128, 128)], O.quantize_weights(w)
+        assert np.array_equal(got, want[0]) and np.array_equal(np.signbit(got), np.signbit(w[0]))
+
+
 def test_quantize_rows_skips_rows_that_are_not_there(B):
     say("quantize rows outside")
     x = dev(np.random.default_rng(1).standard_normal((4, 128)), "bf16")
