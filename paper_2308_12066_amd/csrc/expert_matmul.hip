@@ -182,6 +182,9 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
     const bool live = (lane & 15) < ci.nrows;
     const int o = nb * FP8_BLOCK + tile * 16 + 4 * (lane >> 4);
     if constexpr (std::is_void<Y>::value) {
+        // past the last output are zeros, also where a row or a scale that is not finite made NaN of the weights' zeros
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = o + i < a.n_out ? acc[i] : 0.f;
         auto largest = [&](auto of) {  // of the row's 128 results: four a lane, 16 a wavefront
             float m = maximum(maximum(of(acc[0]), of(acc[1])), maximum(of(acc[2]), of(acc[3])));
             m = maximum(m, __shfl_xor(m, 16));
@@ -637,6 +640,17 @@ __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<R> &ite
     float amax[MC > 0 ? MC : 1];  // of a row's block, where that is quantised
     bool unusual = false;
     if constexpr (std::is_void<Y>::value) {
+        // past the last output are zeros, also where a row or a scale that is not finite made NaN of the weights' zeros
+        if ((block + 1) * FP8_BLOCK > a.n_out) {
+#pragma unroll
+            for (int i = 0; i < OT; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const bool there = o + 4 * RUN * (4 * i / RUN) + 4 * i % RUN + v < a.n_out;
+#pragma unroll
+                    for (int m = 0; m < MC; ++m) acc[i][m][v] = there ? acc[i][m][v] : 0.f;
+                }
+        }
         auto largest = [&](auto of) {
 #pragma unroll
             for (int m = 0; m < MC; ++m) {

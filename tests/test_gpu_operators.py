@@ -778,6 +778,24 @@ def test_expert_matmul_in_tiles_passes_on_what_is_not_finite(B, tile, column):
     assert np.all(q1[zero] == 0) and np.all(s1[:, [zero, odd]] == 2.0 ** -126) and (np.delete(s1, [zero, odd], 1) > 1e-6).all()
 
 
+# rows for a stream of weights, for tiles of 64 rows and for tiles of up to 256
+@pytest.mark.parametrize("counts", [[3, 18], TILED[64], [700, 1, 0, 1017, 530, 64, 1157, 31, 1500, 17, 130, 257]], ids=["few", "64", "256"])
+@pytest.mark.parametrize("n_out", [520, 600])
+def test_codes_past_the_last_output_are_zero(B, counts, n_out):
+    """Also of rows with a NaN, and where a scale is infinite and 0 times it is NaN."""
+    say("matmul past the last output", counts[:3], n_out)
+    p = Product(B, counts, 300, n_out)
+    p.x_q.view(torch.uint8)[5, 7] = 0x7F
+    p.x_scale[1, 9] = float("inf")
+    for kind in ("e4m3", "e5m2"):
+        nb = -(-n_out // 128)
+        q, s = torch.full((p.R, nb * 128), 1.0, device="cuda").to(TORCH[kind]), torch.zeros(nb, p.R, device="cuda")
+        p.run(q, s)
+        assert not bool(q.view(torch.uint8)[:, n_out:].any())
+        got = f64(q)[:, :n_out]
+        assert np.isnan(got[5]).all() and not np.isfinite(got[9]).any() and np.isfinite(np.delete(got, [5, 9], 0)).all() and np.isfinite(f64(s)).all()
+
+
 def test_gradient_of_rows_through_the_transposed_weights(B):
     """d_x = d_y . W^T by the same call on the `backward` tiles: against the formula, and against differences of the product."""
     say("matmul gradient")
