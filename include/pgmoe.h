@@ -487,6 +487,10 @@ int pgmoe_quantize_weights(const void *w, int w_dtype, const pgmoe_fp8_weights *
  * below 2^23 pieces of 16 rows and 128 outputs (at most rows / 16 + experts with rows, times ceil(n_out/128)). */
 int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, const int32_t *expert_offsets, int relu, void *y,
                         int64_t y_stride, int y_dtype, const pgmoe_fp8_rows *y_q, void *stream);
+/* Name of the kernel pgmoe_expert_matmul() launches for x and w (their sizes and x->q_stride; addresses are not looked at)
+ * and results of y_dtype (of a y_q its type): "matmul_few_rows_kernel", "matmul_tiles_kernel, 64 rows" or
+ * "matmul_tiles_kernel, 256 rows".  Static string; NULL if a size is below 1. */
+const char *pgmoe_expert_matmul_kernel_name(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, int y_dtype);
 
 /* ---- observability: duration of the expert-FFN kernel ------------------------------------
  * pgmoe_ffn_timing_begin() makes every following pgmoe_expert_ffn() bracket its main kernel

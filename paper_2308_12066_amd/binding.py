@@ -37,7 +37,7 @@ EXPORTS = [
     "pgmoe_permute", "pgmoe_expert_ffn", "pgmoe_combine", "pgmoe_stack_step", "pgmoe_device_flags",
     "pgmoe_ffn_timing_begin", "pgmoe_ffn_timing_end", "pgmoe_slot_address", "pgmoe_fetch_timing", "pgmoe_trace", "pgmoe_get_block_trace", "pgmoe_fetch_all_experts", "pgmoe_set_schedule",
     "pgmoe_ffn_kernel_name", "pgmoe_set_nonmoe_standin", "pgmoe_check_streams", "pgmoe_expert_ffn_static", "pgmoe_migration_engine", "pgmoe_fetch_experts_as_turn",
-    "pgmoe_route", "pgmoe_route_backward", "pgmoe_group_rows", "pgmoe_quantize_rows", "pgmoe_quantize_weights", "pgmoe_expert_matmul",
+    "pgmoe_route", "pgmoe_route_backward", "pgmoe_group_rows", "pgmoe_quantize_rows", "pgmoe_quantize_weights", "pgmoe_expert_matmul", "pgmoe_expert_matmul_kernel_name",
 ]
 
 
@@ -138,9 +138,11 @@ def _load():
     L.pgmoe_quantize_rows.argtypes = [vp, c_int64, i, i, vp, i, POINTER(FP8Rows), vp]
     L.pgmoe_quantize_weights.argtypes = [vp, i, POINTER(FP8Weights), POINTER(FP8Weights), vp]
     L.pgmoe_expert_matmul.argtypes = [POINTER(FP8Rows), POINTER(FP8Weights), vp, i, vp, c_int64, i, POINTER(FP8Rows), vp]
+    L.pgmoe_expert_matmul_kernel_name.argtypes = [POINTER(FP8Rows), POINTER(FP8Weights), i]
+    L.pgmoe_expert_matmul_kernel_name.restype = c_char_p
     L.pgmoe_ffn_timing_end.argtypes = [vp, POINTER(c_int), POINTER(c_float), POINTER(c_float)]
     for name in EXPORTS:
-        if name not in ("pgmoe_last_error", "pgmoe_expert_bytes", "pgmoe_workspace_bytes", "pgmoe_ffn_kernel_name"):
+        if name not in ("pgmoe_last_error", "pgmoe_expert_bytes", "pgmoe_workspace_bytes", "pgmoe_ffn_kernel_name", "pgmoe_expert_matmul_kernel_name"):
             getattr(L, name).restype = c_int
     return L
 
@@ -345,6 +347,13 @@ def expert_matmul(x_q, x_scale, w_q, w_scale, expert_offsets, n_in, n_out, y, y_
         rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, y.data_ptr(), _row_stride(y, "y"), _dtype(y, "y"), None, _stream(stream))
     if rc:
         raise PgmoeError(rc, last_error())
+
+
+def expert_matmul_kernel_name(rows, n_experts, n_in, n_out, y_dtype=BF16, q_stride=0):
+    """The kernel expert_matmul() launches for these sizes; q_stride: bytes from a row of codes to the next, 0: whole blocks."""
+    x = FP8Rows(None, q_stride or FP8_BLOCK * fp8_blocks(n_in), None, rows, rows, n_in, E4M3)
+    name = lib.pgmoe_expert_matmul_kernel_name(byref(x), byref(FP8Weights(None, None, n_experts, n_in, n_out)), y_dtype)
+    return name.decode() if name is not None else None
 
 
 class Context:

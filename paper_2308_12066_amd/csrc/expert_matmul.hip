@@ -782,45 +782,55 @@ static int launch_tiles(const MatmulArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((matmul_tiles_kernel<XQ, Y, YQ, VEC, R>), dim3(groups), dim3(TILE_THREADS), R::BYTES, s, a);
     return PGMOE_OK;
 }
+// Which kernel, by what there is to deal out; both sides in us a launch, bf16 results, rows dealt to the experts at random,
+// weights through the caches:
+//  * few rows, to 8 an expert: the tiles would be empty mostly (64 experts of 1024 x 4096, 8 rows each 50.4, in tiles of 64 rows 52.1; 12 rows
+//    54.7 / 52.4); also launches of at most two items of 16 rows a CU (64 rows for each of 8 experts of 4096 x 1024 23.3 / 44.2, 128 41.0 / 43.8,
+//    256 for one of 1024 x 4096 11.8 / 15.0; not 512 21.3 / 15.1, 48 for each of 8 19.5 / 14.9), and rows too far apart for the tiles;
+//  * tiles of 64 rows or of up to 256, by rounds of one item a workgroup, of which the larger take 4 / 3 as long (32 for each of 64 experts of
+//    1024 x 4096 55.9 / 63.6, 64 rows 79.7 / 75.8; 512 for each of 8 of 2048 x 768 26.5 / 31.0, 1024 46.3 / 39.4; 96 for each of 8 of
+//    1024 x 4096 17.0 / 20.4, 128 27.1 / 24.4).  An expert has half a chunk more than its rows fill, on the mean.
+// The inputs of few rows are split so that a wavefront has three blocks at least and there are 24 workgroups a CU at most (experts without rows
+// leave empty ones: 128 rows over 46 of 128 experts of 4096 x 1024, room for 1024 items, KS = 1 / 2 / 4 / 8 39.4 / 40.3 / 36.8 / 38.4, of 1024 x 4096 36.9 / 38.6 /
+// 45.2 / 64.2), further while workgroups are no more than two a CU: KS = 1 / 2 / 4 / 8
+// take 33.9 / 33.2 / 32.3 / 43.0 for one row for each of 64 experts of 1024 x 4096 (eight blocks), 6.8 / 5.0 / 5.1 / 5.0 for 64 rows of one, 6.6 / 4.8 / 3.8 / 3.0
+// for 16, 20.5 / 21.1 / 21.6 / 21.6 for 512 rows of one of 4096 x 1024, 38.2 / 31.5 / 25.5 / 23.7 for 64 for each of eight.
+struct MatmulPlan {
+    int tile;         // rows of an item of the tiled kernel, 64 or 256; 0: few rows
+    int ks;           // few rows: wavefronts that share the inputs
+    int64_t items16;  // few rows: pieces of 16 rows and 128 outputs, at most
+};
+static MatmulPlan matmul_plan(int rows, int E, int KB, int NB, int64_t x_stride, bool quantised) {
+    const int64_t active = std::min(E, rows), mean = rows / active, cols = (NB + 1) / 2;
+    const int64_t chunks16 = (rows + 15 * active) / 16, items16 = chunks16 * NB;
+    if (mean > 8 && items16 > 2 * TILE_GROUPS && x_stride < TILE_STRIDE_MAX) {
+        const auto rounds = [&](int most) { return (std::max(active, rows / most + active / 2) * cols + TILE_GROUPS - 1) / TILE_GROUPS; };
+        return {3 * rounds(64) <= 4 * rounds(256) ? 64 : 256, 0, items16};
+    }
+    const auto split = [&](int ks) { return ks * items16 <= (3 * ks <= KB ? 24 : ks <= KB ? 2 : 0) * TILE_GROUPS; };
+    return {0, quantised ? 1 : split(8) ? 8 : split(4) ? 4 : split(2) ? 2 : 1, items16};
+}
+
+template <int XQ, typename Y, int YQ, bool VEC, int KS>
+static void launch_few_rows(const MatmulArgs &a, int64_t items16, hipStream_t s) {
+    const dim3 grid((unsigned)(items16 * KS));
+    if (a.once) hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, true>), grid, dim3(FEW_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, false>), grid, dim3(FEW_THREADS), 0, s, a);
+}
 template <int XQ, typename Y, int YQ, bool VEC>
 static int launch_matmul(const MatmulArgs &a, hipStream_t s) {
-    // Which kernel, by what there is to deal out; both sides in us a launch, bf16 results, rows dealt to the experts at random,
-    // weights through the caches:
-    //  * few rows, to 8 an expert: the tiles would be empty mostly (64 experts of 1024 x 4096, 8 rows each 50.4, in tiles of 64 rows 52.1; 12 rows
-    //    54.7 / 52.4); also launches of at most two items of 16 rows a CU (64 rows for each of 8 experts of 4096 x 1024 23.3 / 44.2, 128 41.0 / 43.8,
-    //    256 for one of 1024 x 4096 11.8 / 15.0; not 512 21.3 / 15.1, 48 for each of 8 19.5 / 14.9), and rows too far apart for the tiles;
-    //  * tiles of 64 rows or of up to 256, by rounds of one item a workgroup, of which the larger take 4 / 3 as long (32 for each of 64 experts of
-    //    1024 x 4096 55.9 / 63.6, 64 rows 79.7 / 75.8; 512 for each of 8 of 2048 x 768 26.5 / 31.0, 1024 46.3 / 39.4; 96 for each of 8 of
-    //    1024 x 4096 17.0 / 20.4, 128 27.1 / 24.4).  An expert has half a chunk more than its rows fill, on the mean.
-    // The inputs of few rows are split so that a wavefront has three blocks at least and there are 24 workgroups a CU at most (experts without rows
-    // leave empty ones: 128 rows over 46 of 128 experts of 4096 x 1024, room for 1024 items, KS = 1 / 2 / 4 / 8 39.4 / 40.3 / 36.8 / 38.4, of 1024 x 4096 36.9 / 38.6 /
-    // 45.2 / 64.2), further while workgroups are no more than two a CU: KS = 1 / 2 / 4 / 8
-    // take 33.9 / 33.2 / 32.3 / 43.0 for one row for each of 64 experts of 1024 x 4096 (eight blocks), 6.8 / 5.0 / 5.1 / 5.0 for 64 rows of one, 6.6 / 4.8 / 3.8 / 3.0
-    // for 16, 20.5 / 21.1 / 21.6 / 21.6 for 512 rows of one of 4096 x 1024, 38.2 / 31.5 / 25.5 / 23.7 for 64 for each of eight.
-    const int64_t active = std::min(a.E, a.rows), mean = a.rows / active, cols = (a.NB + 1) / 2;
-    const int64_t chunks16 = (a.rows + 15 * active) / 16, items16 = chunks16 * a.NB;
-    if (mean > 8 && items16 > 2 * TILE_GROUPS && (int64_t)a.x_stride < TILE_STRIDE_MAX) {
-        const auto rounds = [&](int most) { return (std::max(active, a.rows / most + active / 2) * cols + TILE_GROUPS - 1) / TILE_GROUPS; };
-        if (3 * rounds(64) <= 4 * rounds(256)) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<1, 2>>(a, s);
-        return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<4, 8>>(a, s);
-    }
-    auto few = [&](auto ks_) -> int {
-        constexpr int KS = decltype(ks_)::value;
-        if (items16 * KS * FEW_THREADS > GRID_THREADS_MAX)
-            return fail(nullptr, PGMOE_EINVAL, "pgmoe_expert_matmul: %d rows by n_out=%d are more than one launch holds (%lld items of 16 rows and 128 outputs)", a.rows, a.n_out,
-                        (long long)items16);
-        const dim3 grid((unsigned)(items16 * KS));
-        if (a.once) hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, true>), grid, dim3(FEW_THREADS), 0, s, a);
-        else hipLaunchKernelGGL((matmul_few_rows_kernel<XQ, Y, YQ, VEC, KS, false>), grid, dim3(FEW_THREADS), 0, s, a);
-        return PGMOE_OK;
-    };
+    const MatmulPlan p = matmul_plan(a.rows, a.E, a.KB, a.NB, (int64_t)a.x_stride, std::is_void<Y>::value);
+    if (p.tile == 64) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<1, 2>>(a, s);
+    if (p.tile == 256) return launch_tiles<XQ, Y, YQ, VEC, MatmulShape<4, 8>>(a, s);
+    if (p.items16 * p.ks * FEW_THREADS > GRID_THREADS_MAX)
+        return fail(nullptr, PGMOE_EINVAL, "pgmoe_expert_matmul: %d rows by n_out=%d are more than one launch holds (%lld items of 16 rows and 128 outputs)", a.rows, a.n_out,
+                    (long long)p.items16);
     if constexpr (!std::is_void<Y>::value) {
-        const auto split = [&](int ks) { return ks * items16 <= (3 * ks <= a.KB ? 24 : ks <= a.KB ? 2 : 0) * TILE_GROUPS; };
-        if (split(8)) return few(std::integral_constant<int, 8>());
-        if (split(4)) return few(std::integral_constant<int, 4>());
-        if (split(2)) return few(std::integral_constant<int, 2>());
+        if (p.ks == 8) return launch_few_rows<XQ, Y, YQ, VEC, 8>(a, p.items16, s), PGMOE_OK;
+        if (p.ks == 4) return launch_few_rows<XQ, Y, YQ, VEC, 4>(a, p.items16, s), PGMOE_OK;
+        if (p.ks == 2) return launch_few_rows<XQ, Y, YQ, VEC, 2>(a, p.items16, s), PGMOE_OK;
     }
-    return few(std::integral_constant<int, 1>());
+    return launch_few_rows<XQ, Y, YQ, VEC, 1>(a, p.items16, s), PGMOE_OK;
 }
 template <int XQ, typename Y>
 static int launch_matmul_to(const MatmulArgs &a, hipStream_t s) {
@@ -897,4 +907,10 @@ extern "C" int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weig
     }
     rc = x->dtype == PGMOE_E4M3 ? launch_matmul<PGMOE_E4M3>(a, y_dtype, (hipStream_t)stream) : launch_matmul<PGMOE_E5M2>(a, y_dtype, (hipStream_t)stream);
     return rc ? rc : launched(fn);
+}
+
+extern "C" const char *pgmoe_expert_matmul_kernel_name(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, int y_dtype) {
+    if (!x || !w || x->rows < 1 || w->n_experts < 1 || w->n_in < 1 || w->n_out < 1) return nullptr;
+    const MatmulPlan p = matmul_plan(x->rows, w->n_experts, fp8_blocks(w->n_in), fp8_blocks(w->n_out), x->q_stride, y_dtype == PGMOE_E4M3 || y_dtype == PGMOE_E5M2);
+    return p.tile == 64 ? "matmul_tiles_kernel, 64 rows" : p.tile == 256 ? "matmul_tiles_kernel, 256 rows" : "matmul_few_rows_kernel";
 }

@@ -692,6 +692,27 @@ def test_expert_matmul_of_few_rows_with_its_inputs_split(B, counts, n_in, n_out)
 
 # Enough rows for the tiled kernels, of 64 rows and of up to 256: experts without rows, with one, with a few more than a whole chunk.
 TILED = {64: [20, 0, 65, 3, 64, 17, 1, 40] * 6, 256: [60, 1, 0, 17, 130, 64, 257, 31] * 5}
+# The second list is for tiles of 64 rows too by now, but for its widest results.  Chunks of 64 to 256 rows and what is left over of each:
+TILED["256 rows"] = [700, 1, 0, 1017, 530, 64, 1157, 31, 1500, 17, 130, 257]
+
+
+@pytest.mark.parametrize("n_out", [516, 517, 520, 600, 640, 644, 1100])
+def test_lists_of_rows_are_for_the_kernels_they_name(B, n_out):
+    for out in (B.F32, B.BF16, B.F16, B.E4M3, B.E5M2):
+        name = lambda tile: B.expert_matmul_kernel_name(sum(TILED[tile]), len(TILED[tile]), 640, n_out, out)  # noqa: E731
+        assert name(64) == "matmul_tiles_kernel, 64 rows" and name("256 rows") == "matmul_tiles_kernel, 256 rows"
+
+
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("n_in,n_out", [(1024, 640), (1300, 772)])
+def test_expert_matmul_in_tiles_over_many_blocks_of_inputs(B, relu, n_in, n_out):
+    """Items whose sums run over more blocks than the ring has stages, all types of results, rows of both types."""
+    say("matmul tiles many blocks", relu, n_in, n_out)
+    counts = TILED["256 rows"]
+    assert B.expert_matmul_kernel_name(sum(counts), len(counts), n_in, n_out) == "matmul_tiles_kernel, 256 rows"
+    p = Product(B, counts, n_in, n_out, "e5m2" if relu else "e4m3")
+    for out in ("f32", "bf16", "f16", "e4m3", "e5m2"):
+        p.check(out, relu)
 
 
 @pytest.mark.parametrize("tile", TILED)

@@ -158,6 +158,20 @@ def test_a_grid_has_less_than_2_to_the_32_threads():
             assert got == rc and (rc != B.EINVAL or "launch" in B.last_error()), (n, nb, got)
 
 
+def test_matmul_kernel_name_follows_the_launch_plan():
+    """The sizes its rule was measured at, both sides."""
+    few, t64, t256 = "matmul_few_rows_kernel", "matmul_tiles_kernel, 64 rows", "matmul_tiles_kernel, 256 rows"
+    for each, E, n_in, n_out, name in ((8, 64, 1024, 4096, few), (12, 64, 1024, 4096, t64), (64, 8, 4096, 1024, few), (256, 1, 1024, 4096, few), (512, 1, 1024, 4096, t64),
+                                       (48, 8, 1024, 4096, t64), (32, 64, 1024, 4096, t64), (64, 64, 1024, 4096, t256), (512, 8, 2048, 768, t64),
+                                       (1024, 8, 2048, 768, t256), (96, 8, 1024, 4096, t64), (128, 8, 1024, 4096, t256)):
+        for out in (B.F32, B.BF16, B.E4M3):
+            assert B.expert_matmul_kernel_name(each * E, E, n_in, n_out, out) == name, (each, E, n_in, n_out)
+    assert B.expert_matmul_kernel_name(8192, 8, 1024, 4096, q_stride=1 << 23) == few and B.expert_matmul_kernel_name(8192, 8, 1024, 4096, q_stride=(1 << 23) - 16) == t256
+    assert B.expert_matmul_kernel_name(1, 256, 1, 1) == few
+    assert B.expert_matmul_kernel_name(0, 8, 128, 128) is None and B.expert_matmul_kernel_name(8, 0, 128, 128) is None and B.expert_matmul_kernel_name(8, 8, 0, 128) is None
+    assert B.lib.pgmoe_expert_matmul_kernel_name(None, None, 0) is None
+
+
 def test_nothing_to_do_is_no_error():
     r = byref(router())
     assert B.lib.pgmoe_route(r, None, 64, None, 0, None, None, None, None) == B.OK
