@@ -277,32 +277,34 @@ def _fp8_weights(q, scale, n_in, n_out, name) -> FP8Weights:
 
 
 class Router:
-    """A pgmoe_router: how experts are selected and weighed from logits."""
+    """A pgmoe_router: how experts are selected and weighed from logits.  Threads may share one: a call changes nothing in it."""
 
     def __init__(self, n_experts, top_k, score=SCORE_SOFTMAX, n_groups=1, topk_groups=0, renormalize=False, scale=1.0):
-        self.cfg = RouterConfig(n_experts, top_k, n_groups, topk_groups, score, 1 if renormalize else 0, scale, F32)
+        self._cfgs = {t: RouterConfig(n_experts, top_k, n_groups, topk_groups, score, 1 if renormalize else 0, scale, t) for t in (F32, BF16, F16)}
         self._shape = n_experts, top_k
 
     def _outer(self, logits):
         stride, (T, E) = _row_stride(logits, "logits"), logits.shape
         if E != self._shape[0]:
             raise ValueError(f"logits of {E} experts, the router has {self._shape[0]}")
-        self.cfg.logits_dtype = _dtype(logits, "logits")
-        return T, E, self._shape[1], stride
+        cfg = self._cfgs.get(_DTYPES.get(logits.dtype))
+        if cfg is None:
+            raise TypeError(f"logits have dtype {logits.dtype}, neither float32 nor bfloat16 nor float16")
+        return byref(cfg), T, E, self._shape[1], stride
 
     def route(self, logits, bias, topk_idx, topk_weight, scores_out=None, stream=None):
-        T, E, k, stride = self._outer(logits)
-        rc = lib.pgmoe_route(byref(self.cfg), logits.data_ptr(), stride, None if bias is None else _expect(bias, "bias", (E,), _f32), T,
+        cfg, T, E, k, stride = self._outer(logits)
+        rc = lib.pgmoe_route(cfg, logits.data_ptr(), stride, None if bias is None else _expect(bias, "bias", (E,), _f32), T,
                              _expect(topk_idx, "topk_idx", (T, k), _i32), _expect(topk_weight, "topk_weight", (T, k), _f32),
                              None if scores_out is None else _expect(scores_out, "scores_out", (T, E), _f32), _stream(stream))
         if rc:
             raise PgmoeError(rc, last_error())
 
     def route_backward(self, logits, topk_idx, d_weight, d_scores, d_logits, stream=None):
-        T, E, k, stride = self._outer(logits)
+        cfg, T, E, k, stride = self._outer(logits)
         if d_logits.shape != (T, E) or d_logits.dtype != logits.dtype:
             raise ValueError(f"d_logits is {d_logits.dtype} {tuple(d_logits.shape)}, logits are {logits.dtype} {(T, E)}")
-        rc = lib.pgmoe_route_backward(byref(self.cfg), logits.data_ptr(), stride, _expect(topk_idx, "topk_idx", (T, k), _i32),
+        rc = lib.pgmoe_route_backward(cfg, logits.data_ptr(), stride, _expect(topk_idx, "topk_idx", (T, k), _i32),
                                       _expect(d_weight, "d_weight", (T, k), _f32), None if d_scores is None else _expect(d_scores, "d_scores", (T, E), _f32), T,
                                       d_logits.data_ptr(), _row_stride(d_logits, "d_logits"), _stream(stream))
         if rc:

@@ -238,6 +238,26 @@ def test_binding_refuses_tensors_that_do_not_fit():
         B.expert_matmul(q, s, wq, ws, torch.zeros(3, dtype=torch.int32), 100, 300, torch.zeros(5, 300))
 
 
+def test_a_router_shared_by_threads_keeps_the_types_of_their_logits_apart(monkeypatch):
+    """Another thread's call between the preparation of a call and its launch, as a switch of threads or the released lock allow."""
+    r = B.Router(8, 2)
+    out = lambda: (torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2))  # noqa: E731
+    seen = []
+
+    def launch(cfg, *rest):
+        own = len(seen)
+        seen.append(None)
+        if own == 0:
+            r.route(torch.zeros(4, 8, dtype=torch.bfloat16), None, *out())
+        seen[own] = cfg._obj.logits_dtype
+        return B.OK
+
+    monkeypatch.setattr(B.lib, "pgmoe_route", launch)
+    monkeypatch.setattr(B, "_stream_for", lambda *a: None, raising=False)      # tensors on the CPU
+    r.route(torch.zeros(4, 8), None, *out())
+    assert seen == [B.F32, B.BF16]
+
+
 # ------------------------------------------------------------------------------------ the plain forms
 def test_plain_codes_are_the_types_own():
     """Every finite value of both types is its own code, and values between two go to the nearer, ties to the even one."""
