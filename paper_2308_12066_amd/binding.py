@@ -207,8 +207,8 @@ def unique_experts(idx, n_experts: int):
     return out[:rc].copy()
 
 
-# ---- routing and 8-bit experts: no context; tensors carry their sizes, types and strides.  A call takes a few
-# microseconds on the GPU, so what is checked here is checked on the tensors' own attributes.
+# ---- routing and 8-bit experts: no context; tensors carry their sizes, types and strides, and lie on the current GPU.  A call
+# takes a few microseconds on the GPU, so what is checked here is checked on the tensors' own attributes.
 try:
     import torch as _torch
     _DTYPES = {_torch.float32: F32, _torch.bfloat16: BF16, _torch.float16: F16, _torch.float8_e4m3fn: E4M3, _torch.float8_e5m2: E5M2}
@@ -233,6 +233,18 @@ def _expect(t, name, shape, dtype):
     if not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
     return t.data_ptr()
+
+
+def _on_gpu(*tensors) -> None:
+    """The library launches on the current GPU and sees addresses: all tensors (None: not given) have to be that GPU's."""
+    device = tensors[0].get_device()      # -1: not on a GPU
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors on {tensors[0].device} and on {t.device}")
+    if device < 0:
+        raise ValueError(f"tensors on {tensors[0].device}: the operators take tensors on the GPU")
+    if device != _torch.cuda.current_device():
+        raise ValueError(f"tensors on {tensors[0].device}, the current GPU is cuda:{_torch.cuda.current_device()}")
 
 
 def _row_stride(t, name) -> int:
@@ -294,9 +306,11 @@ class Router:
 
     def route(self, logits, bias, topk_idx, topk_weight, scores_out=None, stream=None):
         cfg, T, E, k, stride = self._outer(logits)
-        rc = lib.pgmoe_route(cfg, logits.data_ptr(), stride, None if bias is None else _expect(bias, "bias", (E,), _f32), T,
-                             _expect(topk_idx, "topk_idx", (T, k), _i32), _expect(topk_weight, "topk_weight", (T, k), _f32),
-                             None if scores_out is None else _expect(scores_out, "scores_out", (T, E), _f32), _stream(stream))
+        args = (cfg, logits.data_ptr(), stride, None if bias is None else _expect(bias, "bias", (E,), _f32), T,
+                _expect(topk_idx, "topk_idx", (T, k), _i32), _expect(topk_weight, "topk_weight", (T, k), _f32),
+                None if scores_out is None else _expect(scores_out, "scores_out", (T, E), _f32))
+        _on_gpu(logits, bias, topk_idx, topk_weight, scores_out)
+        rc = lib.pgmoe_route(*args, _stream(stream))
         if rc:
             raise PgmoeError(rc, last_error())
 
@@ -304,9 +318,10 @@ class Router:
         cfg, T, E, k, stride = self._outer(logits)
         if d_logits.shape != (T, E) or d_logits.dtype != logits.dtype:
             raise ValueError(f"d_logits is {d_logits.dtype} {tuple(d_logits.shape)}, logits are {logits.dtype} {(T, E)}")
-        rc = lib.pgmoe_route_backward(cfg, logits.data_ptr(), stride, _expect(topk_idx, "topk_idx", (T, k), _i32),
-                                      _expect(d_weight, "d_weight", (T, k), _f32), None if d_scores is None else _expect(d_scores, "d_scores", (T, E), _f32), T,
-                                      d_logits.data_ptr(), _row_stride(d_logits, "d_logits"), _stream(stream))
+        args = (cfg, logits.data_ptr(), stride, _expect(topk_idx, "topk_idx", (T, k), _i32), _expect(d_weight, "d_weight", (T, k), _f32),
+                None if d_scores is None else _expect(d_scores, "d_scores", (T, E), _f32), T, d_logits.data_ptr(), _row_stride(d_logits, "d_logits"))
+        _on_gpu(logits, topk_idx, d_weight, d_scores, d_logits)
+        rc = lib.pgmoe_route_backward(*args, _stream(stream))
         if rc:
             raise PgmoeError(rc, last_error())
 
@@ -315,8 +330,9 @@ def quantize_rows(x, q, scale, row_of=None, copies=1, stream=None) -> None:
     """x [T, cols] -> codes q [rows, 128 * blocks] and scales [blocks, rows]; row_of [T * copies] deals the rows out."""
     stride, (T, cols) = _row_stride(x, "x"), x.shape
     out = _fp8_rows(q, scale, cols, "q")
-    rc = lib.pgmoe_quantize_rows(x.data_ptr(), stride, _dtype(x, "x"), T, None if row_of is None else _expect(row_of, "row_of", (T * copies,), _i32), copies,
-                                 byref(out), _stream(stream))
+    args = (x.data_ptr(), stride, _dtype(x, "x"), T, None if row_of is None else _expect(row_of, "row_of", (T * copies,), _i32), copies, byref(out))
+    _on_gpu(x, q, scale, row_of)
+    rc = lib.pgmoe_quantize_rows(*args, _stream(stream))
     if rc:
         raise PgmoeError(rc, last_error())
 
@@ -329,8 +345,9 @@ def quantize_weights(w, forward_q, forward_scale, backward_q=None, backward_scal
     for f in (fwd, bwd):
         if f is not None and f.n_experts != E:
             raise ValueError(f"codes of {f.n_experts} experts for {E}")
-    rc = lib.pgmoe_quantize_weights(_expect(w, "w", (E, n_in, n_out), w.dtype), _dtype(w, "w"), None if fwd is None else byref(fwd),
-                                    None if bwd is None else byref(bwd), _stream(stream))
+    args = (_expect(w, "w", (E, n_in, n_out), w.dtype), _dtype(w, "w"), None if fwd is None else byref(fwd), None if bwd is None else byref(bwd))
+    _on_gpu(w, *((forward_q, forward_scale) if fwd is not None else ()), *((backward_q, backward_scale) if bwd is not None else ()))
+    rc = lib.pgmoe_quantize_weights(*args, _stream(stream))
     if rc:
         raise PgmoeError(rc, last_error())
 
@@ -342,11 +359,13 @@ def expert_matmul(x_q, x_scale, w_q, w_scale, expert_offsets, n_in, n_out, y, y_
     offsets = _expect(expert_offsets, "expert_offsets", (w.n_experts + 1,), _i32)
     if y_scale is not None:
         out = _fp8_rows(y, y_scale, n_out, "y")
-        rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, None, 0, out.dtype, byref(out), _stream(stream))
+        args = (None, 0, out.dtype, byref(out))
     else:
         if y.shape != (x.rows, n_out):
             raise ValueError(f"y has shape {tuple(y.shape)}, not {(x.rows, n_out)}")
-        rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, y.data_ptr(), _row_stride(y, "y"), _dtype(y, "y"), None, _stream(stream))
+        args = (y.data_ptr(), _row_stride(y, "y"), _dtype(y, "y"), None)
+    _on_gpu(x_q, x_scale, w_q, w_scale, expert_offsets, y, y_scale)
+    rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, *args, _stream(stream))
     if rc:
         raise PgmoeError(rc, last_error())
 

@@ -253,9 +253,52 @@ def test_a_router_shared_by_threads_keeps_the_types_of_their_logits_apart(monkey
         return B.OK
 
     monkeypatch.setattr(B.lib, "pgmoe_route", launch)
-    monkeypatch.setattr(B, "_stream_for", lambda *a: None, raising=False)      # tensors on the CPU
+    monkeypatch.setattr(B, "_on_gpu", lambda *a: None, raising=False)           # tensors on the CPU
     r.route(torch.zeros(4, 8), None, *out())
     assert seen == [B.F32, B.BF16]
+
+
+class OnGpu(torch.Tensor):
+    """A tensor that says it is on a GPU (or, set, on another): no launch follows."""
+    gpu = 0
+
+    def get_device(self):
+        return self.gpu
+
+
+def calls(on=lambda t: t.as_subclass(OnGpu)):
+    """Every operator of the binding with tensors that fit: (name, call, tensors by name)."""
+    new = lambda *s, dtype=torch.float32: on(torch.zeros(s, dtype=dtype))  # noqa: E731
+    r, i32, f8 = B.Router(8, 2), torch.int32, torch.float8_e4m3fn
+    (sf, ssf), (sb, ssb) = B.fp8_weight_shapes(2, 100, 300), B.fp8_weight_shapes(2, 300, 100)
+    route = dict(logits=new(4, 8), bias=new(8), topk_idx=new(4, 2, dtype=i32), topk_weight=new(4, 2), scores_out=new(4, 8))
+    back = dict(logits=new(4, 8), topk_idx=new(4, 2, dtype=i32), d_weight=new(4, 2), d_scores=new(4, 8), d_logits=new(4, 8))
+    rows = dict(x=new(4, 100), q=new(8, 128, dtype=f8), scale=new(1, 8), row_of=new(8, dtype=i32))
+    weights = dict(w=new(2, 100, 300), forward_q=new(*sf, dtype=f8), forward_scale=new(*ssf), backward_q=new(*sb, dtype=f8), backward_scale=new(*ssb))
+    wide = dict(x_q=new(4, 128, dtype=f8), x_scale=new(1, 4), w_q=new(*sf, dtype=f8), w_scale=new(*ssf), expert_offsets=new(3, dtype=i32), y=new(4, 300))
+    eight = dict(wide, y=new(4, 384, dtype=f8), y_scale=new(3, 4))
+    return [("pgmoe_route", r.route, route), ("pgmoe_route_backward", r.route_backward, back), ("pgmoe_quantize_rows", lambda **k: B.quantize_rows(copies=2, **k), rows),
+            ("pgmoe_quantize_weights", B.quantize_weights, weights), ("pgmoe_expert_matmul", lambda **k: B.expert_matmul(n_in=100, n_out=300, **k), wide),
+            ("pgmoe_expert_matmul", lambda **k: B.expert_matmul(n_in=100, n_out=300, **k), eight)]
+
+
+@pytest.mark.parametrize("which", range(6))
+def test_binding_refuses_tensors_that_are_not_on_the_current_gpu(monkeypatch, which):
+    launched = []
+    name, call, tensors = calls()[which]
+    monkeypatch.setattr(B.lib, name, lambda *a: launched.append(a) or B.OK)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    call(**tensors, stream=0)
+    assert len(launched) == 1
+    for arg, t in tensors.items():
+        with pytest.raises(ValueError, match="tensors on"):
+            call(**dict(tensors, **{arg: torch.zeros_like(t.as_subclass(torch.Tensor))}), stream=0)      # on the CPU
+    with pytest.raises(ValueError, match="GPU"):
+        call(**{a: t.as_subclass(torch.Tensor) for a, t in tensors.items()}, stream=0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="cuda:1"):
+        call(**tensors, stream=0)
+    assert len(launched) == 1
 
 
 # ------------------------------------------------------------------------------------ the plain forms
