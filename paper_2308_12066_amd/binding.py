@@ -208,11 +208,14 @@ def unique_experts(idx, n_experts: int):
 
 
 # ---- routing and 8-bit experts: no context; tensors carry their sizes, types and strides, and lie on the current GPU.  A call
-# takes a few microseconds on the GPU, so what is checked here is checked on the tensors' own attributes.
+# takes a few microseconds on the GPU, so what is checked here is checked on the tensors' own attributes.  Without a stream a call
+# goes to torch's current one; stream=0 is the null stream.
 try:
     import torch as _torch
     _DTYPES = {_torch.float32: F32, _torch.bfloat16: BF16, _torch.float16: F16, _torch.float8_e4m3fn: E4M3, _torch.float8_e5m2: E5M2}
     _f32, _i32 = _torch.float32, _torch.int32
+    # address of torch's current stream on a GPU: without a Stream object made for each call, 0.3 us of a call instead of 3
+    _current_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: _torch.cuda.current_stream(device).cuda_stream)
 except ImportError:  # the calls below take torch tensors
     _DTYPES, _f32, _i32 = {}, None, None
 
@@ -235,8 +238,9 @@ def _expect(t, name, shape, dtype):
     return t.data_ptr()
 
 
-def _on_gpu(*tensors) -> None:
-    """The library launches on the current GPU and sees addresses: all tensors (None: not given) have to be that GPU's."""
+def _stream_for(stream, *tensors):
+    """The stream of a call: the given one, or torch's current one, on which the caller's torch operations run.  The library
+    launches on the current GPU and sees addresses: all tensors (None: not given) have to be that GPU's."""
     device = tensors[0].get_device()      # -1: not on a GPU
     for t in tensors:
         if t is not None and t.get_device() != device:
@@ -245,6 +249,7 @@ def _on_gpu(*tensors) -> None:
         raise ValueError(f"tensors on {tensors[0].device}: the operators take tensors on the GPU")
     if device != _torch.cuda.current_device():
         raise ValueError(f"tensors on {tensors[0].device}, the current GPU is cuda:{_torch.cuda.current_device()}")
+    return c_void_p(_current_stream(device)) if stream is None else _stream(stream)
 
 
 def _row_stride(t, name) -> int:
@@ -292,16 +297,20 @@ class Router:
     """A pgmoe_router: how experts are selected and weighed from logits.  Threads may share one: a call changes nothing in it."""
 
     def __init__(self, n_experts, top_k, score=SCORE_SOFTMAX, n_groups=1, topk_groups=0, renormalize=False, scale=1.0):
-        self._cfgs = {t: RouterConfig(n_experts, top_k, n_groups, topk_groups, score, 1 if renormalize else 0, scale, t) for t in (F32, BF16, F16)}
+        self._fields = n_experts, top_k, n_groups, topk_groups, score, 1 if renormalize else 0, scale
+        self._cfgs = {F32: RouterConfig(*self._fields, F32)}      # by the logits' type, as they come
         self._shape = n_experts, top_k
 
     def _outer(self, logits):
         stride, (T, E) = _row_stride(logits, "logits"), logits.shape
         if E != self._shape[0]:
             raise ValueError(f"logits of {E} experts, the router has {self._shape[0]}")
-        cfg = self._cfgs.get(_DTYPES.get(logits.dtype))
+        code = _DTYPES.get(logits.dtype)
+        cfg = self._cfgs.get(code)
         if cfg is None:
-            raise TypeError(f"logits have dtype {logits.dtype}, neither float32 nor bfloat16 nor float16")
+            if code not in (BF16, F16):
+                raise TypeError(f"logits have dtype {logits.dtype}, neither float32 nor bfloat16 nor float16")
+            cfg = self._cfgs[code] = RouterConfig(*self._fields, code)
         return byref(cfg), T, E, self._shape[1], stride
 
     def route(self, logits, bias, topk_idx, topk_weight, scores_out=None, stream=None):
@@ -309,8 +318,7 @@ class Router:
         args = (cfg, logits.data_ptr(), stride, None if bias is None else _expect(bias, "bias", (E,), _f32), T,
                 _expect(topk_idx, "topk_idx", (T, k), _i32), _expect(topk_weight, "topk_weight", (T, k), _f32),
                 None if scores_out is None else _expect(scores_out, "scores_out", (T, E), _f32))
-        _on_gpu(logits, bias, topk_idx, topk_weight, scores_out)
-        rc = lib.pgmoe_route(*args, _stream(stream))
+        rc = lib.pgmoe_route(*args, _stream_for(stream, logits, bias, topk_idx, topk_weight, scores_out))
         if rc:
             raise PgmoeError(rc, last_error())
 
@@ -320,8 +328,7 @@ class Router:
             raise ValueError(f"d_logits is {d_logits.dtype} {tuple(d_logits.shape)}, logits are {logits.dtype} {(T, E)}")
         args = (cfg, logits.data_ptr(), stride, _expect(topk_idx, "topk_idx", (T, k), _i32), _expect(d_weight, "d_weight", (T, k), _f32),
                 None if d_scores is None else _expect(d_scores, "d_scores", (T, E), _f32), T, d_logits.data_ptr(), _row_stride(d_logits, "d_logits"))
-        _on_gpu(logits, topk_idx, d_weight, d_scores, d_logits)
-        rc = lib.pgmoe_route_backward(*args, _stream(stream))
+        rc = lib.pgmoe_route_backward(*args, _stream_for(stream, logits, topk_idx, d_weight, d_scores, d_logits))
         if rc:
             raise PgmoeError(rc, last_error())
 
@@ -331,8 +338,7 @@ def quantize_rows(x, q, scale, row_of=None, copies=1, stream=None) -> None:
     stride, (T, cols) = _row_stride(x, "x"), x.shape
     out = _fp8_rows(q, scale, cols, "q")
     args = (x.data_ptr(), stride, _dtype(x, "x"), T, None if row_of is None else _expect(row_of, "row_of", (T * copies,), _i32), copies, byref(out))
-    _on_gpu(x, q, scale, row_of)
-    rc = lib.pgmoe_quantize_rows(*args, _stream(stream))
+    rc = lib.pgmoe_quantize_rows(*args, _stream_for(stream, x, q, scale, row_of))
     if rc:
         raise PgmoeError(rc, last_error())
 
@@ -346,8 +352,8 @@ def quantize_weights(w, forward_q, forward_scale, backward_q=None, backward_scal
         if f is not None and f.n_experts != E:
             raise ValueError(f"codes of {f.n_experts} experts for {E}")
     args = (_expect(w, "w", (E, n_in, n_out), w.dtype), _dtype(w, "w"), None if fwd is None else byref(fwd), None if bwd is None else byref(bwd))
-    _on_gpu(w, *((forward_q, forward_scale) if fwd is not None else ()), *((backward_q, backward_scale) if bwd is not None else ()))
-    rc = lib.pgmoe_quantize_weights(*args, _stream(stream))
+    given = ((forward_q, forward_scale) if fwd is not None else ()) + ((backward_q, backward_scale) if bwd is not None else ())
+    rc = lib.pgmoe_quantize_weights(*args, _stream_for(stream, w, *given))
     if rc:
         raise PgmoeError(rc, last_error())
 
@@ -364,8 +370,7 @@ def expert_matmul(x_q, x_scale, w_q, w_scale, expert_offsets, n_in, n_out, y, y_
         if y.shape != (x.rows, n_out):
             raise ValueError(f"y has shape {tuple(y.shape)}, not {(x.rows, n_out)}")
         args = (y.data_ptr(), _row_stride(y, "y"), _dtype(y, "y"), None)
-    _on_gpu(x_q, x_scale, w_q, w_scale, expert_offsets, y, y_scale)
-    rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, *args, _stream(stream))
+    rc = lib.pgmoe_expert_matmul(byref(x), byref(w), offsets, 1 if relu else 0, *args, _stream_for(stream, x_q, x_scale, w_q, w_scale, expert_offsets, y, y_scale))
     if rc:
         raise PgmoeError(rc, last_error())
 
@@ -378,7 +383,8 @@ def expert_matmul_kernel_name(rows, n_experts, n_in, n_out, y_dtype=BF16, q_stri
 
 
 class Context:
-    """Owns a pgmoe_ctx*.  Methods take tensors (anything with data_ptr()) or raw addresses."""
+    """Owns a pgmoe_ctx*.  Methods take tensors (anything with data_ptr()) or raw addresses; without a stream they launch on
+    the null stream, group_rows() with tensors on torch's current one."""
 
     def __init__(self, cfg: Config):
         self.cfg = cfg
@@ -441,7 +447,10 @@ class Context:
                                       _ptr(expert_offsets), _stream(stream)))
 
     def group_rows(self, topk_idx, T, row_of, expert_offsets, stream=None):
-        self._check(lib.pgmoe_group_rows(self._h, _ptr(topk_idx), T, _ptr(row_of), _ptr(expert_offsets), _stream(stream)))
+        """Without a stream: on torch's current one, as the operators it stands between, if the arguments are tensors."""
+        tensors = topk_idx, row_of, expert_offsets
+        on = _stream_for(stream, *tensors) if all(hasattr(t, "get_device") for t in tensors) else _stream(stream)
+        self._check(lib.pgmoe_group_rows(self._h, _ptr(topk_idx), T, _ptr(row_of), _ptr(expert_offsets), on))
 
     def expert_ffn(self, block, x_perm, expert_offsets, n_rows, y_perm, workspace, stream=None):
         self._check(lib.pgmoe_expert_ffn(self._h, block, _ptr(x_perm), _ptr(expert_offsets), n_rows, _ptr(y_perm),

@@ -253,7 +253,7 @@ def test_a_router_shared_by_threads_keeps_the_types_of_their_logits_apart(monkey
         return B.OK
 
     monkeypatch.setattr(B.lib, "pgmoe_route", launch)
-    monkeypatch.setattr(B, "_on_gpu", lambda *a: None, raising=False)           # tensors on the CPU
+    monkeypatch.setattr(B, "_stream_for", lambda *a: None, raising=False)      # tensors on the CPU
     r.route(torch.zeros(4, 8), None, *out())
     assert seen == [B.F32, B.BF16]
 
@@ -299,6 +299,40 @@ def test_binding_refuses_tensors_that_are_not_on_the_current_gpu(monkeypatch, wh
     with pytest.raises(ValueError, match="cuda:1"):
         call(**tensors, stream=0)
     assert len(launched) == 1
+
+
+@pytest.mark.parametrize("which", range(6))
+def test_binding_launches_on_torchs_current_stream_or_the_given_one(monkeypatch, which):
+    """Torch operations before and after a call run on the current stream: on another one the call would race with them."""
+    launched = []
+    name, call, tensors = calls()[which]
+    monkeypatch.setattr(B.lib, name, lambda *a: launched.append(a[-1]) or B.OK)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+    monkeypatch.setattr(B, "_current_stream", lambda gpu: 0x1230 + gpu)
+    call(**tensors)
+    Other = type("Other", (), {"cuda_stream": 0x4560})
+    call(**tensors, stream=Other)
+    call(**tensors, stream=0x7890)
+    call(**tensors, stream=0)
+    assert [None if s is None else s.value for s in launched] == [0x1230, 0x4560, 0x7890, None]
+
+
+def test_group_rows_launches_on_torchs_current_stream_or_the_given_one(monkeypatch):
+    launched = []
+    monkeypatch.setattr(B.lib, "pgmoe_group_rows", lambda *a: launched.append(a[-1]) or B.OK)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    current = [0x1230]
+    monkeypatch.setattr(B, "_current_stream", lambda gpu: current[gpu])
+    c = B.Context(B.make_config(64, 128, 8, 2, 1, 32, B.BF16, flags=B.FLAG_HOST_ONLY))
+    idx, row_of, offs = (torch.zeros(n, dtype=torch.int32).as_subclass(OnGpu) for n in (8, 8, 9))
+    c.group_rows(idx, 4, row_of, offs)
+    current[0] = 0
+    c.group_rows(idx, 4, row_of, offs)
+    c.group_rows(idx, 4, row_of, offs, 0x4560)
+    c.group_rows(P, 4, P, P)                                            # addresses: the null stream, as all calls of a context
+    assert [None if s is None else s.value for s in launched] == [0x1230, None, 0x4560, None]
+    c.close()
 
 
 # ------------------------------------------------------------------------------------ the plain forms
