@@ -52,7 +52,9 @@ class Block:
         return x.float() @ self.gate
 
     def forward(self, x, logits, stream=None):
-        """x [T, d] bf16, logits [T, E] -> y [T, d] bf16 (this block's buffer).  Nothing is allocated: it may be captured into a graph."""
+        """x [T, d] bf16, logits [T, E] -> y [T, d] bf16 (this block's buffer), on `stream` or torch's current one.  Nothing is allocated:
+        it may be captured into a graph."""
+        stream = stream or torch.cuda.current_stream()   # a context's calls take the null stream otherwise
         (w1, s1), (w2, s2) = self.w[0][:2], self.w[1][:2]
         self.router.route(logits, None, self.idx, self.weight, None, stream)
         self.ctx.group_rows(self.idx, self.T, self.row_of, self.offsets, stream)
@@ -62,8 +64,14 @@ class Block:
         self.ctx.combine(self.y_rows, self.row_of, self.weight, self.T, self.y, stream=stream)
         return self.y
 
-    def backward(self, logits, d_y):
-        """d_y [T, d] float32, after forward() on the same logits -> (d_x through the experts [T, d] bf16, d_logits [T, E])."""
+    def backward(self, logits, d_y, stream=None):
+        """d_y [T, d] float32, after forward() on the same logits -> (d_x through the experts [T, d] bf16, d_logits [T, E]), on `stream` or
+        torch's current one, like forward(): torch's operations and the library's one behind the other."""
+        stream = stream or torch.cuda.current_stream()
+        with torch.cuda.stream(stream):
+            return self._backward(logits, d_y, stream)
+
+    def _backward(self, logits, d_y, stream):
         T, k, R = self.T, self.k, self.T * self.k
         at = self.row_of.long()
         # y[t] = sum over j of weight[t, j] * y_rows[row_of[t, j]]
@@ -79,7 +87,7 @@ class Block:
         d_rows = torch.empty(R, self.d, dtype=torch.bfloat16, device="cuda")
         B.expert_matmul(g, s, *self.w[0][2:], self.offsets, self.f, self.d, d_rows)
         d_x = torch.empty(T, self.d, dtype=torch.bfloat16, device="cuda")
-        self.ctx.combine(d_rows, self.row_of, torch.ones_like(self.weight), T, d_x)
+        self.ctx.combine(d_rows, self.row_of, torch.ones_like(self.weight), T, d_x, stream=stream)
         d_logits = torch.empty_like(logits)
         self.router.route_backward(logits, self.idx, d_weight, None, d_logits)
         return d_x, d_logits

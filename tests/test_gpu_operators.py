@@ -257,6 +257,25 @@ def test_route_reads_strided_logits_on_another_stream(B):
     assert np.allclose(got[1], want[1], rtol=80 * H, atol=0) and np.allclose(got[2], want[2], rtol=80 * H, atol=0)
 
 
+def test_route_on_another_stream_behind_what_filled_its_outputs(B):
+    """As above, the stream waiting until the outputs have been filled; and on torch's current stream without naming it."""
+    say("route stream")
+    wide = dev(np.random.default_rng(7).standard_normal((70, 101)), "bf16")
+    z, r, stream = wide[:, 3:40], B.Router(37, 5), torch.cuda.Stream()
+    want = O.route(f64(z), "softmax", 5)
+    for named in (True, False):
+        idx, w, s = torch.full((70, 5), -7, dtype=torch.int32, device="cuda"), torch.full((70, 5), 7.0, device="cuda"), torch.full((70, 37), 7.0, device="cuda")
+        stream.wait_stream(torch.cuda.current_stream())
+        if named:
+            r.route(z, None, idx, w, s, stream)
+        else:
+            with torch.cuda.stream(stream):
+                r.route(z, None, idx, w, s)
+        stream.synchronize()
+        assert np.array_equal(idx.cpu().numpy(), want[0])
+        assert np.allclose(f64(w), want[1], rtol=80 * H, atol=0) and np.allclose(f64(s), want[2], rtol=80 * H, atol=0)
+
+
 def check_backward(B, z, kind, k, dtype, every, renormalize, scale=1.0, idx=None, strided=False):
     g = np.random.default_rng(z.size + k)
     T, E = z.shape
@@ -963,6 +982,42 @@ def test_example_of_a_block_with_8_bit_experts(example, T, d, f, E, k):
     errors, us, same = example.run(T, d, f, E, k, replays=3)
     assert same and us > 0
     assert errors["y"] < 2.0 ** -4 and all(np.isfinite(v) for v in errors.values()), errors
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_example_on_another_stream(example, given):
+    """Forward and backward, inputs written late on a stream that is not the default one: the bits of the default one."""
+    say("example stream", given)
+    T, d, f, E, k = 200, 256, 512, 8, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w1, w2 = (0.05 * torch.randn(E, a, b, generator=g, device="cuda") for a, b in ((d, f), (f, d)))
+    x, z, dy = torch.randn(T, d, generator=g, device="cuda").bfloat16(), torch.randn(T, E, generator=g, device="cuda"), torch.randn(T, d, generator=g, device="cuda")
+    block = example.Block(w1, w2, None, k, T, renormalize=True)
+    want = block.forward(x, z).clone(), *block.backward(z, dy)
+    torch.cuda.synchronize()
+    for b in (block.y, block.y_rows, block.weight, block.idx, block.row_of, block.offsets):
+        b.zero_()
+    late_x, late_z, late_dy = torch.zeros_like(x), torch.zeros_like(z), torch.zeros_like(dy)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device="cuda")
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for _ in range(3):
+            big = big @ big * 1e-4                           # some milliseconds
+        for to, of in ((late_x, x), (late_z, z), (late_dy, dy)):
+            to.copy_(of)
+        if not given:
+            got = block.forward(late_x, late_z).clone(), *block.backward(late_z, late_dy)
+    if given:
+        block.forward(late_x, late_z, stream)
+        got = block.backward(late_z, late_dy, stream)
+        stream.synchronize()
+        got = block.y.clone(), *got
+    stream.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    block.close()
 
 
 @pytest.mark.parametrize("T,d,f,E,k", [(1, 256, 512, 8, 2), (60, 128, 300, 16, 3)])
