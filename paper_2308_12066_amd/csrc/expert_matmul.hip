@@ -217,8 +217,9 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
 // stages of an item arrive, and the results of the one before leave, under products.  Items of up
 // to 256 rows: eight wavefronts as 2 x 4, wavefront (wn, wm) with 128 outputs (one scale) and the row tiles wm, wm + 4, ..; of up to 64 rows:
 // 8 x 1, 32 outputs and all row tiles each (4 + 4 of 16 conversions a block of inputs, where 2 x 4 would take 8 + 1).
-// What bounds it are the conversions and scales beside the matrix cores' products: 32768 rows over 128 experts of 1024 x 4096 with
-// quantised results 330 us (0.83 PFLOP/s), 8192 rows of one of 4096 x 4096 1.28 PFLOP/s, 4099 over eight of 2048 x 768 (1.2 us a block, one item for
+// 32768 rows over 128 experts of 1024 x 4096 take 318 us with bfloat16 results, 324 to 338 with quantised ones (0.81 to 0.85 PFLOP/s); the products alone
+// would take 204.  In trials that left work out, bfloat16 results, 312 us then: without loads 258, without stores 285, without either 236, of which
+// 32 are conversions and scales beside the products.  8192 rows of one of 4096 x 4096 1.30 PFLOP/s, 4099 over eight of 2048 x 768 (1.2 us a block, one item for
 // 204 of 256 CUs) 25 to 26 us.
 //
 // LDS, a stage: 16 weight tiles of 2 KiB, 64 bytes more behind each; rows of 128 bytes whose 16-byte pieces are

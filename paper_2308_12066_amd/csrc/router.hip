@@ -8,11 +8,12 @@
 // an expert that is unavailable, outside the kept groups, or taken.  The last four bits of a key are the expert's place in its lane
 // (15 the first), so that a lane's largest key names its expert, the first of equal ones.  What is compared are so 32-bit results
 // without their last four bits; hence the chosen neighbours (and the two groups at the border) are looked at once more, and a token where two of them
-// lie closer than CLOSE is decided in 64 bits.  Values that are equal because logit and bias are equal are no such case: either
+// lie close by the measure at CLOSE is decided in 64 bits.  Values that are equal because logit and bias are equal are no such case: either
 // way the lowest index wins.  16-bit logits without a bias have those bits to spare.
 //
 // What bounds it is not bytes but the chain of dependent instructions of the searches: 16384 tokens of 256 experts, 8 of them, sigmoid,
-// bfloat16, take 7.5 us (1.3 TB/s), 12.3 with a bias and 15.9 with groups too; of 128 experts 2, softmax with a bias, 7.3; one token 3.0.
+// bfloat16, take 7.6 us (1.2 TB/s), 12.4 with a bias and 16.5 with groups too; softmax of as many without and with a bias 10.4 and 18.4 (131
+// registers, three wavefronts a SIMD where the sigmoid has four); softmax of 128 experts, 2 of them, 5.4 and 8.5; one token 3.1.
 // The gradient of 16384 x 128 float32 with that of the scores 7.8 us (3.2 TB/s), of 8191 x 256 bfloat16 6.1.
 #include <algorithm>
 #include <climits>
