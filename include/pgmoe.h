@@ -442,7 +442,7 @@ int pgmoe_group_rows(pgmoe_ctx *ctx, const int32_t *topk_idx, int T, int32_t *ro
 
 /* ---- experts in 8-bit floating point, one scale for each block of 128 -----------------------
  * A value is its code times the scale of its block.  Quantising a block: scale = largest magnitude of its
- * finite values / largest value of the type (448 or 57344), at least 2^-126; code = value / scale, a 32-bit
+ * finite values / largest value of the type (448 or 57344), at least 2^-126 (or a power of two, PGMOE_SCALE_POW2 below); code = value / scale, a 32-bit
  * quotient rounded to the nearest, ties to even.  NaN stays NaN; an infinity becomes NaN in e4m3 and stays one in
  * e5m2.  All divisions are correctly rounded: the codes are a function of the input alone.
  *
@@ -454,8 +454,13 @@ typedef struct {
     float *scale;         /* dev [ceil(cols/128), scale_stride] */
     int64_t scale_stride; /* >= rows */
     int32_t rows, cols;
-    int32_t dtype;        /* PGMOE_E4M3 or PGMOE_E5M2 */
+    int32_t dtype;        /* PGMOE_E4M3 or PGMOE_E5M2, possibly | PGMOE_SCALE_POW2 */
 } pgmoe_fp8_rows;
+/* In the dtype of rows that are written: a block's scale is the least power of two, at least 2^-126, by which its largest finite
+ * magnitude is within the type (so that code times scale is a bfloat16 as it stands: pgmoe_expert_weight_gradient() needs a
+ * third of the products); codes are as exact as with any scale.  (A block's value from 2^128 (1 - 2^-5) on, e5m2 2^128 (1 - 2^-4), becomes 2^128, which
+ * float32 takes for an infinity.)  In the dtype of rows that are read: the scales are powers of two, which only that call looks at. */
+#define PGMOE_SCALE_POW2 0x100
 /* Weights, e4m3: the matrices of n_experts experts, y = x . W with W [n_in, n_out] as everywhere in this header, one
  * scale for each 128 x 128 block: scale[(e * ceil(n_out/128) + o/128) * ceil(n_in/128) + i/128].  The code of input i
  * and output o of expert e is byte
@@ -491,6 +496,53 @@ int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, con
  * and results of y_dtype (of a y_q its type): "matmul_few_rows_kernel", "matmul_tiles_kernel, 64 rows" or
  * "matmul_tiles_kernel, 256 rows".  Static string; NULL if a size is below 1. */
 const char *pgmoe_expert_matmul_kernel_name(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, int y_dtype);
+
+/* ---- training a block of experts: rows there and back with weights, and the gradients ------------
+ * Entry n = t * copies + j of row_of dev [T * copies] is the row of token t's copy j, as pgmoe_permute and pgmoe_group_rows give it (copies = k); entries
+ * in [0, n_rows) are distinct, others are copies that were dropped: they write and add nothing.  Rows that no entry names are left as they were.
+ * weight dev [T, copies] f32 | NULL (1 each).  Values have one of PGMOE_F32, BF16, F16 a matrix, rows stride >= d elements apart; arithmetic is in float32, rounded
+ * once.  T * copies is below 2^26.  These calls need no context, allocate nothing and may be captured into a HIP graph, like those above. */
+/* rows[row_of[t, j]] = weight[t, j] * x[t], as values, as codes (rows_q: n_rows x d) or both; either may be NULL.
+ *   x dev [T, d]    rows dev [n_rows, d] out */
+int pgmoe_dispatch_rows(const void *x, int64_t x_stride, int x_dtype, int T, int d, const int32_t *row_of, int copies,
+                        const float *weight, void *rows, int64_t rows_stride, int rows_dtype, int n_rows,
+                        const pgmoe_fp8_rows *rows_q, void *stream);
+/* y[t] = add[t] + sum over j of weight[t, j] * rows[row_of[t, j]], in ascending j; without weights the gradient of
+ * pgmoe_dispatch_rows().
+ *   rows dev [n_rows, d]    add dev [T, d] in y's type | NULL; may be y itself    y dev [T, d] out */
+int pgmoe_combine_rows(const void *rows, int64_t rows_stride, int rows_dtype, int n_rows, const int32_t *row_of, int copies,
+                       const float *weight, const void *add, int64_t add_stride, int T, int d, void *y, int64_t y_stride,
+                       int y_dtype, void *stream);
+/* Gradients of pgmoe_combine_rows() (add's is d_y itself):
+ *   d_rows[row_of[t, j]] = weight[t, j] * d_y[t]         values in rows_dtype, codes (d_rows_q: n_rows x d), both, or neither
+ *   d_weight[t, j] = sum over the columns of d_y[t] * rows[row_of[t, j]], 0 for a dropped copy       dev [T, copies] f32 out | NULL
+ * rows is needed (and read) for d_weight only; it may not be d_rows. */
+int pgmoe_combine_rows_backward(const void *d_y, int64_t d_y_stride, int d_y_dtype, int T, int d, const void *rows,
+                                int64_t rows_stride, int rows_dtype, int n_rows, const int32_t *row_of, int copies,
+                                const float *weight, void *d_rows, int64_t d_rows_stride, const pgmoe_fp8_rows *d_rows_q,
+                                float *d_weight, void *stream);
+/* Gradients d_h dev [rows, cols] of a ReLU's results, of which the codes were kept (what pgmoe_expert_matmul() writes with relu to
+ * y_q; their scales do not matter): d_pre = 0 where the kept value is zero or negative, also where d_h is not finite, and d_h elsewhere.
+ *   h_q dev, 16-byte aligned, rows h_q_stride bytes apart, a multiple of 16 from 128 * ceil(cols/128) on; h_dtype PGMOE_E4M3 or E5M2
+ *   d_pre dev [rows, cols] out | NULL; may be d_h itself if it has its type and stride    d_pre_q (rows x cols) | NULL: codes; one at least */
+int pgmoe_relu_backward(const void *d_h, int64_t d_h_stride, int d_h_dtype, int rows, int cols, const void *h_q,
+                        int64_t h_q_stride, int h_dtype, void *d_pre, int64_t d_pre_stride, int d_pre_dtype,
+                        const pgmoe_fp8_rows *d_pre_q, void *stream);
+/* Gradient of the experts' matrices, y = x . W, from rows kept in 8 bits: for every expert e and its rows [expert_offsets[e],
+ * expert_offsets[e+1]) of x and d_y
+ *   d_w[e] = add[e] + sum over the rows of (code * scale of x)^T . d_y         add[e], or 0, for an expert without rows
+ * on the matrix cores, sums in float32, rounded once.  Operands are bfloat16 pieces that add up to the values (but for a part in 2^32): one for codes whose scales are
+ * powers of two (x->dtype | PGMOE_SCALE_POW2: their exponents are taken, whatever else a scale holds), else three; one for gradients in PGMOE_BF16, two in
+ * F16, three in F32.  Products of pieces i and j are taken while i + j is below the larger count: 1 to 6 for each row, input and output.
+ *   x rows of n_in = x->cols columns, at most 2^24    d_y dev [x->rows, n_out], rows d_y_stride >= n_out elements apart
+ *   expert_offsets dev [n_experts+1]    d_w dev [n_experts, n_in, n_out] out    add: in d_w's type and layout | NULL; may be d_w itself
+ *   workspace dev, 16-byte aligned | NULL, workspace_bytes: where there are few matrices and many rows, these are split over workgroups that leave
+ * float32 partial sums in a workspace of pgmoe_expert_weight_gradient_workspace_bytes() (0: none is used); with less the call
+ * does without, slower and added up in another order.  Calls that may run at once, also as replayed graphs, need workspaces of their own. */
+int pgmoe_expert_weight_gradient(const pgmoe_fp8_rows *x, const void *d_y, int64_t d_y_stride, int d_y_dtype,
+                                 const int32_t *expert_offsets, int n_experts, int n_out, const void *add, void *d_w,
+                                 int d_w_dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t pgmoe_expert_weight_gradient_workspace_bytes(int rows, int n_experts, int n_in, int n_out);
 
 /* ---- observability: duration of the expert-FFN kernel ------------------------------------
  * pgmoe_ffn_timing_begin() makes every following pgmoe_expert_ffn() bracket its main kernel

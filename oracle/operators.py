@@ -1,5 +1,5 @@
-"""Plain 64-bit forms of routing from logits, its gradient, blocks of 8-bit floating point and the experts' products
-(test infrastructure only; numpy, written from the definitions in include/pgmoe.h)."""
+"""Plain 64-bit forms of routing from logits, its gradient, blocks of 8-bit floating point, the experts' products, rows there and
+back with weights, and the gradients of these (test infrastructure only; numpy, written from the definitions in include/pgmoe.h)."""
 from __future__ import annotations
 
 import numpy as np
@@ -114,11 +114,20 @@ def round_to(v, kind):
     return np.where(np.isinf(v), np.nan, out) if kind == "e4m3" else out
 
 
-def block_codes(x, kind):
+def least_power(amax, kind):
+    """The least power of two, at least 2^-126, by which amax is within the type."""
+    s = np.full(np.shape(amax), 2.0 ** -126)
+    for i, a in np.ndenumerate(np.asarray(amax, np.float64)):
+        while a > LARGEST[kind] * s[i]:
+            s[i] *= 2
+    return s.astype(np.float32)
+
+
+def block_codes(x, kind, pow2=False):
     """x [.., block]: float32 values of one block each -> (codes' values float64, scales float32 [..])."""
     x = np.asarray(x, np.float32)
     mag = np.where(np.isfinite(x), np.abs(x), np.float32(0)).max(axis=-1).astype(np.float32)
-    scale = np.maximum(mag / np.float32(LARGEST[kind]), np.float32(2.0 ** -126))
+    scale = least_power(mag, kind) if pow2 else np.maximum(mag / np.float32(LARGEST[kind]), np.float32(2.0 ** -126))
     with np.errstate(invalid="ignore"):
         return round_to(np.float64(x / scale[..., None]), kind), scale
 
@@ -129,11 +138,11 @@ def pad_to(a, n, axis):
     return np.pad(a, widths)
 
 
-def quantize_rows(x, kind):
+def quantize_rows(x, kind, pow2=False):
     """x [T, d] float32 -> (codes' values [T, 128 * blocks], scales [blocks, T])."""
     T, d = x.shape
     blocks = -(-d // BLOCK)
-    q, s = block_codes(pad_to(np.asarray(x, np.float32), blocks * BLOCK, 1).reshape(T, blocks, BLOCK), kind)
+    q, s = block_codes(pad_to(np.asarray(x, np.float32), blocks * BLOCK, 1).reshape(T, blocks, BLOCK), kind, pow2)
     return q.reshape(T, -1), s.T
 
 
@@ -167,3 +176,56 @@ def expert_matmul(x, x_scale, w, w_scale, offsets, relu=False):
         y[lo:hi] = xs[lo:hi] @ ws
         mag[lo:hi] = np.abs(xs[lo:hi]) @ np.abs(ws)
     return (np.where(y < 0, 0.0, y) if relu else y), mag
+
+
+# ------------------------------------------------------------------------------------ rows there and back
+def _entries(row_of, T, n_rows):
+    """(token, copy, row) of the entries that are not dropped."""
+    row_of = np.asarray(row_of).reshape(T, -1)
+    return [(t, j, row_of[t, j]) for t in range(T) for j in range(row_of.shape[1]) if 0 <= row_of[t, j] < n_rows]
+
+
+def dispatch_rows(x, row_of, n_rows, weight=None):
+    """x [T, d] -> rows [n_rows, d] float64; rows that no entry names are NaN."""
+    rows = np.full((n_rows, x.shape[1]), np.nan)
+    for t, j, r in _entries(row_of, len(x), n_rows):
+        rows[r] = x[t] if weight is None else np.float64(weight[t, j]) * x[t]
+    return rows
+
+
+def combine_rows(rows, row_of, T, weight=None, add=None):
+    """-> (y [T, d] float64, the sum of the magnitudes of its terms)."""
+    y = np.zeros((T, rows.shape[1])) if add is None else np.asarray(add, np.float64).copy()
+    mag = np.abs(y)
+    for t, j, r in _entries(row_of, T, len(rows)):
+        w = 1.0 if weight is None else np.float64(weight[t, j])
+        y[t] += w * rows[r]
+        mag[t] += np.abs(w * rows[r])
+    return y, mag
+
+
+def combine_weight_gradient(d_y, rows, row_of):
+    """-> (d_weight [T, copies], the sum of the magnitudes of its terms)."""
+    T = len(d_y)
+    d, mag = np.zeros(np.asarray(row_of).reshape(T, -1).shape), np.zeros(np.asarray(row_of).reshape(T, -1).shape)
+    for t, j, r in _entries(row_of, T, len(rows)):
+        d[t, j], mag[t, j] = (d_y[t] * rows[r]).sum(), np.abs(d_y[t] * rows[r]).sum()
+    return d, mag
+
+
+def relu_backward(d_h, h):
+    """h: the kept results' values."""
+    return np.where(h <= 0, 0.0, d_h)
+
+
+def expert_weight_gradient(x, x_scale, d_y, offsets, add=None):
+    """x [R, n_in] codes' values, x_scale [blocks, R], d_y [R, n_out] -> (d_w [E, n_in, n_out] float64, the sum of the magnitudes of its terms)."""
+    n_in, E = x.shape[1], len(offsets) - 1
+    xs = x * np.repeat(np.asarray(x_scale, np.float64).T, BLOCK, axis=1)[:, :n_in]
+    d_w = np.zeros((E, n_in, d_y.shape[1])) if add is None else np.asarray(add, np.float64).copy()
+    mag = np.abs(d_w)
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        d_w[e] += xs[lo:hi].T @ d_y[lo:hi]
+        mag[e] += np.abs(xs[lo:hi]).T @ np.abs(d_y[lo:hi])
+    return d_w, mag

@@ -18,6 +18,7 @@ F32, BF16, F16, E4M3, E5M2 = 0, 1, 2, 3, 4
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 MAX_GROUPS = 16
 FP8_BLOCK = 128
+SCALE_POW2 = 0x100
 STREAMS_COMPUTE_COPY, STREAMS_COMPUTE_OWN, STREAMS_COPY_OWN = 1, 2, 4
 FLAG_HOST_ONLY = 1
 FLAG_FETCH_MEMCPY = 2
@@ -38,6 +39,8 @@ EXPORTS = [
     "pgmoe_ffn_timing_begin", "pgmoe_ffn_timing_end", "pgmoe_slot_address", "pgmoe_fetch_timing", "pgmoe_trace", "pgmoe_get_block_trace", "pgmoe_fetch_all_experts", "pgmoe_set_schedule",
     "pgmoe_ffn_kernel_name", "pgmoe_set_nonmoe_standin", "pgmoe_check_streams", "pgmoe_expert_ffn_static", "pgmoe_migration_engine", "pgmoe_fetch_experts_as_turn",
     "pgmoe_route", "pgmoe_route_backward", "pgmoe_group_rows", "pgmoe_quantize_rows", "pgmoe_quantize_weights", "pgmoe_expert_matmul", "pgmoe_expert_matmul_kernel_name",
+    "pgmoe_dispatch_rows", "pgmoe_combine_rows", "pgmoe_combine_rows_backward", "pgmoe_relu_backward", "pgmoe_expert_weight_gradient",
+    "pgmoe_expert_weight_gradient_workspace_bytes",
 ]
 
 
@@ -140,9 +143,18 @@ def _load():
     L.pgmoe_expert_matmul.argtypes = [POINTER(FP8Rows), POINTER(FP8Weights), vp, i, vp, c_int64, i, POINTER(FP8Rows), vp]
     L.pgmoe_expert_matmul_kernel_name.argtypes = [POINTER(FP8Rows), POINTER(FP8Weights), i]
     L.pgmoe_expert_matmul_kernel_name.restype = c_char_p
+    rows8 = POINTER(FP8Rows)
+    L.pgmoe_dispatch_rows.argtypes = [vp, c_int64, i, i, i, vp, i, vp, vp, c_int64, i, i, rows8, vp]
+    L.pgmoe_combine_rows.argtypes = [vp, c_int64, i, i, vp, i, vp, vp, c_int64, i, i, vp, c_int64, i, vp]
+    L.pgmoe_combine_rows_backward.argtypes = [vp, c_int64, i, i, i, vp, c_int64, i, i, vp, i, vp, vp, c_int64, rows8, vp, vp]
+    L.pgmoe_relu_backward.argtypes = [vp, c_int64, i, i, i, vp, c_int64, i, vp, c_int64, i, rows8, vp]
+    L.pgmoe_expert_weight_gradient.argtypes = [rows8, vp, c_int64, i, vp, i, i, vp, vp, i, vp, c_size_t, vp]
+    L.pgmoe_expert_weight_gradient_workspace_bytes.argtypes = [i, i, i, i]
+    L.pgmoe_expert_weight_gradient_workspace_bytes.restype = c_size_t
     L.pgmoe_ffn_timing_end.argtypes = [vp, POINTER(c_int), POINTER(c_float), POINTER(c_float)]
     for name in EXPORTS:
-        if name not in ("pgmoe_last_error", "pgmoe_expert_bytes", "pgmoe_workspace_bytes", "pgmoe_ffn_kernel_name", "pgmoe_expert_matmul_kernel_name"):
+        if name not in ("pgmoe_last_error", "pgmoe_expert_bytes", "pgmoe_workspace_bytes", "pgmoe_ffn_kernel_name", "pgmoe_expert_matmul_kernel_name",
+                        "pgmoe_expert_weight_gradient_workspace_bytes"):
             getattr(L, name).restype = c_int
     return L
 
@@ -258,7 +270,7 @@ def _row_stride(t, name) -> int:
     if len(shape) != 2:
         raise ValueError(f"{name} has {len(shape)} dimensions, not 2")
     row, col = t.stride()
-    if col != 1 and shape[1] > 1:
+    if col != 1 and shape[1] > 1 and shape[0] > 0:
         raise ValueError(f"the elements of a row of {name} do not lie side by side")
     return row if shape[0] > 1 else max(row, shape[1])
 
@@ -267,8 +279,8 @@ def fp8_blocks(n: int) -> int:
     return (n + FP8_BLOCK - 1) // FP8_BLOCK
 
 
-def _fp8_rows(q, scale, cols, name) -> FP8Rows:
-    """q [rows, >= 128 * blocks] codes, scale [blocks, >= rows] float32."""
+def _fp8_rows(q, scale, cols, name, pow2=False) -> FP8Rows:
+    """q [rows, >= 128 * blocks] codes, scale [blocks, >= rows] float32; pow2: the scales are, or shall be, powers of two."""
     code = _DTYPES.get(q.dtype)
     if code != E4M3 and code != E5M2:
         raise TypeError(f"{name} has dtype {q.dtype}, not an 8-bit one")
@@ -277,7 +289,7 @@ def _fp8_rows(q, scale, cols, name) -> FP8Rows:
         raise ValueError(f"{name} has {width} columns, fewer than the {FP8_BLOCK * blocks} of whole blocks")
     if scale.shape != (blocks, rows) or scale.dtype != _f32:
         raise ValueError(f"{name}'s scale is {scale.dtype} {tuple(scale.shape)}, not float32 {(blocks, rows)}")
-    return FP8Rows(q.data_ptr(), stride, scale.data_ptr(), _row_stride(scale, "a scale"), rows, cols, code)
+    return FP8Rows(q.data_ptr(), stride, scale.data_ptr(), _row_stride(scale, "a scale"), rows, cols, code | SCALE_POW2 if pow2 else code)
 
 
 def fp8_weight_shapes(n_experts: int, n_in: int, n_out: int):
@@ -333,10 +345,10 @@ class Router:
             raise PgmoeError(rc, last_error())
 
 
-def quantize_rows(x, q, scale, row_of=None, copies=1, stream=None) -> None:
-    """x [T, cols] -> codes q [rows, 128 * blocks] and scales [blocks, rows]; row_of [T * copies] deals the rows out."""
+def quantize_rows(x, q, scale, row_of=None, copies=1, stream=None, pow2=False) -> None:
+    """x [T, cols] -> codes q [rows, 128 * blocks] and scales [blocks, rows], powers of two if asked for; row_of [T * copies] deals the rows out."""
     stride, (T, cols) = _row_stride(x, "x"), x.shape
-    out = _fp8_rows(q, scale, cols, "q")
+    out = _fp8_rows(q, scale, cols, "q", pow2)
     args = (x.data_ptr(), stride, _dtype(x, "x"), T, None if row_of is None else _expect(row_of, "row_of", (T * copies,), _i32), copies, byref(out))
     rc = lib.pgmoe_quantize_rows(*args, _stream_for(stream, x, q, scale, row_of))
     if rc:
@@ -358,13 +370,13 @@ def quantize_weights(w, forward_q, forward_scale, backward_q=None, backward_scal
         raise PgmoeError(rc, last_error())
 
 
-def expert_matmul(x_q, x_scale, w_q, w_scale, expert_offsets, n_in, n_out, y, y_scale=None, relu=False, stream=None) -> None:
-    """y[rows] = act(x[rows] . W_e) for the rows of every expert e; y [rows, n_out], or codes with y_scale."""
+def expert_matmul(x_q, x_scale, w_q, w_scale, expert_offsets, n_in, n_out, y, y_scale=None, relu=False, stream=None, pow2=False) -> None:
+    """y[rows] = act(x[rows] . W_e) for the rows of every expert e; y [rows, n_out], or codes with y_scale (pow2: powers of two)."""
     x = _fp8_rows(x_q, x_scale, n_in, "x_q")
     w = _fp8_weights(w_q, w_scale, n_in, n_out, "w_q")
     offsets = _expect(expert_offsets, "expert_offsets", (w.n_experts + 1,), _i32)
     if y_scale is not None:
-        out = _fp8_rows(y, y_scale, n_out, "y")
+        out = _fp8_rows(y, y_scale, n_out, "y", pow2)
         args = (None, 0, out.dtype, byref(out))
     else:
         if y.shape != (x.rows, n_out):
@@ -380,6 +392,115 @@ def expert_matmul_kernel_name(rows, n_experts, n_in, n_out, y_dtype=BF16, q_stri
     x = FP8Rows(None, q_stride or FP8_BLOCK * fp8_blocks(n_in), None, rows, rows, n_in, E4M3)
     name = lib.pgmoe_expert_matmul_kernel_name(byref(x), byref(FP8Weights(None, None, n_experts, n_in, n_out)), y_dtype)
     return name.decode() if name is not None else None
+
+
+# ---- training a block: rows there and back with weights, and the gradients
+def _entries(row_of, T, weight):
+    """row_of [T * copies] or [T, copies], weight [T, copies] -> (address of row_of, copies, address of weight)."""
+    n = row_of.numel()
+    copies = n // T if T else 1
+    if copies * T != n or (T and n == 0):
+        raise ValueError(f"row_of has {n} entries for {T} tokens")
+    return _expect(row_of, "row_of", row_of.shape, _i32), copies, None if weight is None else _expect(weight, "weight", (T, copies), _f32)
+
+
+def _values(t, name, rows, cols):
+    """The address, row stride and type of a matrix [rows, cols]; without one what a call takes for none."""
+    if t is None:
+        return None, 0, F32
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(rows, cols)}")
+    return t.data_ptr(), _row_stride(t, name), _dtype(t, name)
+
+
+def _codes_of(q, scale, rows, cols, name, pow2):
+    if q is None:
+        if scale is not None:
+            raise ValueError(f"a scale without {name}")
+        return None
+    if scale is None:
+        raise ValueError(f"{name} without its scale")
+    out = _fp8_rows(q, scale, cols, name, pow2)
+    if out.rows != rows:
+        raise ValueError(f"{name} has {out.rows} rows, not {rows}")
+    return byref(out)
+
+
+def dispatch_rows(x, row_of, rows=None, q=None, scale=None, weight=None, pow2=False, stream=None) -> None:
+    """rows[row_of[t, j]] = weight[t, j] * x[t], as values `rows` [R, d], as codes q with scales (powers of two with pow2), or both."""
+    T, d = x.shape
+    of, copies, w = _entries(row_of, T, weight)
+    if rows is None and q is None:
+        raise ValueError("both rows and q are None")
+    R = (q if rows is None else rows).shape[0]
+    args = (*_values(x, "x", T, d), T, d, of, copies, w, *_values(rows, "rows", R, d), R, _codes_of(q, scale, R, d, "q", pow2))
+    rc = lib.pgmoe_dispatch_rows(*args, _stream_for(stream, x, row_of, rows, q, scale, weight))
+    if rc:
+        raise PgmoeError(rc, last_error())
+
+
+def combine_rows(rows, row_of, y, weight=None, add=None, stream=None) -> None:
+    """y[t] = add[t] + sum over j of weight[t, j] * rows[row_of[t, j]]; without weights the gradient of dispatch_rows()."""
+    T, d = y.shape
+    of, copies, w = _entries(row_of, T, weight)
+    if add is not None and add.dtype != y.dtype:
+        raise TypeError(f"add has dtype {add.dtype}, y {y.dtype}")
+    args = (*_values(rows, "rows", rows.shape[0], d), rows.shape[0], of, copies, w, *_values(add, "add", T, d)[:2], T, d, *_values(y, "y", T, d))
+    rc = lib.pgmoe_combine_rows(*args, _stream_for(stream, y, row_of, rows, weight, add))
+    if rc:
+        raise PgmoeError(rc, last_error())
+
+
+def combine_rows_backward(d_y, rows, row_of, weight=None, d_rows=None, d_weight=None, q=None, scale=None, pow2=False, stream=None) -> None:
+    """Gradients of combine_rows(): d_rows[row_of[t, j]] = weight[t, j] * d_y[t], as values in the type of `rows`, as codes q, or both;
+    d_weight[t, j] = <d_y[t], rows[row_of[t, j]]>, for which alone `rows` is needed (else it may be None)."""
+    T, d = d_y.shape
+    of, copies, w = _entries(row_of, T, weight)
+    given = [t for t in (rows, d_rows, q) if t is not None]
+    if not given:
+        raise ValueError("rows, d_rows and q are None")
+    R = given[0].shape[0]
+    if rows is not None and d_rows is not None and rows.dtype != d_rows.dtype:
+        raise TypeError(f"d_rows has dtype {d_rows.dtype}, rows {rows.dtype}")
+    in_rows, out_rows = _values(rows, "rows", R, d), _values(d_rows, "d_rows", R, d)
+    args = (*_values(d_y, "d_y", T, d), T, d, *in_rows[:2], (out_rows if rows is None else in_rows)[2], R, of, copies, w, *out_rows[:2], _codes_of(q, scale, R, d, "q", pow2),
+            None if d_weight is None else _expect(d_weight, "d_weight", (T, copies), _f32))
+    rc = lib.pgmoe_combine_rows_backward(*args, _stream_for(stream, d_y, rows, row_of, weight, d_rows, d_weight, q, scale))
+    if rc:
+        raise PgmoeError(rc, last_error())
+
+
+def relu_backward(d_h, h_q, d_pre=None, q=None, scale=None, pow2=False, stream=None) -> None:
+    """d_pre = d_h where the codes h_q of a ReLU's results are above zero, else 0, as values (d_h itself may take them), as codes q, or both."""
+    R, n = d_h.shape
+    if h_q.shape[0] != R or h_q.shape[1] < FP8_BLOCK * fp8_blocks(n):
+        raise ValueError(f"h_q has shape {tuple(h_q.shape)}, not {(R, FP8_BLOCK * fp8_blocks(n))}")
+    code = _DTYPES.get(h_q.dtype)
+    if code != E4M3 and code != E5M2:
+        raise TypeError(f"h_q has dtype {h_q.dtype}, not an 8-bit one")
+    args = (*_values(d_h, "d_h", R, n), R, n, h_q.data_ptr(), _row_stride(h_q, "h_q"), code, *_values(d_pre, "d_pre", R, n), _codes_of(q, scale, R, n, "q", pow2))
+    rc = lib.pgmoe_relu_backward(*args, _stream_for(stream, d_h, h_q, d_pre, q, scale))
+    if rc:
+        raise PgmoeError(rc, last_error())
+
+
+def expert_weight_gradient_workspace_bytes(rows, n_experts, n_in, n_out) -> int:
+    return int(lib.pgmoe_expert_weight_gradient_workspace_bytes(rows, n_experts, n_in, n_out))
+
+
+def expert_weight_gradient(x_q, x_scale, d_y, expert_offsets, d_w, add=None, pow2=False, workspace=None, stream=None) -> None:
+    """d_w[e] = add[e] + (rows of expert e of x)^T . d_y, d_w [E, n_in, n_out], x in codes (pow2: their scales are powers of two, which they are not
+    asked about).  workspace: a contiguous tensor of expert_weight_gradient_workspace_bytes(); calls that may run at once need one each."""
+    E, n_in, n_out = d_w.shape
+    x = _fp8_rows(x_q, x_scale, n_in, "x_q", pow2)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace is not contiguous")
+    args = (byref(x), *_values(d_y, "d_y", x.rows, n_out), _expect(expert_offsets, "expert_offsets", (E + 1,), _i32), E, n_out,
+            None if add is None else _expect(add, "add", d_w.shape, d_w.dtype), _expect(d_w, "d_w", d_w.shape, d_w.dtype), _dtype(d_w, "d_w"),
+            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size())
+    rc = lib.pgmoe_expert_weight_gradient(*args, _stream_for(stream, d_w, x_q, x_scale, d_y, expert_offsets, add, workspace))
+    if rc:
+        raise PgmoeError(rc, last_error())
 
 
 class Context:

@@ -36,6 +36,7 @@ struct MatmulArgs {
     size_t y_q_stride;
     float *y_scale;
     size_t y_scale_stride;
+    bool y_pow2;  // y_scale's are powers of two
 };
 
 // The operand of a lane: 32 of the 128 inputs of row (or output) lane % 16.  Which ones a lane takes is free as long as both
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(FEW_THREADS) void matmul_few_rows_kernel(const Matm
             __syncthreads();
             amax = largest(finite_magnitude);
         }
-        const float scale = fp8_scale<YQ>(amax);
+        const float scale = fp8_scale<YQ>(amax, a.y_pow2);
         const Fp8CarefulDivisor by(scale);
         if (live) {
             *reinterpret_cast<uint32_t *>(a.y_q + (size_t)row * a.y_q_stride + o) = fp8_pack<YQ>(by(acc[0]), by(acc[1]), by(acc[2]), by(acc[3]));
@@ -695,7 +696,7 @@ __device__ inline int matmul_item(const MatmulArgs &a, const MatmulItems<R> &ite
         const int in_chunk = (wm + R::WM * m) * 16 + (lane & 15), row = it.row0 + in_chunk;
         const bool live = in_chunk < it.nrows;
         if constexpr (std::is_void<Y>::value) {
-            const float scale = fp8_scale<YQ>(amax[m]);
+            const float scale = fp8_scale<YQ>(amax[m], a.y_pow2);
             uint32_t codes[OT];
             auto quantise = [&](auto by) {
 #pragma unroll
@@ -904,14 +905,15 @@ extern "C" int pgmoe_expert_matmul(const pgmoe_fp8_rows *x, const pgmoe_fp8_weig
         a.y_q_stride = (size_t)y_q->q_stride;
         a.y_scale = y_q->scale;
         a.y_scale_stride = (size_t)y_q->scale_stride;
-        y_dtype = y_q->dtype;
+        a.y_pow2 = (y_q->dtype & PGMOE_SCALE_POW2) != 0;
+        y_dtype = fp8_type(y_q->dtype);
     }
-    rc = x->dtype == PGMOE_E4M3 ? launch_matmul<PGMOE_E4M3>(a, y_dtype, (hipStream_t)stream) : launch_matmul<PGMOE_E5M2>(a, y_dtype, (hipStream_t)stream);
+    rc = fp8_type(x->dtype) == PGMOE_E4M3 ? launch_matmul<PGMOE_E4M3>(a, y_dtype, (hipStream_t)stream) : launch_matmul<PGMOE_E5M2>(a, y_dtype, (hipStream_t)stream);
     return rc ? rc : launched(fn);
 }
 
 extern "C" const char *pgmoe_expert_matmul_kernel_name(const pgmoe_fp8_rows *x, const pgmoe_fp8_weights *w, int y_dtype) {
     if (!x || !w || x->rows < 1 || w->n_experts < 1 || w->n_in < 1 || w->n_out < 1) return nullptr;
-    const MatmulPlan p = matmul_plan(x->rows, w->n_experts, fp8_blocks(w->n_in), fp8_blocks(w->n_out), x->q_stride, y_dtype == PGMOE_E4M3 || y_dtype == PGMOE_E5M2);
+    const MatmulPlan p = matmul_plan(x->rows, w->n_experts, fp8_blocks(w->n_in), fp8_blocks(w->n_out), x->q_stride, fp8_type(y_dtype) == PGMOE_E4M3 || fp8_type(y_dtype) == PGMOE_E5M2);
     return p.tile == 64 ? "matmul_tiles_kernel, 64 rows" : p.tile == 256 ? "matmul_tiles_kernel, 256 rows" : "matmul_few_rows_kernel";
 }

@@ -41,9 +41,17 @@ struct Fp8CarefulDivisor {
         return fabsf(q) < INFINITY ? by(x * up) : q;
     }
 };
+// The least power of two, at least 2^-126, that is no less than amax / largest (amax: finite, not negative).  The largest values are
+// 1.75 * 2^8 and 1.75 * 2^15: of amax = m * 2^e that is 2^(e - 8) up to m = 1.75, and 2^(e - 7) beyond.
 template <int Q>
-__device__ inline float fp8_scale(float amax) {
-    return fmaxf(amax / fp8_largest<Q>, 0x1p-126f);
+__device__ inline float fp8_scale_pow2(float amax) {
+    const int bits = ((__float_as_int(amax) + 0x1fffff) & 0x7f800000) - ((Q == PGMOE_E4M3 ? 8 : 15) << 23);
+    return __int_as_float(max(bits, 0x00800000));
+}
+// The scale of a block of largest finite magnitude amax.
+template <int Q>
+__device__ inline float fp8_scale(float amax, bool pow2) {
+    return pow2 ? fp8_scale_pow2<Q>(amax) : fmaxf(amax / fp8_largest<Q>, 0x1p-126f);
 }
 // Is there a block among the wavefront's, of largest magnitude amax, that needs the careful form?
 template <int Q>
@@ -90,13 +98,14 @@ __device__ inline void load_eight(const L *p, int col, int cols, float (&v)[8]) 
 }
 
 // ---- argument checks
+inline int fp8_type(int dtype) { return dtype & ~PGMOE_SCALE_POW2; }  // of codes, whatever their scales are
 inline int check_float_type(int dtype, const char *fn, const char *what) {
     if (dtype == PGMOE_F32 || dtype == PGMOE_BF16 || dtype == PGMOE_F16) return PGMOE_OK;
     return fail(nullptr, PGMOE_EINVAL, "%s: %s=%d is neither f32 nor bf16 nor f16", fn, what, dtype);
 }
 inline int check_fp8_rows(const pgmoe_fp8_rows *r, const char *fn, const char *what) {
     if (!r) return fail(nullptr, PGMOE_EINVAL, "%s: %s is NULL", fn, what);
-    if (r->dtype != PGMOE_E4M3 && r->dtype != PGMOE_E5M2) return fail(nullptr, PGMOE_EINVAL, "%s: %s has dtype %d, neither e4m3 nor e5m2", fn, what, r->dtype);
+    if (fp8_type(r->dtype) != PGMOE_E4M3 && fp8_type(r->dtype) != PGMOE_E5M2) return fail(nullptr, PGMOE_EINVAL, "%s: %s has dtype %d, neither e4m3 nor e5m2", fn, what, r->dtype);
     if (r->rows < 0 || r->cols < 1 || r->cols > FP8_COLS_MAX)
         return fail(nullptr, PGMOE_EINVAL, "%s: %s has %d rows of %d columns: 0 and more of 1 to %d", fn, what, r->rows, r->cols, FP8_COLS_MAX);
     if (r->q_stride < (int64_t)FP8_BLOCK * fp8_blocks(r->cols) || r->q_stride % 16)

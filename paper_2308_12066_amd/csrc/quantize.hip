@@ -15,6 +15,7 @@ struct QuantizeRowsArgs {
     float *scale;
     size_t scale_stride;
     int rows;
+    bool pow2;
 };
 
 // Sixteen lanes take the 128 columns of one block, eight each; a workgroup takes the same block of 16 consecutive rows, whose
@@ -42,7 +43,7 @@ __global__ __launch_bounds__(QR_THREADS) void quantize_rows_kernel(const Quantiz
     float amax = largest([](float x) { return fabsf(x); });
     const bool unusual = fp8_unusual<Q>(amax);
     if (unusual) amax = largest(finite_magnitude);
-    const float scale = fp8_scale<Q>(amax);
+    const float scale = fp8_scale<Q>(amax, a.pow2);
     auto quantise = [&](auto by) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = by(v[j]);
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(QW_THREADS) void quantize_weights_kernel(const Quan
         __syncthreads();
         amax = largest(finite_magnitude);
     }
-    const float scale = fp8_scale<PGMOE_E4M3>(amax);
+    const float scale = fp8_scale<PGMOE_E4M3>(amax, false);
     auto quantise = [&](auto by) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -198,10 +199,11 @@ int pgmoe_quantize_rows(const void *x, int64_t x_stride, int x_dtype, int T, con
     NEED_PTR(nullptr, fn, x, dtype_bytes(x_dtype));
     OPT_PTR(nullptr, fn, row_of, 4);
     const QuantizeRowsArgs a = {x, (size_t)x_stride, T, out->cols, row_of, copies, (uint8_t *)out->q, (size_t)out->q_stride, out->scale,
-                                (size_t)out->scale_stride, out->rows};
-    if (x_dtype == PGMOE_F32) launch_quantize_rows<float>(a, out->dtype, (hipStream_t)stream);
-    else if (x_dtype == PGMOE_BF16) launch_quantize_rows<__bf16>(a, out->dtype, (hipStream_t)stream);
-    else launch_quantize_rows<_Float16>(a, out->dtype, (hipStream_t)stream);
+                                (size_t)out->scale_stride, out->rows, (out->dtype & PGMOE_SCALE_POW2) != 0};
+    const int q_dtype = fp8_type(out->dtype);
+    if (x_dtype == PGMOE_F32) launch_quantize_rows<float>(a, q_dtype, (hipStream_t)stream);
+    else if (x_dtype == PGMOE_BF16) launch_quantize_rows<__bf16>(a, q_dtype, (hipStream_t)stream);
+    else launch_quantize_rows<_Float16>(a, q_dtype, (hipStream_t)stream);
     return launched(fn);
 }
 

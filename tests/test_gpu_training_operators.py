@@ -1,0 +1,511 @@
+"""Rows there and back with weights, the way back through a ReLU kept in 8 bits, and the gradient of the experts' matrices, against
+their plain forms in 64 bits (oracle/operators.py).  H is half a step of float32 at 1, 2^-24; tolerances count roundings."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as O
+
+pytestmark = pytest.mark.gpu
+
+H = 2.0 ** -24
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}                                         # of the value
+TINY = {"f32": 2.0 ** -150, "bf16": 2.0 ** -134, "f16": 2.0 ** -25}                                      # half the least step
+DTYPES = ("f32", "bf16", "f16")
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2308_12066_amd import binding
+    return binding
+
+
+def dev(a, kind="f32"):
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda().to(TORCH[kind])
+
+
+def ints(a):
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float32 if t.element_size() == 1 else t.dtype).double().numpy()
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def near(got, want, err, kind):
+    """|got - want|: `err` before the last rounding, and that."""
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    with np.errstate(invalid="ignore"):
+        assert np.all(np.abs(got - want) <= err + HALF[kind] * (np.abs(want) + err) + TINY[kind]), np.nanmax(np.abs(got - want) - err - HALF[kind] * np.abs(want))
+
+
+def entries(g, T, k, dropped=0, spare=0):
+    """row_of [T * k] and the rows there are: some entries name no row, some rows have no entry."""
+    row_of = g.permutation(T * k + spare)[:T * k].astype(np.int32)
+    if dropped:
+        row_of[g.permutation(T * k)[:dropped]] = g.choice(np.array([-1, T * k + spare, -2 ** 31, 2 ** 31 - 1], np.int32), dropped)
+    return row_of, T * k + spare
+
+
+def check_codes(q, s, values, cols, kind, pow2, named=None):
+    """Codes and scales are a function of the float32 values: equal."""
+    want_q, want_s = O.quantize_rows(values.astype(np.float32), kind, pow2)
+    named = np.ones(len(values), bool) if named is None else named
+    got_q, got_s = f64(q), f64(s)
+    assert np.array_equal(got_q[named], want_q[named], equal_nan=True) and np.array_equal(got_s[:, named], want_s[:, named].astype(np.float64))
+    assert np.all(got_q[named][:, cols:] == 0)
+    assert np.all(got_q[~named] == 1) and np.all(got_s[:, ~named] == 7)
+
+
+def codes_for(rows, cols, kind):
+    nb = -(-cols // 128)
+    return torch.full((rows, nb * 128), 1.0, device="cuda").to(TORCH[kind]), torch.full((nb, rows), 7.0, device="cuda")
+
+
+SHAPES = [(1, 1, 1), (1, 2, 1024), (3, 2, 130), (7, 3, 516), (40, 8, 64), (17, 1, 4100), (300, 4, 520), (5, 300, 24), (1100, 1, 96)]
+
+
+# ------------------------------------------------------------------------------------ dispatch
+@pytest.mark.parametrize("T,k,d", SHAPES)
+@pytest.mark.parametrize("weighed", [False, True])
+def test_dispatch_rows(B, T, k, d, weighed):
+    say("dispatch", T, k, d, weighed)
+    g = np.random.default_rng(T + d + k)
+    for n, (x_kind, kind, q_kind, pow2) in enumerate((("bf16", "bf16", None, False), ("f32", "bf16", "e5m2", True), ("f16", "f32", "e4m3", False), ("bf16", None, "e4m3", True),
+                                                       ("f32", "f16", "e5m2", False), ("f32", "f32", None, False))):
+        row_of, R = entries(g, T, k, dropped=(T * k) // 5, spare=n % 3)
+        x = dev(g.standard_normal((T, d)) * np.exp(g.standard_normal((T, 1))), x_kind)
+        w = g.standard_normal((T, k)).astype(np.float32) if weighed else None
+        rows = torch.full((R, d), 7.0, device="cuda").to(TORCH[kind]) if kind else None
+        q, s = codes_for(R, d, q_kind) if q_kind else (None, None)
+        B.dispatch_rows(x, ints(row_of), rows, q, s, None if w is None else dev(w), pow2)
+        torch.cuda.synchronize()
+        want = O.dispatch_rows(f64(x), row_of, R, w)
+        named = ~np.isnan(want[:, 0])
+        if kind:
+            near(f64(rows)[named], want[named], H * np.abs(want[named]) + 2.0 ** -150, kind)
+            assert np.all(f64(rows)[~named] == 7)
+        if q_kind:  # the product in 64 bits, rounded to 32, is the float32 product
+            check_codes(q, s, np.nan_to_num(want), d, q_kind, pow2, named)
+
+
+def test_dispatch_of_values_that_are_not_finite(B):
+    """They stay in their columns, and a weight that is not finite leaves the codes past the last column zero."""
+    say("dispatch not finite")
+    d = 200
+    x = np.random.default_rng(1).standard_normal((6, d)).astype(np.float32)
+    x[0, 3], x[1, 130], x[2, :], x[3, 5] = np.inf, np.nan, 0.0, -np.inf
+    w = np.array([[1, 2], [1, 0], [np.inf, 1], [0, np.nan], [np.inf, 3], [1e-45, 1e38]], np.float32)
+    row_of = np.arange(12, dtype=np.int32)[::-1].copy()
+    rows = torch.zeros(12, d, device="cuda")
+    for kind in ("e4m3", "e5m2"):
+        for pow2 in (False, True):
+            q, s = codes_for(12, d, kind)
+            B.dispatch_rows(dev(x), ints(row_of), rows, q, s, dev(w), pow2)
+            torch.cuda.synchronize()
+            with np.errstate(all="ignore"):
+                want = np.zeros((12, d), np.float32)
+                want[row_of] = (np.float32(w)[:, :, None] * x[:, None]).reshape(12, d)
+                assert np.array_equal(f64(rows), want.astype(np.float64), equal_nan=True)
+                check_codes(q, s, want, d, kind, pow2)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("d", [1, 128, 300])
+def test_scales_that_are_powers_of_two(B, kind, d):
+    """quantize_rows and dispatch_rows give the same codes, those of the plain form: at the borders of a scale, for zeros, tiny and huge values."""
+    say("pow2", kind, d)
+    g = np.random.default_rng(d)
+    x = (g.standard_normal((64, d)) * np.exp2(g.integers(-140, 120, (64, 1)))).astype(np.float32)
+    top = np.float32(O.LARGEST[kind])
+    x[:8] = 0
+    x[1:8, 0] = [top, np.nextafter(top, np.float32(1e9)), np.nextafter(top, np.float32(0)), -top * 2, 1e-45, 2.0 ** -126, 3.3e38]
+    q, s = codes_for(64, d, kind)
+    B.quantize_rows(dev(x), q, s, pow2=True)
+    p, t = codes_for(64, d, kind)
+    B.dispatch_rows(dev(x), ints(np.arange(64)), None, p, t, pow2=True)
+    torch.cuda.synchronize()
+    check_codes(q, s, x, d, kind, True)
+    assert torch.equal(q.view(torch.uint8), p.view(torch.uint8)) and torch.equal(s, t)
+
+
+def test_expert_matmul_with_scales_that_are_powers_of_two(B):
+    """Quantised results of each of the product's kernels: codes times scales are the float32 results to half a step, every scale the least power for
+    the largest result, give or take a rounding of that."""
+    say("matmul pow2")
+    g = np.random.default_rng(8)
+    for counts, n_in, n_out in (([3, 0, 5], 200, 300), ([64] * 40, 200, 517), ([1500] * 40, 130, 520)):
+        E, R = len(counts), sum(counts)
+        names = {B.expert_matmul_kernel_name(R, E, n_in, n_out, B.E4M3)}
+        w = dev(0.05 * g.standard_normal((E, n_in, n_out)))
+        qs, ss = B.fp8_weight_shapes(E, n_in, n_out)
+        wq, ws = torch.zeros(qs, device="cuda").to(torch.float8_e4m3fn), torch.zeros(ss, device="cuda")
+        B.quantize_weights(w, wq, ws)
+        xq, xs = codes_for(R, n_in, "e4m3")
+        B.quantize_rows(dev(g.standard_normal((R, n_in))), xq, xs, pow2=True)
+        offs = ints(np.concatenate([[0], np.cumsum(counts)]))
+        y = torch.zeros(R, n_out, device="cuda")
+        B.expert_matmul(xq, xs, wq, ws, offs, n_in, n_out, y, relu=True)
+        for kind in ("e4m3", "e5m2"):
+            q, s = codes_for(R, n_out, kind)
+            B.expert_matmul(xq, xs, wq, ws, offs, n_in, n_out, q, s, relu=True, pow2=True)
+            torch.cuda.synchronize()
+            v, c, sc = f64(y), f64(q), f64(s)
+            assert np.all(np.frexp(sc)[0] == 0.5) and np.all(c[:, n_out:] == 0), names
+            half, least = (2.0 ** -4, 2.0 ** -10) if kind == "e4m3" else (2.0 ** -3, 2.0 ** -17)
+            for b in range(sc.shape[0]):
+                cols = slice(b * 128, min(n_out, b * 128 + 128))
+                amax = np.abs(v[:, cols]).max(1)
+                # the float32 results of both calls are sums in the same order or in another: each within n_in + 4 roundings of terms whose magnitudes sum to a few amax
+                slack = 1 + 64 * n_in * H
+                assert np.all(amax <= O.LARGEST[kind] * sc[b] * slack) and np.all((amax * slack > O.LARGEST[kind] * sc[b] / 2) | (sc[b] == 2.0 ** -126)), names
+                assert np.all(np.abs(c[:, cols] * sc[b][:, None] - v[:, cols]) <= np.maximum(half * np.abs(v[:, cols]), least * sc[b][:, None]) + 64 * n_in * H * amax[:, None]), names
+
+
+# ------------------------------------------------------------------------------------ combine
+@pytest.mark.parametrize("T,k,d", SHAPES)
+@pytest.mark.parametrize("weighed,added", [(False, False), (True, False), (True, True)])
+def test_combine_rows(B, T, k, d, weighed, added):
+    say("combine", T, k, d, weighed, added)
+    g = np.random.default_rng(T + d + k)
+    for n, (r_kind, kind) in enumerate((("bf16", "bf16"), ("f32", "f16"), ("f16", "f32"), ("bf16", "f32"))):
+        row_of, R = entries(g, T, k, dropped=(T * k) // 4, spare=n % 2)
+        rows = dev(g.standard_normal((R, d)), r_kind)
+        w = g.standard_normal((T, k)).astype(np.float32) if weighed else None
+        add = dev(g.standard_normal((T, d)), kind) if added else None
+        y = torch.full((T, d), 7.0, device="cuda").to(TORCH[kind])
+        B.combine_rows(rows, ints(row_of), y, None if w is None else dev(w), add)
+        torch.cuda.synchronize()
+        want, mag = O.combine_rows(f64(rows), row_of, T, w, None if add is None else f64(add))
+        near(y, want, (k + 1) * H * mag, kind)
+        if added:  # in place
+            B.combine_rows(rows, ints(row_of), add, None if w is None else dev(w), add)
+            torch.cuda.synchronize()
+            assert torch.equal(add, y)
+
+
+def test_combine_skips_dropped_copies_whatever_their_weights(B):
+    say("combine dropped")
+    rows = torch.full((4, 40), float("nan"), device="cuda")
+    rows[1] = 2.0
+    w = torch.tensor([[float("nan"), 3.0], [float("inf"), float("nan")]], device="cuda")
+    y = torch.full((2, 40), 7.0, device="cuda")
+    B.combine_rows(rows, ints([-1, 1, 4, 2 ** 31 - 1]), y, w)
+    torch.cuda.synchronize()
+    assert torch.all(y[0] == 6) and torch.all(y[1] == 0)
+    empty = torch.zeros(0, 40, device="cuda")
+    B.combine_rows(empty, ints([0, 1, 2, 3]), y, w, torch.ones_like(y))          # no rows at all
+    torch.cuda.synchronize()
+    assert torch.all(y == 1)
+
+
+# ------------------------------------------------------------------------------------ combine's gradient
+@pytest.mark.parametrize("T,k,d", SHAPES)
+@pytest.mark.parametrize("weighed", [False, True])
+def test_combine_rows_backward(B, T, k, d, weighed):
+    say("combine backward", T, k, d, weighed)
+    g = np.random.default_rng(T + d + k)
+    for n, (x_kind, kind, q_kind, values) in enumerate((("bf16", "bf16", None, True), ("f32", "bf16", "e5m2", True), ("f16", "f32", "e4m3", False), ("f32", "f16", None, False),
+                                                        ("bf16", "f32", "e5m2", True))):
+        row_of, R = entries(g, T, k, dropped=(T * k) // 5, spare=n % 3)
+        d_y, rows = dev(g.standard_normal((T, d)), x_kind), dev(g.standard_normal((R, d)), kind)
+        w = g.standard_normal((T, k)).astype(np.float32) if weighed else None
+        wt = None if w is None else dev(w)
+        d_rows = torch.full((R, d), 7.0, device="cuda").to(TORCH[kind]) if values else None
+        q, s = codes_for(R, d, q_kind) if q_kind else (None, None)
+        d_w = torch.full((T, k), 7.0, device="cuda")
+        B.combine_rows_backward(d_y, rows, ints(row_of), wt, d_rows, d_w, q, s, pow2=bool(n % 2))
+        torch.cuda.synchronize()
+        want = O.dispatch_rows(f64(d_y), row_of, R, w)
+        named = ~np.isnan(want[:, 0])
+        if values:
+            near(f64(d_rows)[named], want[named], H * np.abs(want[named]) + 2.0 ** -150, kind)
+            assert np.all(f64(d_rows)[~named] == 7)
+        if q_kind:
+            check_codes(q, s, np.nan_to_num(want), d, q_kind, bool(n % 2), named)
+        want_w, mag = O.combine_weight_gradient(f64(d_y), f64(rows), row_of)
+        # a lane's products one after the other, six sums over the lanes, three over the wavefronts
+        near(d_w, want_w, (8 * -(-d // 512) + 9) * H * mag + 2.0 ** -140, "f32")
+        if values:  # without the weights' gradient the rows are not asked for: same bits
+            again = torch.full_like(d_rows, 7.0)
+            B.combine_rows_backward(d_y, None, ints(row_of), wt, again)
+            torch.cuda.synchronize()
+            assert torch.equal(again, d_rows)
+
+
+def test_gradients_of_a_combine_are_those_of_differences_of_the_call(B):
+    """Combine is linear in rows and weights: a step of one value is off by roundings alone."""
+    say("combine differences")
+    g = np.random.default_rng(3)
+    T, k, d = 6, 3, 40
+    row_of, R = entries(g, T, k, dropped=3)
+    rows, w, c = g.standard_normal((R, d)).astype(np.float32), g.standard_normal((T, k)).astype(np.float32), g.standard_normal((T, d)).astype(np.float32)
+    d_rows, d_w = torch.zeros(R, d, device="cuda"), torch.zeros(T, k, device="cuda")
+    B.combine_rows_backward(dev(c), dev(rows), ints(row_of), dev(w), d_rows, d_w)
+
+    def loss(rows, w):
+        y = torch.zeros(T, d, device="cuda")
+        B.combine_rows(dev(rows), ints(row_of), y, dev(w))
+        torch.cuda.synchronize()
+        return (f64(y) * c).sum()
+    # values of order one: k + 1 roundings of each of T * d sums of k terms, over the step of 2
+    tol = (k + 1) * H * T * d * k * 8 / 2
+    for r, i in ((0, 0), (7, 39), (R - 1, 11)):
+        step = np.zeros_like(rows)
+        step[r, i] = 1
+        assert abs((loss(rows + step, w) - loss(rows - step, w)) / 2 - f64(d_rows)[r, i]) <= tol
+    for t, j in ((0, 0), (3, 2), (5, 1)):
+        step = np.zeros_like(w)
+        step[t, j] = 1
+        assert abs((loss(rows, w + step) - loss(rows, w - step)) / 2 - f64(d_w)[t, j]) <= tol
+
+
+def test_rows_there_and_back_is_the_transposed_map(B):
+    """<dispatch(x), g> = <x, combine(g)>, both with the same weights and dropped copies: the calls are each other's gradients."""
+    say("transposed")
+    g = np.random.default_rng(4)
+    T, k, d = 50, 3, 72
+    row_of, R = entries(g, T, k, dropped=20, spare=5)
+    x, r, w = g.standard_normal((T, d)), g.standard_normal((R, d)), g.standard_normal((T, k))
+    there, back = torch.zeros(R, d, device="cuda"), torch.zeros(T, d, device="cuda")
+    B.dispatch_rows(dev(x), ints(row_of), there, weight=dev(w))
+    B.combine_rows(dev(r), ints(row_of), back, dev(w))
+    torch.cuda.synchronize()
+    x, r = x.astype(np.float32).astype(np.float64), r.astype(np.float32).astype(np.float64)
+    mag = (np.abs(f64(there)) * np.abs(r)).sum()
+    assert abs((f64(there) * r).sum() - (x * f64(back)).sum()) <= (k + 3) * H * mag
+
+
+# ------------------------------------------------------------------------------------ through the ReLU
+@pytest.mark.parametrize("R,n", [(1, 1), (1, 4096), (3, 130), (17, 516), (130, 64), (40, 2050), (257, 384)])
+@pytest.mark.parametrize("h_kind", ["e4m3", "e5m2"])
+def test_relu_backward(B, R, n, h_kind):
+    say("relu", R, n, h_kind)
+    g = np.random.default_rng(R + n)
+    width = -(-n // 128) * 128
+    for x_kind, kind, q_kind, pow2 in (("f32", "bf16", "e5m2", True), ("bf16", "bf16", None, False), ("f16", None, "e4m3", False), ("bf16", "f32", "e5m2", False), ("f32", "f32", None, False),
+                                       ("f32", "f16", "e4m3", True)):
+        codes = torch.from_numpy(g.integers(0, 256, (R, width)).astype(np.uint8)).cuda().view(TORCH[h_kind])     # every code there is
+        d_h = dev(g.standard_normal((R, n)), x_kind)
+        blocked = (f64(codes)[:, :n] <= 0) & (g.random((R, n)) < 0.1)
+        d_h[torch.from_numpy(blocked).cuda()] = float("nan") if R % 2 else float("inf")
+        want = O.relu_backward(f64(d_h), f64(codes)[:, :n])
+        d_pre = torch.full((R, n), 7.0, device="cuda").to(TORCH[kind]) if kind else None
+        q, s = codes_for(R, n, q_kind) if q_kind else (None, None)
+        B.relu_backward(d_h, codes, d_pre, q, s, pow2)
+        torch.cuda.synchronize()
+        if kind:
+            near(d_pre, want, 0, kind)
+        if q_kind:
+            check_codes(q, s, want, n, q_kind, pow2)
+        if kind == x_kind:  # in place
+            B.relu_backward(d_h, codes, d_h)
+            torch.cuda.synchronize()
+            assert torch.equal(d_h, d_pre)
+
+
+# ------------------------------------------------------------------------------------ gradient of the matrices
+class Gradient:
+    def __init__(self, B, counts, n_in, n_out, x_kind="e4m3", y_kind="bf16", pow2=True, seed=0):
+        g = np.random.default_rng(seed + n_in + n_out + sum(counts))
+        self.B, self.n_in, self.n_out, self.pow2 = B, n_in, n_out, pow2
+        self.E, self.R = len(counts), int(sum(counts))
+        x = (g.standard_normal((self.R, n_in)) * np.exp(g.standard_normal((self.R, 1)))).astype(np.float32)
+        nb = -(-n_in // 128)
+        self.x, self.x_s = O.quantize_rows(x, x_kind, pow2) if self.R else (np.zeros((0, nb * 128)), np.zeros((nb, 0), np.float32))
+        self.offs = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        self.x_q, self.x_scale, self.offsets = dev(self.x, x_kind), dev(self.x_s), ints(self.offs)
+        self.d_y = dev(g.standard_normal((self.R, n_out)) * np.exp(g.standard_normal((self.R, 1))), y_kind)
+        self.terms = {(True, "bf16"): 1, (True, "f16"): 2, (True, "f32"): 3, (False, "bf16"): 3, (False, "f16"): 5, (False, "f32"): 6}[pow2, y_kind]
+        self.most = max(counts) if counts else 0
+
+    def run(self, out, add=None, stream=None, workspace=True):
+        d_w = torch.full((self.E, self.n_in, self.n_out), 7.0, device="cuda").to(TORCH[out])
+        need = self.B.expert_weight_gradient_workspace_bytes(self.R, self.E, self.n_in, self.n_out)
+        ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda") if need and workspace else None
+        self.B.expert_weight_gradient(self.x_q, self.x_scale, self.d_y, self.offsets, d_w, add, self.pow2, ws, stream)
+        torch.cuda.synchronize()
+        return d_w
+
+    def check(self, out="f32", add=None, workspace=True):
+        want, mag = O.expert_weight_gradient(self.x[:, :self.n_in], self.x_s, f64(self.d_y), self.offs, None if add is None else f64(add))
+        got = self.run(out, add, workspace=workspace)
+        # a product goes through at most one rounding a term of the sum, and there are `terms` for each row; parts of a sum and `add` are one more each.  Code times scale is
+        # rounded once.  Pieces are cut off after 8 bits: the second is below 2^-7 of the value, the third below 2^-14, the three are the value but for 2^-32.  Left out are
+        # second times third both ways and third times third: below 2 * 2^-21 + 2^-28 of the product, 17 H
+        near(got, want, (self.terms * self.most + 16 + 1 + (17 if self.terms > 4 else 1)) * H * mag, out)
+        return got
+
+
+COUNTS = [[1], [0, 1, 0], [2, 0, 3], [0, 0, 0], [31, 0, 32, 33], [64, 65, 0, 63], [130, 1, 0, 257], [1] * 40, [600]]
+
+
+@pytest.mark.parametrize("counts", COUNTS, ids=lambda c: "x".join(map(str, c[:6])))
+@pytest.mark.parametrize("n_in,n_out", [(128, 128), (1, 1), (200, 300), (384, 517), (136, 264)])
+def test_expert_weight_gradient(B, counts, n_in, n_out):
+    say("gradient", counts[:6], n_in, n_out)
+    for i, (pow2, y_kind) in enumerate([(p, y) for p in (True, False) for y in DTYPES]):
+        p = Gradient(B, counts, n_in, n_out, "e5m2" if i % 2 else "e4m3", y_kind, pow2)
+        for out in DTYPES if y_kind == "bf16" else ("f32",):
+            p.check(out)
+
+
+@pytest.mark.parametrize("counts,n_in,n_out,y_kind,pow2", [([700, 300], 1024, 640, "bf16", True), ([90] * 20, 768, 512, "bf16", True), ([4, 2, 0, 7] * 16, 512, 264, "f32", False),
+                                                           ([2000, 0, 9], 256, 256, "bf16", True), ([1500], 300, 520, "f16", False), ([40] * 8, 512, 1024, "f16", True)])
+def test_expert_weight_gradient_of_ordinary_sizes(B, counts, n_in, n_out, y_kind, pow2):
+    say("gradient", counts[:6], n_in, n_out, y_kind, pow2)
+    p = Gradient(B, counts, n_in, n_out, "e4m3", y_kind, pow2)
+    p.check("f32")
+    p.check("bf16")
+
+
+@pytest.mark.parametrize("out", DTYPES)
+@pytest.mark.parametrize("n_in,n_out", [(200, 136), (130, 77)])
+def test_expert_weight_gradient_is_added(B, out, n_in, n_out):
+    """To another tensor and in place; an expert without rows gives what is added."""
+    say("gradient added", out, n_in, n_out)
+    p = Gradient(B, [40, 0, 70], n_in, n_out)
+    add = dev(np.random.default_rng(1).standard_normal((3, n_in, n_out)), out)
+    got = p.check(out, add)
+    assert torch.equal(got[1], add[1])
+    ws = p.B.expert_weight_gradient_workspace_bytes(p.R, p.E, n_in, n_out)
+    p.B.expert_weight_gradient(p.x_q, p.x_scale, p.d_y, p.offsets, add, add, True, torch.zeros(ws, dtype=torch.uint8, device="cuda") if ws else None)
+    torch.cuda.synchronize()
+    assert torch.equal(got, add)
+
+
+def test_expert_weight_gradient_of_operands_with_strides(B):
+    """Rows inside wider buffers, at addresses that wide loads do not reach, neighbours that are not finite, on another stream."""
+    say("gradient strides")
+    p = Gradient(B, [20, 0, 45, 130], 200, 136)
+    want, mag = O.expert_weight_gradient(p.x[:, :200], p.x_s, f64(p.d_y), p.offs)
+    wide = torch.full((p.R, 384 + 16), float("nan"), device="cuda").to(torch.float8_e4m3fn)
+    wide[:, 16:16 + 256] = p.x_q
+    p.x_q = wide[:, 16:16 + 256]
+    scale = torch.full((2, p.R + 9), float("nan"), device="cuda")
+    scale[:, 4:4 + p.R] = p.x_scale
+    p.x_scale = scale[:, 4:4 + p.R]
+    stream = torch.cuda.Stream()
+    for at, width in ((8, 160), (3, 151)):
+        d_y = torch.full((p.R, width), float("nan"), device="cuda").to(torch.bfloat16)
+        d_y[:, at:at + 136] = p.d_y
+        kept, p.d_y = p.d_y, d_y[:, at:at + 136]
+        torch.cuda.synchronize()
+        near(p.run("f32", stream=stream), want, (130 + 20) * H * mag, "f32")
+        p.d_y = kept
+
+
+def test_expert_weight_gradient_of_offsets_that_are_none(B):
+    """Offsets outside the rows, or that fall, are taken as far as there are rows."""
+    say("gradient offsets")
+    p = Gradient(B, [50, 50], 130, 140)
+    for offs in ([-5, 40, 2000], [60, 30, 90], [100, 100, 100], [-2 ** 31, 0, 2 ** 31 - 1]):
+        p.offsets = ints(offs)
+        got = p.run("f32")
+        for e in range(2):
+            lo = max(0, min(offs[e], p.R))
+            hi = max(lo, min(offs[e + 1], p.R))
+            want, mag = O.expert_weight_gradient(p.x[lo:hi, :130], p.x_s[:, lo:hi], f64(p.d_y)[lo:hi], [0, hi - lo])
+            near(got[e:e + 1], want, (hi - lo + 20) * H * mag, "f32")
+
+
+@pytest.mark.parametrize("pow2,y_kind", [(True, "bf16"), (True, "f16"), (True, "f32"), (False, "bf16"), (False, "f32")])
+def test_expert_weight_gradient_passes_on_what_is_not_finite(B, pow2, y_kind):
+    """To the row and column of the product it is in, and to no other expert: not from the rows behind an expert's last, which end in the middle of what is
+    multiplied at once."""
+    say("gradient not finite", pow2, y_kind)
+    p = Gradient(B, [37, 20, 3], 136, 144, "e5m2", y_kind, pow2)
+    finite = p.run("f32")
+    d_y, x = p.d_y.clone(), p.x_q.clone()
+    p.d_y[40, 7] = float("nan")            # expert 1
+    p.d_y[57, 100] = float("inf")          # expert 2
+    got = p.run("f32")
+    assert torch.equal(got[0], finite[0])
+    assert torch.isnan(got[1][:, 7]).all()
+    keep = torch.ones(144, dtype=torch.bool, device="cuda")
+    keep[7] = False
+    assert torch.equal(got[1][:, keep], finite[1][:, keep])
+    keep[7], keep[100] = True, False
+    assert torch.equal(got[2][:, keep], finite[2][:, keep])
+    xv = torch.from_numpy(p.x[57, :136]).cuda()
+    assert torch.equal(got[2][:, 100] == float("inf"), xv > 0) and torch.equal(got[2][:, 100] == -float("inf"), xv < 0)
+    p.d_y = d_y
+    x[2, 5], x[59, 130] = float("nan"), float("-inf")
+    p.x_q = x
+    got = p.run("f32")
+    assert torch.isnan(got[0][5]).all() and torch.equal(got[1], finite[1])
+    rows = torch.arange(136, device="cuda")
+    assert torch.equal(got[0][rows != 5], finite[0][rows != 5]) and torch.equal(got[2][rows != 130], finite[2][rows != 130])
+    last = p.d_y[59].float()
+    assert torch.equal(got[2][130] == -float("inf"), last > 0) and torch.equal(got[2][130] == float("inf"), last < 0)
+
+
+def test_expert_weight_gradient_is_that_of_differences_of_the_product(B):
+    """The loss <x . W, c> of expert_matmul is linear in W: for a W of one code the product is that entry's column of x times it."""
+    say("gradient differences")
+    g = np.random.default_rng(6)
+    counts, n_in, n_out = [9, 0, 50], 200, 140
+    E, R = len(counts), sum(counts)
+    offs = ints(np.concatenate([[0], np.cumsum(counts)]))
+    xq, xs = codes_for(R, n_in, "e4m3")
+    B.quantize_rows(dev(g.standard_normal((R, n_in))), xq, xs, pow2=True)
+    c = dev(g.standard_normal((R, n_out)), "bf16")
+    d_w = torch.zeros(E, n_in, n_out, device="cuda")
+    B.expert_weight_gradient(xq, xs, c, offs, d_w, pow2=True)
+    qs, ss = B.fp8_weight_shapes(E, n_in, n_out)
+    for e, i, o in ((0, 0, 0), (2, 150, 139), (2, 199, 64), (1, 3, 3)):
+        w = torch.zeros(E, n_in, n_out, device="cuda")
+        w[e, i, o] = 448.0
+        wq, ws = torch.zeros(qs, device="cuda").to(torch.float8_e4m3fn), torch.zeros(ss, device="cuda")
+        B.quantize_weights(w, wq, ws)
+        y = torch.zeros(R, n_out, device="cuda")
+        B.expert_matmul(xq, xs, wq, ws, offs, n_in, n_out, y)
+        torch.cuda.synchronize()
+        terms = f64(y) * f64(c) / 448
+        assert abs(terms.sum() - f64(d_w)[e, i, o]) <= (50 + 20) * H * np.abs(terms).sum()
+
+
+def test_expert_weight_gradient_with_offsets_that_pass_32_bits(B):
+    """Rows of gradients and codes, and results, beyond the first 4 GiB of their buffers."""
+    say("gradient 32 bits")
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of memory")
+    R, E, n_in, n_out = 300, 3, 130, 136
+    p = Gradient(B, [100, 50, 150], n_in, n_out)
+    d_y = torch.empty(R * (1 << 23), dtype=torch.bfloat16, device="cuda").as_strided((R, n_out), (1 << 23, 1))      # 5 GB
+    d_y.copy_(p.d_y)
+    x = torch.empty(R * (1 << 24), dtype=torch.uint8, device="cuda").as_strided((R, 256), (1 << 24, 1)).view(torch.float8_e4m3fn)  # 5 GB
+    x.view(torch.uint8).copy_(p.x_q.view(torch.uint8))
+    want = p.run("f32")
+    p.d_y, p.x_q = d_y, x
+    assert torch.equal(p.run("f32"), want)
+    del d_y, x
+    p = Gradient(B, [1, 2] + [0] * 248 + [3], 4096, 4104)       # 4.2 G results
+    got = p.run("bf16")
+    last, mag = O.expert_weight_gradient(p.x[3:, :4096], p.x_s[:, 3:], f64(p.d_y)[3:], [0, 3])
+    near(got[250:], last, 23 * H * mag, "bf16")
+    assert not got[249].any() and not got[100].any()
+
+
+def test_dispatch_and_combine_with_offsets_that_pass_32_bits(B):
+    say("rows 32 bits")
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of memory")
+    T, d = 300, 136
+    g = np.random.default_rng(2)
+    x = dev(g.standard_normal((T, d)), "bf16")
+    rows = torch.empty(T * (1 << 23), dtype=torch.bfloat16, device="cuda").as_strided((T, d), (1 << 23, 1))
+    row_of = g.permutation(T).astype(np.int32)
+    B.dispatch_rows(x, ints(row_of), rows)
+    y, d_w = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, 1, device="cuda")
+    B.combine_rows(rows, ints(row_of), y)
+    B.combine_rows_backward(x, rows, ints(row_of), None, None, d_w)
+    torch.cuda.synchronize()
+    assert torch.equal(y, x)
+    xs = f64(x)
+    near(d_w[:, 0], (xs * xs).sum(1), 17 * H * (xs * xs).sum(1), "f32")
