@@ -5,6 +5,7 @@
 // The scales of x vary along the sum, so they cannot be taken out of it: the matrix cores' operand is code times scale.  Where scales are
 // powers of two that is a bfloat16 as it stands (four bits), and one product a row, input and output is exact.  Otherwise code times scale in 32
 // bits is taken apart into three bfloat16 whose sum it is, and so are gradients of 32 bits; those of 16-bit floating point are the sum of two.
+#include <algorithm>
 #include <atomic>
 
 #include "ffn_common.h"
@@ -24,8 +25,12 @@ struct GradientArgs {
     const void *add;  // | nullptr
     void *d_w;
     int dtype;  // of d_w and add
-    int tiles_in, tiles_out;
+    int parts;  // an expert's rows are split into: each writes a float32 plane of its own to d_w, [parts][E][n_in][n_out]
+    int tiles_in, tiles_out, group_in, group_out;
 };
+
+// The steps of part `part` of an expert's `steps`: none for some parts if there are few.
+__host__ __device__ inline int first_step(int steps, int part, int parts) { return (int)((int64_t)steps * part / parts); }
 
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
@@ -36,15 +41,15 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 // PIECES bfloat16 whose sum is v but for a part in 2^32 (of two: 16 bits, of three: 24).  All have v's sign and none is zero if v is not, so
 // that an infinity times each of them is the infinity that it times v is: pieces are cut off, not rounded, and what is left of v is
 // raised by that part.  (Products of pieces that are left out are below 2^-20 of the first, on the mean 2^-23.)
-__device__ inline uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
+__device__ inline int high_halves(float a, float b) { return (int)__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
 template <int PIECES>
-__device__ inline void take_apart(const float (&v)[8], uint4 (&to)[PIECES]) {
+__device__ inline void take_apart(const float (&v)[8], intx4 (&to)[PIECES]) {
     float rest[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) rest[j] = __builtin_canonicalizef(v[j]);  // NaN: with a bit that is not cut off
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-        to[p] = make_uint4(high_halves(rest[0], rest[1]), high_halves(rest[2], rest[3]), high_halves(rest[4], rest[5]), high_halves(rest[6], rest[7]));
+        to[p] = intx4{high_halves(rest[0], rest[1]), high_halves(rest[2], rest[3]), high_halves(rest[4], rest[5]), high_halves(rest[6], rest[7])};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float left = fmaf(v[j], 0x1p-32f, rest[j] - __uint_as_float(__float_as_uint(rest[j]) & 0xffff0000u));
@@ -55,18 +60,18 @@ __device__ inline void take_apart(const float (&v)[8], uint4 (&to)[PIECES]) {
 
 // Eight codes times their scale.
 template <int Q, int PIECES>
-__device__ inline void open_codes(intx2 codes, float scale, uint4 (&to)[PIECES]) {
+__device__ inline void open_codes(intx2 codes, float scale, intx4 (&to)[PIECES]) {
     if constexpr (PIECES == 1) {  // the conversion takes the scale's exponent
-        uint32_t pairs[4];
+        int pairs[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             bf16x2 pair;
             if constexpr (Q == PGMOE_E4M3)
                 pair = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j >> 1], scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j >> 1], scale, false);
             else pair = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(codes[j >> 1], scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(codes[j >> 1], scale, false);
-            pairs[j] = __builtin_bit_cast(uint32_t, pair);
+            pairs[j] = __builtin_bit_cast(int, pair);
         }
-        to[0] = make_uint4(pairs[0], pairs[1], pairs[2], pairs[3]);
+        to[0] = intx4{pairs[0], pairs[1], pairs[2], pairs[3]};
     } else {
         float v[8];
 #pragma unroll
@@ -98,172 +103,411 @@ __device__ inline bf16x8 operand_of(const char *tile, int stride, int lane) {
 template <typename Y>
 constexpr int pieces_of = sizeof(Y) == 4 ? 3 : std::is_same<Y, __bf16>::value ? 1 : 2;
 
-// A workgroup takes 128 inputs by 128 outputs of one expert and goes through its rows 32 at a time: both sides come through registers, where codes are
-// converted, into one of two buffers in LDS while the other is multiplied.  Rows in LDS have 32 bytes more behind them than their 128 columns: the eight rows of 32
-// bytes that half a wavefront reads at once then lie in different banks.
-constexpr int WG_TILE = 128, WG_K = 32, WG_THREADS = 256, WG_STRIDE = 2 * WG_TILE + 32, WG_PLANE = WG_K * WG_STRIDE;
-template <int XQ, typename Y, int PX, bool VEC>
-__global__ __launch_bounds__(WG_THREADS) void weight_gradient_kernel(const GradientArgs a) {
-    constexpr int PY = pieces_of<Y>, BUFFER = (PX + PY) * WG_PLANE, KEPT = PX > PY ? PX : PY;  // KEPT: pieces i and j are multiplied where i + j < KEPT
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int e = blockIdx.x / (a.tiles_in * a.tiles_out), tile = blockIdx.x - e * a.tiles_in * a.tiles_out, ti = tile / a.tiles_out, to = tile - ti * a.tiles_out;
-    const int lo = max(0, min(a.offsets[e], a.rows)), hi = max(lo, min(a.offsets[e + 1], a.rows)), steps = (hi - lo + WG_K - 1) / WG_K;
-
-    // what a thread brings: eight columns of rows threadIdx.x / 16 and 16 + threadIdx.x / 16 of a step
-    const int piece = threadIdx.x & 15, row = threadIdx.x >> 4;
-    const uint8_t *x = a.x + (size_t)ti * WG_TILE + piece * 8;
-    const float *x_scale = a.x_scale + (size_t)ti * a.x_scale_stride;
-    const int col = min(to * WG_TILE + piece * 8, VEC ? a.n_out - 8 : a.n_out - 1);  // columns past the last are there, but nobody's
-    const Y *d_y = reinterpret_cast<const Y *>(a.d_y);
-    intx2 codes[2];
-    float scale[2];
-    struct { Y v[8]; } grad[2];
-    bool there[2];
-    auto request = [&](int step) {
+// Results of a wavefront's NI x 4 tiles from input `in` and output `out` on.  Gradients were the first operand: a lane's four results of a product are neighbouring
+// outputs of one input.  They leave in whole lines, past the caches, which then keep the rows: 128 bytes of each of eight inputs at once (16 bytes a lane in 64 bytes of
+// each of 16 inputs: 1024 x 4096 float32 for each of 64 experts from 32768 rows 503 us, whole lines 460).  VEC: 16 bytes of results are all there or none.
+template <typename W, int NI>
+__device__ inline void store_lines(const GradientArgs &a, int e, int in, int out, int lane, floatx4 (&acc)[NI][4]) {
+    constexpr int UNITS = sizeof(W) == 4 ? 4 : 2;  // of 64 bytes a row: a tile, or two
+    typedef W Wx4 __attribute__((ext_vector_type(4)));
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));  // worked out again: what depends on it is not kept in registers across the products
+    const bool up = lane & 8;
+    const int g = lane >> 4;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = lo + step * WG_K + i * 16 + row;
-            there[i] = r < hi;
-            const size_t at = there[i] ? r : hi - 1;
-            codes[i] = *reinterpret_cast<const intx2 *>(x + at * a.x_stride);
-            scale[i] = x_scale[at];
-            const Y *g = d_y + at * a.d_y_stride;
-            if constexpr (VEC) {
-                typedef Y Yx8 __attribute__((ext_vector_type(8), aligned(16)));
-                *reinterpret_cast<Yx8 *>(grad[i].v) = *reinterpret_cast<const Yx8 *>(g + col);
-            } else {
+    for (int i = 0; i < NI; ++i) {
+        intx4 unit[UNITS];
+        if constexpr (sizeof(W) == 4) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) grad[i].v[j] = g[min(col + j, a.n_out - 1)];
-            }
-        }
-    };
-    auto keep = [&](char *to) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            char *at = to + (i * 16 + row) * WG_STRIDE + piece * 16;
-            const uint4 none = make_uint4(0, 0, 0, 0);
-            uint4 px[PX], py[PY];
-            open_codes<XQ, PX>(codes[i], scale[i], px);
-            if constexpr (PY == 1) {
-                py[0] = __builtin_bit_cast(uint4, grad[i]);
-            } else {
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (float)grad[i].v[j];
-                take_apart<PY>(v, py);
-            }
-            // rows behind the last are zero on both sides, whatever the last one holds
-#pragma unroll
-            for (int p = 0; p < PX; ++p) *reinterpret_cast<uint4 *>(at + p * WG_PLANE) = there[i] ? px[p] : none;
-#pragma unroll
-            for (int p = 0; p < PY; ++p) *reinterpret_cast<uint4 *>(at + (PX + p) * WG_PLANE) = there[i] ? py[p] : none;
-        }
-    };
-
-    // wavefronts as 2 x 2, each with 64 inputs and 64 outputs.  Gradients are the first operand: a lane's four results of a product are neighbouring outputs of one input.
-    const int wi = wave >> 1, wo = wave & 1;
-    floatx4 acc[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int o = 0; o < 4; ++o) acc[i][o] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (steps > 0) {
-        request(0);
-        keep(lds);
-    }
-    for (int step = 0; step < steps; ++step) {
-        lds_barrier();  // this step's rows are there for everyone, and everyone has read the one before
-        const bool more = step + 1 < steps;
-        if (more) request(step + 1);
-        __builtin_amdgcn_sched_barrier(0);
-        const char *now = lds + (step & 1) * BUFFER;
-        bf16x8 px[4][PX];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int p = 0; p < PX; ++p) px[i][p] = operand_of(now + p * WG_PLANE + (wi * 64 + i * 16) * 2, WG_STRIDE, lane);
-#pragma unroll
-        for (int o = 0; o < 4; ++o) {
-            bf16x8 py[PY];
-#pragma unroll
-            for (int p = 0; p < PY; ++p) py[p] = operand_of(now + (PX + p) * WG_PLANE + (wo * 64 + o * 16) * 2, WG_STRIDE, lane);
-            // small products first
-#pragma unroll
-            for (int s = KEPT - 1; s >= 0; --s)
-#pragma unroll
-                for (int p = 0; p < PY; ++p)
-                    if (s - p >= 0 && s - p < PX) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(py[p], px[i][s - p >= 0 && s - p < PX ? s - p : 0], acc[i][o], 0, 0, 0);
-                    }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (more) keep(lds + ((step + 1) & 1) * BUFFER);
-    }
-
-    auto finish = [&](auto type) {
-        using W = decltype(type);
-        typedef W Wx4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int in = ti * WG_TILE + wi * 64 + i * 16 + (lane & 15);
-            if (in >= a.n_in) continue;
-            const size_t first = ((size_t)e * a.n_in + in) * a.n_out;
+            for (int o = 0; o < 4; ++o) unit[o] = __builtin_bit_cast(intx4, acc[i][o]);
+        } else {
+            const int row = in + i * 16 + (lane & 15);
 #pragma unroll
             for (int o = 0; o < 4; ++o) {
-                const int out = to * WG_TILE + wo * 64 + o * 16 + 4 * (lane >> 4);
-                W *p = reinterpret_cast<W *>(a.d_w) + first + out;
-                const W *q = reinterpret_cast<const W *>(a.add) + first + out;
-                floatx4 v = acc[i][o];
-                if (VEC) {
-                    if (out >= a.n_out) continue;
-                    if (a.add) {
-                        const Wx4 u = *reinterpret_cast<const Wx4 *>(q);
+                const int col = out + o * 16 + 4 * g;
+                if (a.add && row < a.n_in && col < a.n_out) {
+                    const Wx4 u = *reinterpret_cast<const Wx4 *>(reinterpret_cast<const W *>(a.add) + ((size_t)e * a.n_in + row) * a.n_out + col);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] += (float)u[j];
-                    }
-                    *reinterpret_cast<Wx4 *>(p) = Wx4{(W)v[0], (W)v[1], (W)v[2], (W)v[3]};
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (out + j < a.n_out) p[j] = (W)(a.add ? v[j] + (float)q[j] : v[j]);
+                    for (int j = 0; j < 4; ++j) acc[i][o][j] += (float)u[j];
                 }
             }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {  // odd and even quarters of the wavefront swap two tiles' halves: a lane then has eight neighbours
+                const intx2 p = __builtin_bit_cast(intx2, Wx4{(W)acc[i][2 * u][0], (W)acc[i][2 * u][1], (W)acc[i][2 * u][2], (W)acc[i][2 * u][3]});
+                const intx2 q = __builtin_bit_cast(intx2, Wx4{(W)acc[i][2 * u + 1][0], (W)acc[i][2 * u + 1][1], (W)acc[i][2 * u + 1][2], (W)acc[i][2 * u + 1][3]});
+                const auto x = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), y = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
+                unit[u] = intx4{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
+            }
         }
+#pragma unroll
+        for (int u = 0; u < UNITS; u += 2) {  // the upper eight inputs of a unit for the lower eight of the next
+            intx4 low, high;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int got = __builtin_amdgcn_update_dpp(0, up ? unit[u][j] : unit[u + 1][j], 0x128, 0xf, 0xf, true);  // row_ror:8
+                low[j] = up ? got : unit[u][j];
+                high[j] = up ? unit[u + 1][j] : got;
+            }
+            const int col = out + (sizeof(W) == 4 ? (u + (up ? 1 : 0)) * 16 + 4 * g : (u + (up ? 1 : 0)) * 32 + (g & 1) * 16 + (g >> 1) * 8);
+            const int row = in + i * 16 + (lane & 7);
+            const size_t at = ((size_t)e * a.n_in + row) * a.n_out + col;
+            auto put = [&](intx4 v, int r, size_t at) {
+                if (r >= a.n_in || col >= a.n_out) return;
+                if constexpr (sizeof(W) == 4)
+                    if (a.add) v = __builtin_bit_cast(intx4, __builtin_bit_cast(floatx4, v) + *reinterpret_cast<const floatx4 *>(reinterpret_cast<const float *>(a.add) + at));
+                intx4 *to = reinterpret_cast<intx4 *>(reinterpret_cast<W *>(a.d_w) + at);
+                if (a.parts == 1) __builtin_nontemporal_store(v, to);
+                else *to = v;  // gradient_parts_kernel reads it at once
+            };
+            put(low, row, at);
+            put(high, row + 8, at + (size_t)8 * a.n_out);
+        }
+    }
+}
+template <typename W, int NI>
+__device__ inline void store_singly(const GradientArgs &a, int e, int in, int out, int lane, const floatx4 (&acc)[NI][4]) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int row = in + i * 16 + (lane & 15);
+        if (row >= a.n_in) continue;
+#pragma unroll
+        for (int o = 0; o < 4; ++o) {
+            const int col = out + o * 16 + 4 * (lane >> 4);
+            const size_t at = ((size_t)e * a.n_in + row) * a.n_out + col;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (col + j < a.n_out) reinterpret_cast<W *>(a.d_w)[at + j] = (W)(a.add ? acc[i][o][j] + (float)reinterpret_cast<const W *>(a.add)[at + j] : acc[i][o][j]);
+        }
+    }
+}
+template <bool VEC, int NI>
+__device__ inline void store_gradient(const GradientArgs &a, int e, int in, int out, int lane, floatx4 (&acc)[NI][4]) {
+    auto finish = [&](auto type) {
+        if constexpr (VEC) store_lines<decltype(type)>(a, e, in, out, lane, acc);
+        else store_singly<decltype(type)>(a, e, in, out, lane, acc);
     };
     if (a.dtype == PGMOE_F32) finish(float());
     else if (a.dtype == PGMOE_BF16) finish(__bf16());
     else finish(_Float16());
 }
 
-template <int XQ, typename Y, int PX, bool VEC>
-static int launch_gradient(const GradientArgs &a, hipStream_t s) {
-    constexpr int LDS = 2 * (PX + pieces_of<Y>) * WG_PLANE;
-    if (LDS > 48 * 1024) {  // the kernel's limit is raised once per device
-        static std::atomic<uint64_t> raised{0};
-        int device = 0;
-        if (const hipError_t e = hipGetDevice(&device))
-            return e == hipErrorNoDevice ? fail(nullptr, PGMOE_ENODEVICE, "pgmoe_expert_weight_gradient: no HIP device is visible") : hip_fail(nullptr, e, "hipGetDevice");
-        if (!(raised.load(std::memory_order_relaxed) >> (device & 63) & 1)) {
-            PG_HIP(nullptr, hipFuncSetAttribute(reinterpret_cast<const void *>(&weight_gradient_kernel<XQ, Y, PX, VEC>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-            raised.fetch_or(1ull << (device & 63), std::memory_order_relaxed);
+// Which tile, of which part of an expert's rows, is item number i.  Workgroups go to the 8 dies in turn: one takes group_in x group_out neighbouring tiles, whose rows
+// its L2 then holds.  e >= E: none from here on; ti >= tiles_in or to >= tiles_out: none at this number.
+struct GradientItem {
+    int e, part, ti, to;
+};
+__device__ inline GradientItem gradient_item(const GradientArgs &a, int i) {
+    const int group_items = a.group_in * a.group_out, turn = i >> 3, group = turn / group_items * 8 + (i & 7), in_group = turn % group_items;
+    const int groups_out = (a.tiles_out + a.group_out - 1) / a.group_out, groups_in = (a.tiles_in + a.group_in - 1) / a.group_in;
+    const int m = group / (groups_in * groups_out), at = group - m * groups_in * groups_out, e = m / a.parts;
+    return {e, m - e * a.parts, at / groups_out * a.group_in + in_group / a.group_out, at % groups_out * a.group_out + in_group % a.group_out};
+}
+
+// An item is BI inputs by BO outputs; a workgroup takes every gridDim-th of them and goes through its rows K at a time.  Both sides come through registers, where codes are converted,
+// into one of two buffers in LDS while the other is multiplied, also from one item to the next: the first rows of an item arrive under the last products of the one before.
+// Rows in LDS have 32 bytes more behind them than their columns: the eight rows of 32 bytes that half a wavefront reads at once then lie in different banks.
+template <int WI_, int WO_, int NI_, int K_>
+struct GradientShape {
+    static constexpr int WI = WI_, WO = WO_, NI = NI_, NO = 4, K = K_;  // wavefronts; 16 x 16 tiles of one
+    static constexpr int BI = WI * NI * 16, BO = WO * NO * 16, THREADS = WI * WO * 64;
+    // a thread brings XP and YP pieces of eight columns of rows that lie XR and YR apart; bytes from one row to the next in LDS
+    static constexpr int XR = THREADS * 8 / BI, YR = THREADS * 8 / BO, XP = K / XR, YP = K / YR, XS = 2 * BI + 32, YS = 2 * BO + 32;
+    static_assert(BI % 128 == 0 && BO % 128 == 0 && XP * XR == K && YP * YR == K && K % 32 == 0, "whole pieces");
+    static constexpr int buffer(int px, int py) { return K * (px * XS + py * YS); }
+    // wavefronts a SIMD: of small tiles with few pieces four workgroups fit into a CU
+    static constexpr int waves(int px, int py) { return THREADS == 256 && px * py == 1 ? 4 : THREADS == 256 && px * py < 4 ? 3 : 2; }
+};
+template <int XQ, typename Y, int PX, bool VEC, typename S>
+__global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight_gradient_kernel(const GradientArgs a) {
+    constexpr int XPLANE = S::K * S::XS, YPLANE = S::K * S::YS, PY = pieces_of<Y>, BUFFER = S::buffer(PX, PY), KEPT = PX > PY ? PX : PY;  // KEPT: pieces i and j are multiplied where i + j < KEPT
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / S::WO, wo = wave % S::WO;
+    const int x_piece = threadIdx.x % (S::BI / 8), x_row = threadIdx.x / (S::BI / 8), y_piece = threadIdx.x % (S::BO / 8), y_row = threadIdx.x / (S::BO / 8);
+
+    struct Item {
+        GradientItem at;
+        int first, rows;  // of d_y and x
+    };
+    auto find = [&](int &i, Item &it) {  // the item at number i or the next of this workgroup behind it -> is there one?
+        for (;; i += gridDim.x) {
+            it.at = gradient_item(a, i);
+            if (it.at.e >= a.E) return false;
+            if (it.at.ti >= a.tiles_in || it.at.to >= a.tiles_out) continue;
+            const int lo = max(0, min(a.offsets[it.at.e], a.rows)), n = max(lo, min(a.offsets[it.at.e + 1], a.rows)) - lo;
+            if (a.parts == 1) {
+                it.first = lo;
+                it.rows = n;
+                return true;
+            }
+            const int steps = (n + S::K - 1) / S::K, from = first_step(steps, it.at.part, a.parts) * S::K, to = min(first_step(steps, it.at.part + 1, a.parts) * S::K, n);
+            if (to <= from) continue;  // its plane is not read
+            it.first = lo + from;
+            it.rows = to - from;
+            return true;
         }
+    };
+
+    // what a thread brings of an item; columns past the last are others', nobody's result
+    const uint8_t *x;
+    const float *x_scale;
+    const Y *d_y;
+    unsigned x_col;
+    int col, left;  // rows that are not requested
+    auto open = [&](const Item &it) {
+        const int block = min(it.at.ti * (S::BI / 128) + x_piece / 16, fp8_blocks(a.n_in) - 1);
+        x_col = block * 128 + x_piece % 16 * 8;
+        col = min(it.at.to * S::BO + y_piece * 8, VEC ? a.n_out - 8 : a.n_out - 1);
+        x = a.x + (size_t)it.first * a.x_stride;
+        x_scale = a.x_scale + (size_t)block * a.x_scale_stride + it.first;
+        d_y = reinterpret_cast<const Y *>(a.d_y) + (size_t)it.first * a.d_y_stride;
+        left = it.rows;
+    };
+    intx2 codes[S::XP];
+    float scale[S::XP];
+    struct { Y v[8]; } grad[S::YP];
+    int requested;  // rows
+    auto request = [&] {  // past the last row the last one, which keep() clears
+#pragma unroll
+        for (int i = 0; i < S::XP; ++i) {
+            const int r = min(x_row + i * S::XR, left - 1);
+            scale[i] = x_scale[r];
+            if constexpr (VEC) codes[i] = *reinterpret_cast<const intx2 *>(x + ((unsigned)r * (unsigned)a.x_stride + x_col));  // less than 2^32 bytes a step
+            else codes[i] = *reinterpret_cast<const intx2 *>(x + (size_t)r * a.x_stride + x_col);
+        }
+#pragma unroll
+        for (int i = 0; i < S::YP; ++i) {
+            const int r = min(y_row + i * S::YR, left - 1);
+            if constexpr (VEC) {
+                typedef Y Yx8 __attribute__((ext_vector_type(8), aligned(16)));
+                *reinterpret_cast<Yx8 *>(grad[i].v) =
+                    *reinterpret_cast<const Yx8 *>(reinterpret_cast<const char *>(d_y) + ((unsigned)r * ((unsigned)a.d_y_stride * (unsigned)sizeof(Y)) + col * (unsigned)sizeof(Y)));
+            } else {
+                const Y *g = d_y + (size_t)r * a.d_y_stride;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) grad[i].v[j] = g[min(col + j, a.n_out - 1)];
+            }
+        }
+        requested = left;
+        left -= S::K;
+        x += (size_t)S::K * a.x_stride;
+        x_scale += S::K;
+        d_y += (size_t)S::K * a.d_y_stride;
+    };
+    int buffer = 0;
+    auto keep = [&](int at) {
+        char *to = lds + at * BUFFER;
+        const intx4 none = {0, 0, 0, 0};  // rows behind the last are zero on both sides, whatever the last one holds
+#pragma unroll
+        for (int i = 0; i < S::XP; ++i) {
+            const int r = x_row + i * S::XR;
+            intx4 px[PX];
+            open_codes<XQ, PX>(codes[i], scale[i], px);
+#pragma unroll
+            for (int p = 0; p < PX; ++p) *reinterpret_cast<intx4 *>(to + p * XPLANE + r * S::XS + x_piece * 16) = r < requested ? px[p] : none;
+        }
+#pragma unroll
+        for (int i = 0; i < S::YP; ++i) {
+            const int r = y_row + i * S::YR;
+            intx4 py[PY];
+            if constexpr (PY == 1) {
+                py[0] = __builtin_bit_cast(intx4, grad[i]);
+            } else {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = (float)grad[i].v[j];
+                take_apart<PY>(v, py);
+            }
+#pragma unroll
+            for (int p = 0; p < PY; ++p) *reinterpret_cast<intx4 *>(to + PX * XPLANE + p * YPLANE + r * S::YS + y_piece * 16) = r < requested ? py[p] : none;
+        }
+    };
+    // Gradients are the first operand: a lane's four results of a product are neighbouring outputs of one input.
+    floatx4 acc[S::NI][S::NO];
+    auto multiply = [&](int at) {
+#pragma unroll
+        for (int k = 0; k < S::K; k += 32) {
+            const char *now = lds + at * BUFFER;
+            bf16x8 px[S::NI][PX];
+#pragma unroll
+            for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+                for (int p = 0; p < PX; ++p) px[i][p] = operand_of(now + p * XPLANE + k * S::XS + (wi * S::NI + i) * 32, S::XS, lane);
+#pragma unroll
+            for (int o = 0; o < S::NO; ++o) {
+                bf16x8 py[PY];
+#pragma unroll
+                for (int p = 0; p < PY; ++p) py[p] = operand_of(now + PX * XPLANE + p * YPLANE + k * S::YS + (wo * S::NO + o) * 32, S::YS, lane);
+                // small products first
+                static_for<KEPT>([&](auto s_) {
+                    static_for<PY>([&](auto p_) {
+                        constexpr int s = KEPT - 1 - decltype(s_)::value, p = decltype(p_)::value;
+                        if constexpr (s >= p && s - p < PX) {
+#pragma unroll
+                            for (int i = 0; i < S::NI; ++i) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(py[p], px[i][s - p], acc[i][o], 0, 0, 0);
+                        }
+                    });
+                });
+            }
+        }
+    };
+
+    int i = blockIdx.x;
+    Item it, next;
+    if (!find(i, it)) return;  // uniform over the workgroup, as all below
+    if (it.rows > 0) {
+        open(it);
+        request();
+        keep(buffer);
     }
-    hipLaunchKernelGGL((weight_gradient_kernel<XQ, Y, PX, VEC>), dim3((unsigned)((int64_t)a.E * a.tiles_in * a.tiles_out)), dim3(WG_THREADS), LDS, s, a);
+    for (;;) {
+        i += gridDim.x;
+        const bool more = find(i, next);
+#pragma unroll
+        for (int x = 0; x < S::NI; ++x)
+#pragma unroll
+            for (int o = 0; o < S::NO; ++o) acc[x][o] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int rows = it.rows; rows > 0; rows -= S::K) {
+            lds_barrier();  // these rows are there for everyone, and everyone has read the ones before
+            const bool last = rows <= S::K, any = !last || (more && next.rows > 0);
+            if (last && any) open(next);
+            if (any) request();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);  // before another wavefront's conversions: 2 to 4 %
+            multiply(buffer);
+            __builtin_amdgcn_s_setprio(0);
+            if (any) keep(buffer ^ 1);
+            buffer ^= 1;
+        }
+        if (it.rows == 0 && more && next.rows > 0) {
+            open(next);
+            request();
+            keep(buffer);
+        }
+        store_gradient<VEC>(a, it.at.part * a.E + it.at.e, it.at.ti * S::BI + wi * S::NI * 16, it.at.to * S::BO + wo * S::NO * 16, lane, acc);
+        if (!more) return;
+        it = next;
+    }
+}
+
+// The planes of an expert's parts, added up in their order.
+template <typename W, bool VEC>
+__global__ __launch_bounds__(256) void gradient_parts_kernel(const float *parts, const GradientArgs a, int K) {
+    constexpr int N = VEC ? 4 : 1;
+    typedef W WxN __attribute__((ext_vector_type(N)));
+    typedef float FxN __attribute__((ext_vector_type(N)));
+    const int64_t size = (int64_t)a.n_in * a.n_out, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N;
+    const int e = blockIdx.y;
+    if (at >= size) return;
+    const int lo = max(0, min(a.offsets[e], a.rows)), steps = (max(lo, min(a.offsets[e + 1], a.rows)) - lo + K - 1) / K;
+    FxN sum = {};
+#pragma unroll 4
+    for (int p = 0; p < a.parts; ++p)
+        if (first_step(steps, p + 1, a.parts) > first_step(steps, p, a.parts)) sum += *reinterpret_cast<const FxN *>(parts + ((int64_t)p * a.E + e) * size + at);
+    const int64_t to = e * size + at;
+    WxN out;
+    if (a.add) {
+        const WxN add = *reinterpret_cast<const WxN *>(reinterpret_cast<const W *>(a.add) + to);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += (float)add[j];
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) out[j] = (W)sum[j];
+    *reinterpret_cast<WxN *>(reinterpret_cast<W *>(a.d_w) + to) = out;
+}
+
+using SmallTile = GradientShape<2, 2, 4, 32>;
+using WideTile = GradientShape<2, 4, 4, 32>;
+using LargeTile = GradientShape<2, 4, 8, 64>;
+
+// More than 48 KiB of LDS: the kernel's limit is raised once per device.
+static int raise_lds(const void *kernel, int bytes, std::atomic<uint64_t> &raised) {
+    int device = 0;
+    if (const hipError_t e = hipGetDevice(&device))
+        return e == hipErrorNoDevice ? fail(nullptr, PGMOE_ENODEVICE, "pgmoe_expert_weight_gradient: no HIP device is visible") : hip_fail(nullptr, e, "hipGetDevice");
+    if (!(raised.load(std::memory_order_relaxed) >> (device & 63) & 1)) {
+        PG_HIP(nullptr, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        raised.fetch_or(1ull << (device & 63), std::memory_order_relaxed);
+    }
     return PGMOE_OK;
 }
+// Tiles in groups of up to 1024 x 1024, as long as there are two for each die -> item numbers.
+static int64_t gradient_items(GradientArgs &a, int tile_in, int tile_out) {
+    a.tiles_in = (a.n_in + tile_in - 1) / tile_in;
+    a.tiles_out = (a.n_out + tile_out - 1) / tile_out;
+    a.group_in = std::min(a.tiles_in, 1024 / tile_in);
+    a.group_out = std::min(a.tiles_out, 1024 / tile_out);
+    const auto groups = [&] { return (int64_t)a.E * a.parts * ((a.tiles_in + a.group_in - 1) / a.group_in) * ((a.tiles_out + a.group_out - 1) / a.group_out); };
+    while (groups() < 16 && a.group_in * a.group_out > 1) (a.group_in > a.group_out ? a.group_in : a.group_out) = (std::max(a.group_in, a.group_out) + 1) / 2;
+    return (groups() + 7) / 8 * 8 * a.group_in * a.group_out;
+}
+template <int XQ, typename Y, int PX, bool VEC, typename S>
+static int launch_shape(GradientArgs a, hipStream_t s, int64_t most = 0) {  // most: workgroups (0: one an item)
+    constexpr int LDS = 2 * S::buffer(PX, pieces_of<Y>);
+    static std::atomic<uint64_t> raised{0};
+    int64_t grid = gradient_items(a, S::BI, S::BO);
+    if (grid * S::THREADS > GRID_THREADS_MAX)
+        return fail(nullptr, PGMOE_EINVAL, "pgmoe_expert_weight_gradient: %d matrices of %d x %d are more than one launch holds", a.E, a.n_in, a.n_out);
+    if (most) grid = std::min(grid, most);
+    if (LDS > 48 * 1024)
+        if (const int rc = raise_lds(reinterpret_cast<const void *>(&weight_gradient_kernel<XQ, Y, PX, VEC, S>), LDS, raised)) return rc;
+    hipLaunchKernelGGL((weight_gradient_kernel<XQ, Y, PX, VEC, S>), dim3((unsigned)grid), dim3(S::THREADS), LDS, s, a);
+    return PGMOE_OK;
+}
+// Into how many parts the rows of each expert are split where there are fewer tiles than workgroups run at once.  A tile by itself takes 18.5 ns a row; parts cost two more
+// launches' overhead and a write and a read of 64 KiB each at 3 TB/s.  us without parts / with as many as this says, bfloat16 gradients: one expert of 512 x 1024 from 512 rows 13.9 (2 parts
+// would take 14.7), 1024 21.5 / 18.1, 4096 81 / 26, 16384 303 / 40; one of 1024 x 4096 from 1024 rows 26.7 (2: 31.0), 4096 81 / 60; eight of 512 x 512 from 512 rows each
+// 15.0 (2: 19.2), 2048 44 / 29; eight of 1024 x 1024 from 4096 each 93 (2: 142).
+constexpr int GRADIENT_PARTS = 16, CUS = 256;
+static int gradient_parts(int rows, int E, int n_in, int n_out) {
+    const int64_t tiles = (int64_t)E * fp8_blocks(n_in) * fp8_blocks(n_out);
+    if (tiles > CUS) return 1;
+    const int each = rows / E, parts = std::min({512 / (int)tiles, each / 256, GRADIENT_PARTS});
+    if (parts < 2) return 1;
+    return 0.0185 * each * (parts - 1) / parts > 4 + 0.021 * tiles * parts ? parts : 1;
+}
+template <int XQ, typename Y, int PX, bool VEC>
+static int launch_parts(const GradientArgs &a, float *planes, hipStream_t s) {
+    GradientArgs p = a;
+    p.d_w = planes;
+    p.add = nullptr;
+    p.dtype = PGMOE_F32;
+    const int rc = launch_shape<XQ, Y, PX, VEC, SmallTile>(p, s);
+    if (rc) return rc;
+    const int64_t size = (int64_t)a.n_in * a.n_out;
+    const dim3 grid((unsigned)((size / (VEC ? 4 : 1) + 255) / 256), a.E);
+    if (a.dtype == PGMOE_F32) hipLaunchKernelGGL((gradient_parts_kernel<float, VEC>), grid, dim3(256), 0, s, planes, a, SmallTile::K);
+    else if (a.dtype == PGMOE_BF16) hipLaunchKernelGGL((gradient_parts_kernel<__bf16, VEC>), grid, dim3(256), 0, s, planes, a, SmallTile::K);
+    else hipLaunchKernelGGL((gradient_parts_kernel<_Float16, VEC>), grid, dim3(256), 0, s, planes, a, SmallTile::K);
+    return PGMOE_OK;
+}
+// Which tiles (us, bfloat16 gradients with scales that are powers of two unless said otherwise, float32 results):
+//  * 256 x 256, one workgroup a CU: from 256 rows an expert on the mean on, if the last round of a tile for each CU leaves at most a fifth of them idle (64 experts of 1024 x 4096 from 64 rows each 232, 128 x 128
+//    214, 256 rows 325 / 363, 512 430 / 492; 16 of 512 x 2048 from 256 24.1 / 23.9, 2048 80 / 96; 192 tiles: eight of 768 x 2048 from 512 30.3 / 26.5, 2048 73 / 68);
+//  * 128 x 256, where pieces of both sides leave room in LDS for one workgroup a CU of either kind, if there are more of 128 x 128 than CUs: 16 experts of 2048 x 768 from 512 rows each, three and three pieces
+//    160, 128 x 128 231; eight of 1024 x 1024 from 32 rows 15.8 / 20.3; eight of 512 x 512 from 512 rows, three and two pieces 42.7 / 34.5;
+//  * 128 x 128 otherwise.
+template <int XQ, typename Y, int PX, bool VEC>
+static int launch_gradient(const GradientArgs &a, float *planes, hipStream_t s) {
+    if (a.parts > 1) return launch_parts<XQ, Y, PX, VEC>(a, planes, s);
+    const auto tiles = [&](int in, int out) { return (int64_t)a.E * ((a.n_in + in - 1) / in) * ((a.n_out + out - 1) / out); };
+    if constexpr (PX * pieces_of<Y> == 1 && VEC) {
+        const int64_t large = tiles(256, 256), rounds = (large + CUS - 1) / CUS;
+        if (a.rows / a.E >= 256 && 5 * large >= 4 * CUS * rounds) return launch_shape<XQ, Y, PX, VEC, LargeTile>(a, s, CUS);
+    }
+    if constexpr (PX == 3 && pieces_of<Y> > 1)
+        if (tiles(128, 128) > CUS) return launch_shape<XQ, Y, PX, VEC, WideTile>(a, s);
+    return launch_shape<XQ, Y, PX, VEC, SmallTile>(a, s);
+}
 template <int XQ, typename Y>
-static int launch_gradient(const GradientArgs &a, bool pow2, hipStream_t s) {
-    const bool vec = a.n_out % 8 == 0 && a.d_y_stride * sizeof(Y) % 16 == 0 && aligned(a.d_y, 16) && aligned(a.d_w, 16) && aligned(a.add, 16);
-    if (pow2) return vec ? launch_gradient<XQ, Y, 1, true>(a, s) : launch_gradient<XQ, Y, 1, false>(a, s);
-    return vec ? launch_gradient<XQ, Y, 3, true>(a, s) : launch_gradient<XQ, Y, 3, false>(a, s);
+static int launch_gradient(const GradientArgs &a, bool pow2, float *planes, hipStream_t s) {
+    const bool vec = a.n_out % 8 == 0 && a.d_y_stride * sizeof(Y) % 16 == 0 && a.d_y_stride * sizeof(Y) < (1 << 25) && a.x_stride < (1 << 25) && a.x_scale_stride < (1 << 28) && aligned(a.d_y, 16) && aligned(a.d_w, 16) && aligned(a.add, 16);
+    if (pow2) return vec ? launch_gradient<XQ, Y, 1, true>(a, planes, s) : launch_gradient<XQ, Y, 1, false>(a, planes, s);
+    return vec ? launch_gradient<XQ, Y, 3, true>(a, planes, s) : launch_gradient<XQ, Y, 3, false>(a, planes, s);
 }
 template <int XQ>
-static int launch_gradient(const GradientArgs &a, int y_dtype, bool pow2, hipStream_t s) {
-    if (y_dtype == PGMOE_F32) return launch_gradient<XQ, float>(a, pow2, s);
-    if (y_dtype == PGMOE_BF16) return launch_gradient<XQ, __bf16>(a, pow2, s);
-    return launch_gradient<XQ, _Float16>(a, pow2, s);
+static int launch_gradient(const GradientArgs &a, int y_dtype, bool pow2, float *planes, hipStream_t s) {
+    if (y_dtype == PGMOE_F32) return launch_gradient<XQ, float>(a, pow2, planes, s);
+    if (y_dtype == PGMOE_BF16) return launch_gradient<XQ, __bf16>(a, pow2, planes, s);
+    return launch_gradient<XQ, _Float16>(a, pow2, planes, s);
 }
 
 }  // namespace pgmoe
@@ -272,7 +516,11 @@ using namespace pgmoe;
 
 extern "C" {
 
-size_t pgmoe_expert_weight_gradient_workspace_bytes(int rows, int n_experts, int n_in, int n_out) { return 0; }
+size_t pgmoe_expert_weight_gradient_workspace_bytes(int rows, int n_experts, int n_in, int n_out) {
+    if (rows < 1 || n_experts < 1 || n_in < 1 || n_out < 1) return 0;
+    const int parts = gradient_parts(rows, n_experts, n_in, n_out);
+    return parts > 1 ? (size_t)parts * n_experts * n_in * n_out * sizeof(float) : 0;
+}
 
 int pgmoe_expert_weight_gradient(const pgmoe_fp8_rows *x, const void *d_y, int64_t d_y_stride, int d_y_dtype, const int32_t *expert_offsets, int n_experts, int n_out,
                                  const void *add, void *d_w, int d_w_dtype, void *workspace, size_t workspace_bytes, void *stream) {
@@ -285,13 +533,11 @@ int pgmoe_expert_weight_gradient(const pgmoe_fp8_rows *x, const void *d_y, int64
     if (n_out < 1 || n_out > FP8_COLS_MAX) return fail(nullptr, PGMOE_EINVAL, "%s: n_out=%d outside 1..%d", fn, n_out, FP8_COLS_MAX);
     if (x->rows > (1 << 24)) return fail(nullptr, PGMOE_EINVAL, "%s: %d rows: at most 2^24", fn, x->rows);
     if (d_y_stride < n_out) return fail(nullptr, PGMOE_EINVAL, "%s: d_y_stride=%lld is less than n_out=%d", fn, (long long)d_y_stride, n_out);
-    const int tiles_in = fp8_blocks(x->cols), tiles_out = (n_out + WG_TILE - 1) / WG_TILE;
-    if ((int64_t)n_experts * tiles_in * tiles_out * WG_THREADS > GRID_THREADS_MAX)
-        return fail(nullptr, PGMOE_EINVAL, "%s: %d matrices of %d x %d are more than one launch holds", fn, n_experts, x->cols, n_out);
     if (x->rows > 0) NEED_PTR(nullptr, fn, d_y, dtype_bytes(d_y_dtype));
     NEED_PTR(nullptr, fn, expert_offsets, 4);
     NEED_PTR(nullptr, fn, d_w, dtype_bytes(d_w_dtype));
     OPT_PTR(nullptr, fn, add, dtype_bytes(d_w_dtype));
+    OPT_PTR(nullptr, fn, workspace, 16);
     GradientArgs a = {};
     a.x = (const uint8_t *)x->q;
     a.x_stride = (size_t)x->q_stride;
@@ -307,10 +553,12 @@ int pgmoe_expert_weight_gradient(const pgmoe_fp8_rows *x, const void *d_y, int64
     a.add = add;
     a.d_w = d_w;
     a.dtype = d_w_dtype;
-    a.tiles_in = tiles_in;
-    a.tiles_out = tiles_out;
+    const size_t need = pgmoe_expert_weight_gradient_workspace_bytes(x->rows, n_experts, x->cols, n_out);
+    const bool split = need > 0 && workspace && workspace_bytes >= need;
+    a.parts = split ? (int)(need / sizeof(float) / ((size_t)n_experts * x->cols * n_out)) : 1;
+    float *planes = (float *)workspace;
     const bool pow2 = (x->dtype & PGMOE_SCALE_POW2) != 0;
-    rc = fp8_type(x->dtype) == PGMOE_E4M3 ? launch_gradient<PGMOE_E4M3>(a, d_y_dtype, pow2, (hipStream_t)stream) : launch_gradient<PGMOE_E5M2>(a, d_y_dtype, pow2, (hipStream_t)stream);
+    rc = fp8_type(x->dtype) == PGMOE_E4M3 ? launch_gradient<PGMOE_E4M3>(a, d_y_dtype, pow2, planes, (hipStream_t)stream) : launch_gradient<PGMOE_E5M2>(a, d_y_dtype, pow2, planes, (hipStream_t)stream);
     return rc ? rc : launched(fn);
 }
 

@@ -356,12 +356,18 @@ def test_expert_weight_gradient(B, counts, n_in, n_out):
 
 
 @pytest.mark.parametrize("counts,n_in,n_out,y_kind,pow2", [([700, 300], 1024, 640, "bf16", True), ([90] * 20, 768, 512, "bf16", True), ([4, 2, 0, 7] * 16, 512, 264, "f32", False),
-                                                           ([2000, 0, 9], 256, 256, "bf16", True), ([1500], 300, 520, "f16", False), ([40] * 8, 512, 1024, "f16", True)])
+                                                           ([2000, 0, 9], 256, 256, "bf16", True), ([1500], 300, 520, "f16", False), ([40] * 8, 512, 1024, "f16", True),
+                                                           ([0, 2000, 1, 31, 64, 65, 700] + [150] * 9, 500, 2040, "bf16", True), ([0, 64, 1] + [300] * 13, 512, 2048, "bf16", True),
+                                                           ([33] * 20, 520, 300, "f16", False), ([20, 0, 70] * 8, 300, 530, "f32", False), ([3000], 130, 200, "bf16", False),
+                                                           ([0, 4000, 1, 20], 250, 252, "f32", True)])
 def test_expert_weight_gradient_of_ordinary_sizes(B, counts, n_in, n_out, y_kind, pow2):
     say("gradient", counts[:6], n_in, n_out, y_kind, pow2)
     p = Gradient(B, counts, n_in, n_out, "e4m3", y_kind, pow2)
     p.check("f32")
-    p.check("bf16")
+    add = dev(np.random.default_rng(1).standard_normal((p.E, n_in, n_out)), "bf16")
+    p.check("bf16", add)
+    if B.expert_weight_gradient_workspace_bytes(p.R, p.E, n_in, n_out):
+        p.check("f32", workspace=False)
 
 
 @pytest.mark.parametrize("out", DTYPES)

@@ -70,7 +70,7 @@ BAD = [
     ("gradient", dict(n_experts=0), "n_experts"), ("gradient", dict(n_experts=257), "n_experts"), ("gradient", dict(n_out=0), "n_out"), ("gradient", dict(n_out=(1 << 22) + 1), "n_out"),
     ("gradient", dict(d_y_stride=299), "d_y_stride"), ("gradient", dict(d_y=None), "d_y is NULL"), ("gradient", dict(d_y=P + 1), "d_y is not"), ("gradient", dict(offsets=None), "expert_offsets"),
     ("gradient", dict(d_w=None), "d_w is NULL"), ("gradient", dict(d_w=P + 2), "d_w is not"), ("gradient", dict(add=P + 2), "add is not"),
-    ("gradient", dict(x=rows8(cols=1 << 22, q_stride=1 << 22), n_out=1 << 20, d_y_stride=1 << 20), "launch"),
+    ("gradient", dict(x=rows8(cols=1 << 22, q_stride=1 << 22), n_out=1 << 20, d_y_stride=1 << 20), "launch"), ("gradient", dict(workspace=P + 8, bytes=64), "workspace"),
 ]
 
 
@@ -116,6 +116,11 @@ def test_workspace_of_the_weight_gradient():
     for args in ((0, 8, 512, 512), (64, 0, 512, 512), (64, 8, 0, 512), (64, 8, 512, -1)):
         assert B.expert_weight_gradient_workspace_bytes(*args) == 0
     assert B.expert_weight_gradient_workspace_bytes(32768, 64, 1024, 4096) == 0          # many matrices
+    # one matrix and many rows, in parts: planes of float32; the sizes its rule was measured at, both sides
+    for rows, E, n_in, n_out, parts in ((512, 1, 512, 1024, 1), (1024, 1, 512, 1024, 4), (4096, 1, 512, 1024, 16), (1 << 24, 1, 512, 1024, 16), (1024, 1, 1024, 4096, 1), (4096, 1, 1024, 4096, 2),
+                                        (4096, 8, 512, 512, 1), (16384, 8, 512, 512, 4), (32768, 8, 1024, 1024, 1)):
+        assert B.expert_weight_gradient_workspace_bytes(rows, E, n_in, n_out) == (4 * parts * E * n_in * n_out if parts > 1 else 0), (rows, E, n_in, n_out)
+    assert B.expert_weight_gradient_workspace_bytes((1 << 31) - 1, 1, 1 << 22, 1 << 22) == 0
 
 
 # ------------------------------------------------------------------------------------ the binding
