@@ -284,12 +284,15 @@ def _fp8_rows(q, scale, cols, name, pow2=False) -> FP8Rows:
     code = _DTYPES.get(q.dtype)
     if code != E4M3 and code != E5M2:
         raise TypeError(f"{name} has dtype {q.dtype}, not an 8-bit one")
-    stride, (rows, width), blocks = _row_stride(q, name), q.shape, (cols + FP8_BLOCK - 1) // FP8_BLOCK
+    if len(q.shape) != 2:
+        raise ValueError(f"{name} has {len(q.shape)} dimensions, not 2")
+    rows, width = q.shape
+    stride, blocks = max(q.stride(0), width) if q.is_contiguous() else _row_stride(q, name), (cols + FP8_BLOCK - 1) // FP8_BLOCK
     if width < FP8_BLOCK * blocks:
         raise ValueError(f"{name} has {width} columns, fewer than the {FP8_BLOCK * blocks} of whole blocks")
     if scale.shape != (blocks, rows) or scale.dtype != _f32:
         raise ValueError(f"{name}'s scale is {scale.dtype} {tuple(scale.shape)}, not float32 {(blocks, rows)}")
-    return FP8Rows(q.data_ptr(), stride, scale.data_ptr(), _row_stride(scale, "a scale"), rows, cols, code | SCALE_POW2 if pow2 else code)
+    return FP8Rows(q.data_ptr(), stride, scale.data_ptr(), max(scale.stride(0), rows) if scale.is_contiguous() else _row_stride(scale, "a scale"), rows, cols, code | SCALE_POW2 if pow2 else code)
 
 
 def fp8_weight_shapes(n_experts: int, n_in: int, n_out: int):
@@ -410,7 +413,8 @@ def _values(t, name, rows, cols):
         return None, 0, F32
     if t.shape != (rows, cols):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(rows, cols)}")
-    return t.data_ptr(), _row_stride(t, name), _dtype(t, name)
+    code = _DTYPES.get(t.dtype)
+    return t.data_ptr(), cols if t.is_contiguous() else _row_stride(t, name), _dtype(t, name) if code is None else code
 
 
 def _codes_of(q, scale, rows, cols, name, pow2):
@@ -478,7 +482,7 @@ def relu_backward(d_h, h_q, d_pre=None, q=None, scale=None, pow2=False, stream=N
     code = _DTYPES.get(h_q.dtype)
     if code != E4M3 and code != E5M2:
         raise TypeError(f"h_q has dtype {h_q.dtype}, not an 8-bit one")
-    args = (*_values(d_h, "d_h", R, n), R, n, h_q.data_ptr(), _row_stride(h_q, "h_q"), code, *_values(d_pre, "d_pre", R, n), _codes_of(q, scale, R, n, "q", pow2))
+    args = (*_values(d_h, "d_h", R, n), R, n, h_q.data_ptr(), max(h_q.stride(0), h_q.shape[1]) if h_q.is_contiguous() else _row_stride(h_q, "h_q"), code, *_values(d_pre, "d_pre", R, n), _codes_of(q, scale, R, n, "q", pow2))
     rc = lib.pgmoe_relu_backward(*args, _stream_for(stream, d_h, h_q, d_pre, q, scale))
     if rc:
         raise PgmoeError(rc, last_error())

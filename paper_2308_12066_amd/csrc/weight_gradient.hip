@@ -113,8 +113,18 @@ __device__ inline void store_lines(const GradientArgs &a, int e, int in, int out
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));  // worked out again: what depends on it is not kept in registers across the products
     const bool up = lane & 8;
     const int g = lane >> 4;
+    constexpr int AT_ONCE = NI == 8 ? 2 : 1;  // of the 16-input tiles whose float32 addends are requested together, as far as registers go
+    floatx4 addend[AT_ONCE][4];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
+        if constexpr (sizeof(W) == 4)
+            if (a.add && i % AT_ONCE == 0) {
+#pragma unroll
+                for (int n = 0; n < AT_ONCE * 4; ++n) {
+                    const int row = in + (i + n / 4) * 16 + (lane & 7) + (n & 1) * 8, col = out + ((n & 2) + (up ? 1 : 0)) * 16 + 4 * g;
+                    if (row < a.n_in && col < a.n_out) addend[n / 4][n & 3] = *reinterpret_cast<const floatx4 *>(reinterpret_cast<const float *>(a.add) + ((size_t)e * a.n_in + row) * a.n_out + col);
+                }
+            }
         intx4 unit[UNITS];
         if constexpr (sizeof(W) == 4) {
 #pragma unroll
@@ -150,16 +160,16 @@ __device__ inline void store_lines(const GradientArgs &a, int e, int in, int out
             const int col = out + (sizeof(W) == 4 ? (u + (up ? 1 : 0)) * 16 + 4 * g : (u + (up ? 1 : 0)) * 32 + (g & 1) * 16 + (g >> 1) * 8);
             const int row = in + i * 16 + (lane & 7);
             const size_t at = ((size_t)e * a.n_in + row) * a.n_out + col;
-            auto put = [&](intx4 v, int r, size_t at) {
+            auto put = [&](intx4 v, int r, size_t at, int n) {
                 if (r >= a.n_in || col >= a.n_out) return;
                 if constexpr (sizeof(W) == 4)
-                    if (a.add) v = __builtin_bit_cast(intx4, __builtin_bit_cast(floatx4, v) + *reinterpret_cast<const floatx4 *>(reinterpret_cast<const float *>(a.add) + at));
+                    if (a.add) v = __builtin_bit_cast(intx4, __builtin_bit_cast(floatx4, v) + addend[i % AT_ONCE][n]);
                 intx4 *to = reinterpret_cast<intx4 *>(reinterpret_cast<W *>(a.d_w) + at);
                 if (a.parts == 1) __builtin_nontemporal_store(v, to);
                 else *to = v;  // gradient_parts_kernel reads it at once
             };
-            put(low, row, at);
-            put(high, row + 8, at + (size_t)8 * a.n_out);
+            put(low, row, at, u);
+            put(high, row + 8, at + (size_t)8 * a.n_out, u + 1);
         }
     }
 }
