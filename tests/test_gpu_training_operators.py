@@ -515,3 +515,157 @@ def test_dispatch_and_combine_with_offsets_that_pass_32_bits(B):
     assert torch.equal(y, x)
     xs = f64(x)
     near(d_w[:, 0], (xs * xs).sum(1), 17 * H * (xs * xs).sum(1), "f32")
+
+
+# ------------------------------------------------------------------------------------ together
+@pytest.fixture(scope="module")
+def example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "fp8_experts.py")
+    spec = importlib.util.spec_from_file_location("fp8_experts", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@pytest.mark.parametrize("train", [False, True])
+@pytest.mark.parametrize("T,d,f,E,k", [(1, 256, 512, 8, 2), (60, 128, 300, 16, 3), (400, 256, 520, 4, 2)])
+def test_gradients_of_the_matrices_of_a_block(example, T, d, f, E, k, train):
+    """Of examples/fp8_experts.py, against the chain in 64 bits from what the forward left and the calls' own 16-bit gradients' definition."""
+    say("block gradients", T, d, f, E, k, train)
+    g = np.random.default_rng(T)
+    w1, w2 = ((0.05 * g.standard_normal(s)).astype(np.float32) for s in ((E, d, f), (E, f, d)))
+    x, z, dy = dev(g.standard_normal((T, d)), "bf16"), dev(g.standard_normal((T, E))), g.standard_normal((T, d)).astype(np.float32)
+    block = example.Block(dev(w1), dev(w2), None, k, T, train=train, renormalize=True)
+    block.forward(x, z)
+    without = block.backward(z, dev(dy))
+    start = [dev(g.standard_normal(s)) for s in ((E, d, f), (E, f, d))]
+    d_w = [t.clone() for t in start]
+    with_them = block.backward(z, dev(dy), d_w=d_w)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(without, with_them))
+    row_of, offs, wt = block.row_of.cpu().numpy(), block.offsets.cpu().numpy(), f64(block.weight)
+    d_rows = np.nan_to_num(O.dispatch_rows(dy.astype(np.float64), row_of, T * k, wt.astype(np.float32)))
+    x_q, h_q = f64(block.x_q[0])[:, :d], f64(block.h_q[0])[:, :f]
+    x_s, h_s = f64(block.x_q[1]), f64(block.h_q[1])
+    if train:
+        assert np.all(np.frexp(x_s)[0] == 0.5) and np.all(np.frexp(h_s)[0] == 0.5)
+    most = int(np.diff(offs).max())
+    want, mag = O.expert_weight_gradient(h_q, h_s, d_rows, offs, f64(start[1]))
+    # gradients of the rows rounded to bfloat16, 2^-8 of each, then the product's roundings (three for each row at most)
+    near(d_w[1], want, (2.0 ** -8 * (1 + H) + (3 * most + 20) * H) * mag, "f32")
+    qv, qs = O.quantize_rows(d_rows.astype(np.float32), "e5m2")
+    q2, s2 = O.quantize_weights(w2)
+    d_h, d_h_mag = O.expert_matmul(qv[:, :d], qs, q2.transpose(0, 2, 1), s2.transpose(0, 2, 1), offs)
+    d_pre = O.relu_backward(d_h, h_q)
+    want, mag = O.expert_weight_gradient(x_q, x_s, d_pre, offs, f64(start[0]))
+    _, off = O.expert_weight_gradient(x_q, x_s, np.where(h_q > 0, (128 + 4 * -(-d // 128)) * H * d_h_mag, 0), offs)      # what the product before may be off
+    near(d_w[0], want, (2.0 ** -8 * (1 + H) + (3 * most + 20) * H) * (mag + off) + off, "f32")
+    block.close()
+
+
+def test_step_of_training_replays_from_a_captured_graph(example):
+    """Forward, backward and gradients of the matrices of a block, captured; replays with the eager work of other inputs between them give the eager bits."""
+    say("training captured")
+    T, d, f, E, k = 96, 128, 260, 8, 2
+    g = torch.Generator(device="cuda").manual_seed(5)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    w1, w2 = 0.05 * normal(E, d, f), 0.05 * normal(E, f, d)
+    block = example.Block(w1, w2, None, k, T, train=True, renormalize=True)
+    x, z, dy, d_w = normal(T, d).bfloat16(), normal(T, E), normal(T, d), (torch.zeros(E, d, f, device="cuda"), torch.zeros(E, f, d, device="cuda"))
+    inputs = [(normal(T, d).bfloat16(), normal(T, E), normal(T, d)) for _ in range(3)]
+
+    def step(stream=None):
+        return block.forward(x, z, stream), *block.backward(z, dy, stream, d_w=d_w)
+
+    def put(values):
+        for to, of in zip((x, z, dy), values):
+            to.copy_(of)
+        for t in d_w:
+            t.zero_()
+        torch.cuda.synchronize()
+
+    eager = []
+    for values in inputs:
+        put(values)
+        eager.append([t.clone() for t in (*step(), *d_w)])
+        torch.cuda.synchronize()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        outputs = step(stream)
+    for rep in range(3):
+        for values, want in zip(inputs, eager):
+            put(values)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip((*outputs, *d_w), want)), rep
+            put(inputs[rep])
+            step()
+            torch.cuda.synchronize()
+    del graph
+    block.close()
+
+
+def test_training_calls_on_another_stream_behind_what_fills_their_inputs(B):
+    """Torch's current stream is another than the default one and busy: each call waits for its inputs, and torch for it."""
+    say("training stream")
+    g = np.random.default_rng(2)
+    T, k, d, n_out, counts = 64, 2, 200, 136, [50, 0, 78]
+    row_of, R = entries(g, T, k)
+    x, w, of, offs = dev(g.standard_normal((T, d))), dev(g.random((T, k))), ints(row_of), ints(np.concatenate([[0], np.cumsum(counts)]))
+    d_y = dev(g.standard_normal((R, n_out)), "bf16")
+
+    def run(x, w, d_y):
+        rows, y, d_w, d_rows = (torch.zeros(s, device="cuda") for s in ((R, d), (T, d), (T, k), (R, d)))
+        q, s = codes_for(R, d, "e4m3")
+        B.dispatch_rows(x, of, rows, q, s, w, pow2=True)
+        B.combine_rows(rows, of, y, w)
+        B.combine_rows_backward(y, rows, of, w, d_rows, d_w)
+        d_pre = torch.zeros(R, d, device="cuda")
+        B.relu_backward(d_rows, q, d_pre)
+        grad = torch.zeros(3, d, n_out, device="cuda")
+        B.expert_weight_gradient(q, s, d_y, offs, grad, pow2=True)
+        return [t.clone() for t in (rows, y, d_w, d_rows, d_pre, grad)]
+    want = run(x, w, d_y)
+    torch.cuda.synchronize()
+    late = [torch.zeros_like(t) for t in (x, w, d_y)]
+    big = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for _ in range(3):
+            big = big @ big * 1e-4                           # some milliseconds
+        for to, t in zip(late, (x, w, d_y)):
+            to.copy_(t)
+        got = run(*late)
+        torch.cuda.current_stream().synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_calls_of_training_leave_the_devices_memory_alone(B):
+    """No call allocates, and the same call twice gives the same bits."""
+    say("training bits")
+    g = np.random.default_rng(9)
+    p = Gradient(B, [5000, 0, 40], 200, 264)
+    assert B.expert_weight_gradient_workspace_bytes(p.R, p.E, p.n_in, p.n_out) > 0
+    first = p.run("f32")
+    for _ in range(3):
+        assert torch.equal(p.run("f32"), first)
+    need = B.expert_weight_gradient_workspace_bytes(p.R, p.E, p.n_in, p.n_out)
+    for size in (need - 4, need, need + 400):       # with too small a workspace: without one
+        ws = torch.full((size + 256,), 0xff, dtype=torch.uint8, device="cuda")
+        d_w = torch.zeros(p.E, p.n_in, p.n_out, device="cuda")
+        B.expert_weight_gradient(p.x_q, p.x_scale, p.d_y, p.offsets, d_w, None, True, ws[:size])
+        torch.cuda.synchronize()
+        assert torch.equal(d_w, first if size >= need else p.run("f32", workspace=False)) and torch.all(ws[size:] == 0xff)
+        if size < need:
+            assert torch.all(ws == 0xff)
+    T, d = 3000, 300
+    row_of, R = entries(g, T, 2)
+    x, rows = dev(g.standard_normal((T, d))), dev(g.standard_normal((R, d)))
+    d_w = [torch.zeros(T, 2, device="cuda") for _ in range(2)]
+    free = torch.cuda.mem_get_info()[0]
+    for t in d_w:
+        B.combine_rows_backward(x, rows, ints(row_of), None, None, t)
+    torch.cuda.synchronize()
+    assert torch.equal(*d_w) and torch.cuda.mem_get_info()[0] >= free - (4 << 20)
