@@ -284,15 +284,15 @@ def _fp8_rows(q, scale, cols, name, pow2=False) -> FP8Rows:
     code = _DTYPES.get(q.dtype)
     if code != E4M3 and code != E5M2:
         raise TypeError(f"{name} has dtype {q.dtype}, not an 8-bit one")
-    if len(q.shape) != 2:
-        raise ValueError(f"{name} has {len(q.shape)} dimensions, not 2")
+    if q.dim() != 2:
+        raise ValueError(f"{name} has {q.dim()} dimensions, not 2")
     rows, width = q.shape
-    stride, blocks = max(q.stride(0), width) if q.is_contiguous() else _row_stride(q, name), (cols + FP8_BLOCK - 1) // FP8_BLOCK
+    stride, blocks = width if rows > 1 and q.is_contiguous() else _row_stride(q, name), (cols + FP8_BLOCK - 1) // FP8_BLOCK
     if width < FP8_BLOCK * blocks:
         raise ValueError(f"{name} has {width} columns, fewer than the {FP8_BLOCK * blocks} of whole blocks")
     if scale.shape != (blocks, rows) or scale.dtype != _f32:
         raise ValueError(f"{name}'s scale is {scale.dtype} {tuple(scale.shape)}, not float32 {(blocks, rows)}")
-    return FP8Rows(q.data_ptr(), stride, scale.data_ptr(), max(scale.stride(0), rows) if scale.is_contiguous() else _row_stride(scale, "a scale"), rows, cols, code | SCALE_POW2 if pow2 else code)
+    return FP8Rows(q.data_ptr(), stride, scale.data_ptr(), rows if blocks > 1 and scale.is_contiguous() else _row_stride(scale, "a scale"), rows, cols, code | SCALE_POW2 if pow2 else code)
 
 
 def fp8_weight_shapes(n_experts: int, n_in: int, n_out: int):
@@ -477,12 +477,13 @@ def combine_rows_backward(d_y, rows, row_of, weight=None, d_rows=None, d_weight=
 def relu_backward(d_h, h_q, d_pre=None, q=None, scale=None, pow2=False, stream=None) -> None:
     """d_pre = d_h where the codes h_q of a ReLU's results are above zero, else 0, as values (d_h itself may take them), as codes q, or both."""
     R, n = d_h.shape
-    if h_q.shape[0] != R or h_q.shape[1] < FP8_BLOCK * fp8_blocks(n):
-        raise ValueError(f"h_q has shape {tuple(h_q.shape)}, not {(R, FP8_BLOCK * fp8_blocks(n))}")
+    rows, width = h_q.shape
+    if rows != R or width < FP8_BLOCK * fp8_blocks(n):
+        raise ValueError(f"h_q has shape {(rows, width)}, not {(R, FP8_BLOCK * fp8_blocks(n))}")
     code = _DTYPES.get(h_q.dtype)
     if code != E4M3 and code != E5M2:
         raise TypeError(f"h_q has dtype {h_q.dtype}, not an 8-bit one")
-    args = (*_values(d_h, "d_h", R, n), R, n, h_q.data_ptr(), max(h_q.stride(0), h_q.shape[1]) if h_q.is_contiguous() else _row_stride(h_q, "h_q"), code, *_values(d_pre, "d_pre", R, n), _codes_of(q, scale, R, n, "q", pow2))
+    args = (*_values(d_h, "d_h", R, n), R, n, h_q.data_ptr(), width if rows > 1 and h_q.is_contiguous() else _row_stride(h_q, "h_q"), code, *_values(d_pre, "d_pre", R, n), _codes_of(q, scale, R, n, "q", pow2))
     rc = lib.pgmoe_relu_backward(*args, _stream_for(stream, d_h, h_q, d_pre, q, scale))
     if rc:
         raise PgmoeError(rc, last_error())

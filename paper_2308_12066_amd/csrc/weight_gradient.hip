@@ -493,7 +493,8 @@ static int launch_parts(const GradientArgs &a, float *planes, hipStream_t s) {
 //  * 256 x 256, one workgroup a CU: from 256 rows an expert on the mean on, if the last round of a tile for each CU leaves at most a fifth of them idle (64 experts of 1024 x 4096 from 64 rows each 232, 128 x 128
 //    214, 256 rows 325 / 363, 512 430 / 492; 16 of 512 x 2048 from 256 24.1 / 23.9, 2048 80 / 96; 192 tiles: eight of 768 x 2048 from 512 30.3 / 26.5, 2048 73 / 68);
 //  * 128 x 256, where pieces of both sides leave room in LDS for one workgroup a CU of either kind, if there are more of 128 x 128 than CUs: 16 experts of 2048 x 768 from 512 rows each, three and three pieces
-//    160, 128 x 128 231; eight of 1024 x 1024 from 32 rows 15.8 / 20.3; eight of 512 x 512 from 512 rows, three and two pieces 42.7 / 34.5;
+//    160, 128 x 128 231; eight of 1024 x 1024 from 32 rows 15.8 / 20.3; eight of 512 x 512 from 512 rows, three and two pieces 42.7 / 34.5.  Two workgroups a CU, the second when the first ends: 16 of 2048 x 1024, three and two pieces, from 512 rows each 170 (a workgroup an item 173, one a CU
+//    168), from 32 44.1 (48.8, 42.9), of 512 x 2048 with a fifth of 8192 rows in one 136.7 (136.9, 163.7);
 //  * 128 x 128 otherwise.
 template <int XQ, typename Y, int PX, bool VEC>
 static int launch_gradient(const GradientArgs &a, float *planes, hipStream_t s) {
@@ -504,7 +505,7 @@ static int launch_gradient(const GradientArgs &a, float *planes, hipStream_t s) 
         if (a.rows / a.E >= 256 && 5 * large >= 4 * CUS * rounds) return launch_shape<XQ, Y, PX, VEC, LargeTile>(a, s, CUS);
     }
     if constexpr (PX == 3 && pieces_of<Y> > 1)
-        if (tiles(128, 128) > CUS) return launch_shape<XQ, Y, PX, VEC, WideTile>(a, s);
+        if (tiles(128, 128) > CUS) return launch_shape<XQ, Y, PX, VEC, WideTile>(a, s, 2 * CUS);
     return launch_shape<XQ, Y, PX, VEC, SmallTile>(a, s);
 }
 template <int XQ, typename Y>
