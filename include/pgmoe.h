@@ -501,7 +501,7 @@ const char *pgmoe_expert_matmul_kernel_name(const pgmoe_fp8_rows *x, const pgmoe
  * Entry n = t * copies + j of row_of dev [T * copies] is the row of token t's copy j, as pgmoe_permute and pgmoe_group_rows give it (copies = k); entries
  * in [0, n_rows) are distinct, others are copies that were dropped: they write and add nothing.  Rows that no entry names are left as they were.
  * weight dev [T, copies] f32 | NULL (1 each).  Values have one of PGMOE_F32, BF16, F16 a matrix, rows stride >= d elements apart; arithmetic is in float32, rounded
- * once.  T * copies is below 2^26.  These calls need no context, allocate nothing and may be captured into a HIP graph, like those above. */
+ * once.  T * copies is at most 2^26 - 4.  These calls need no context, allocate nothing and may be captured into a HIP graph, like those above. */
 /* rows[row_of[t, j]] = weight[t, j] * x[t], as values, as codes (rows_q: n_rows x d) or both; either may be NULL.
  *   x dev [T, d]    rows dev [n_rows, d] out */
 int pgmoe_dispatch_rows(const void *x, int64_t x_stride, int x_dtype, int T, int d, const int32_t *row_of, int copies,

@@ -251,7 +251,7 @@ static int check_deal(int T, int d, int copies, int n_rows, const char *fn) {
     if (T < 0 || copies < 1) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d, copies=%d: 0 and 1 at least", fn, T, copies);
     if (d < 1 || d > FP8_COLS_MAX) return fail(nullptr, PGMOE_EINVAL, "%s: d=%d outside 1..%d", fn, d, FP8_COLS_MAX);
     if (n_rows < 0) return fail(nullptr, PGMOE_EINVAL, "%s: n_rows=%d is negative", fn, n_rows);
-    if ((int64_t)T * copies * 64 > GRID_THREADS_MAX - 255) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d tokens by copies=%d are more than one launch holds", fn, T, copies);
+    if ((int64_t)T * copies > (GRID_THREADS_MAX - 255) / 64) return fail(nullptr, PGMOE_EINVAL, "%s: T=%d tokens by copies=%d are more than one launch holds", fn, T, copies);
     return PGMOE_OK;
 }
 static int check_codes(const pgmoe_fp8_rows *q, int rows, int cols, const char *fn, const char *what) {

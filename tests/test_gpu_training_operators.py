@@ -517,6 +517,69 @@ def test_dispatch_and_combine_with_offsets_that_pass_32_bits(B):
     near(d_w[:, 0], (xs * xs).sum(1), 17 * H * (xs * xs).sum(1), "f32")
 
 
+@pytest.mark.parametrize("at,width", [(1, 140), (3, 151), (8, 160), (4, 148)])
+@pytest.mark.parametrize("kind", DTYPES)
+def test_rows_inside_wider_buffers(B, kind, at, width):
+    """Rows of every call at addresses that nothing but the type aligns: the bits of rows that lie side by side, and neighbours stay as they are."""
+    say("strides", kind, at, width)
+    g = np.random.default_rng(at)
+    T, k, d = 1100, 2, 131 if at % 2 else 136
+    row_of, R = entries(g, T, k, dropped=100)
+    of, w = ints(row_of), dev(g.random((T, k)))
+
+    def wide(t):
+        b = torch.full((t.shape[0], width), float("nan"), device="cuda").to(t.dtype)
+        b[:, at:at + d] = t
+        return b[:, at:at + d], b
+
+    def alike(view, buffer, want):
+        torch.cuda.synchronize()
+        assert torch.equal(view, want)
+        buffer[:, at:at + d] = float("nan")
+        assert torch.isnan(buffer).all()
+    x, rows = dev(g.standard_normal((T, d)), kind), dev(g.standard_normal((R, d)), kind)
+    h = torch.from_numpy(g.integers(0, 256, (R, 256)).astype(np.uint8)).cuda().view(torch.float8_e4m3fn)
+    (xw, _), (rw, _) = wide(x), wide(rows)
+    for q_kind in (None, "e5m2"):
+        codes = lambda: codes_for(R, d, q_kind) if q_kind else (None, None)  # noqa: E731
+        same = lambda a, b: q_kind is None or (torch.equal(a[0].view(torch.uint8), b[0].view(torch.uint8)) and torch.equal(a[1], b[1]))  # noqa: E731
+        for call in (lambda x, r, o, c: B.dispatch_rows(x, of, o, *c, weight=w), lambda x, r, o, c: B.relu_backward(r, h, o, *c)):
+            out, c, cw = torch.full_like(rows, 7.0), codes(), codes()
+            call(x, rows, out, c)
+            o, buffer = wide(torch.full_like(rows, 7.0))
+            call(xw, rw, o, cw)
+            alike(o, buffer, out)
+            assert same(c, cw)
+        out, c, cw, d_w, d_ww = torch.full_like(rows, 7.0), codes(), codes(), torch.zeros(T, k, device="cuda"), torch.ones(T, k, device="cuda")
+        B.combine_rows_backward(x, rows, of, w, out, d_w, *c)
+        o, buffer = wide(torch.full_like(rows, 7.0))
+        B.combine_rows_backward(xw, rw, of, w, o, d_ww, *cw)
+        alike(o, buffer, out)
+        assert same(c, cw) and torch.equal(d_w, d_ww)
+    out = torch.full_like(x, 7.0)
+    B.combine_rows(rows, of, out, w, x)
+    o, buffer = wide(torch.full_like(x, 7.0))
+    B.combine_rows(rw, of, o, w, xw)
+    alike(o, buffer, out)
+
+
+def test_first_call_of_a_kernel_inside_a_capture(B):
+    """A kernel with more LDS than a launch gets by itself, run for the first time in this process while a graph is captured."""
+    say("first call captured")
+    p = Gradient(B, [3, 0, 40], 130, 100, "e5m2", "f32", False)
+    d_w = torch.zeros(3, 130, 100, device="cuda")
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        B.expert_weight_gradient(p.x_q, p.x_scale, p.d_y, p.offsets, d_w, stream=stream)
+    for _ in range(3):
+        d_w.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(d_w, p.run("f32"))
+    del graph
+
+
 # ------------------------------------------------------------------------------------ together
 @pytest.fixture(scope="module")
 def example():

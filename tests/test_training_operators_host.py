@@ -45,7 +45,7 @@ def call(which, **kw):
 
 BAD = [
     ("dispatch", dict(T=-1), "T=-1"), ("dispatch", dict(copies=0), "copies=0"), ("dispatch", dict(d=0), "d=0"), ("dispatch", dict(d=(1 << 22) + 1), "d="),
-    ("dispatch", dict(n_rows=-1), "n_rows"), ("dispatch", dict(T=1 << 25, copies=2), "launch"), ("dispatch", dict(x_dtype=B.E4M3), "x_dtype"),
+    ("dispatch", dict(n_rows=-1), "n_rows"), ("dispatch", dict(T=1 << 25, copies=2), "launch"), ("dispatch", dict(T=(1 << 31) - 1, copies=(1 << 31) - 1), "launch"), ("dispatch", dict(T=(1 << 26) - 3, copies=1), "launch"), ("dispatch", dict(x_dtype=B.E4M3), "x_dtype"),
     ("dispatch", dict(rows_dtype=9), "rows_dtype"), ("dispatch", dict(x=None), "x is NULL"), ("dispatch", dict(x=P + 1), "x is not"), ("dispatch", dict(x_stride=199), "x has rows"),
     ("dispatch", dict(rows=P + 2), "rows is not"), ("dispatch", dict(rows_stride=199), "rows has rows"), ("dispatch", dict(row_of=None), "row_of is NULL"),
     ("dispatch", dict(row_of=P + 2), "row_of"), ("dispatch", dict(weight=P + 2), "weight"), ("dispatch", dict(rows=None, q=None), "both"),
