@@ -91,11 +91,12 @@ __device__ inline void open_codes(intx2 codes, float scale, intx4 (&to)[PIECES])
 __device__ inline shortx4 read_transposed(const char *at) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4 *)at);
 }
-// The operand of a lane: column lane % 16 and eight of 32 rows.  Which rows a lane takes is free as long as both operands agree: 4 * (lane / 16) ..
-// and 16 + 4 * (lane / 16) ..
-__device__ inline bf16x8 operand_of(const char *tile, int stride, int lane) {
-    const char *at = tile + (size_t)((lane >> 4) * 4 + (lane >> 2 & 3)) * stride + (lane & 3) * 8;
-    const shortx4 low = read_transposed(at), high = read_transposed(at + 16 * stride);
+// An operand of 16 columns and 32 rows: of 64 neighbouring columns tile t of four takes 4 t .. 4 t + 3 of each 16.  Which rows a lane takes is free as long as
+// both operands agree: quarters of a wavefront start at rows 0, 16, 4 and 20, and go on eight rows further down.  With rows 8 bytes past a multiple
+// of 256 apart the 32 pieces of 8 bytes that half a wavefront reads at once lie in different banks.
+__device__ inline bf16x8 operand_of(const char *columns, int t, int stride, int lane) {
+    const char *at = columns + (size_t)((lane >> 4 & 1) * 16 + (lane >> 5) * 4 + (lane >> 2 & 3)) * stride + (lane & 3) * 32 + t * 8;
+    const shortx4 low = read_transposed(at), high = read_transposed(at + 8 * stride);
     typedef short shortx8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8, shortx8{low[0], low[1], low[2], low[3], high[0], high[1], high[2], high[3]});
 }
@@ -103,96 +104,78 @@ __device__ inline bf16x8 operand_of(const char *tile, int stride, int lane) {
 template <typename Y>
 constexpr int pieces_of = sizeof(Y) == 4 ? 3 : std::is_same<Y, __bf16>::value ? 1 : 2;
 
-// Results of a wavefront's NI x 4 tiles from input `in` and output `out` on.  Gradients were the first operand: a lane's four results of a product are neighbouring
-// outputs of one input.  They leave in whole lines, past the caches, which then keep the rows: 128 bytes of each of eight inputs at once (16 bytes a lane in 64 bytes of
-// each of 16 inputs: 1024 x 4096 float32 for each of 64 experts from 32768 rows 503 us, whole lines 460).  VEC: 16 bytes of results are all there or none.
-template <typename W, int NI>
-__device__ inline void store_lines(const GradientArgs &a, int e, int in, int out, int lane, floatx4 (&acc)[NI][4]) {
-    constexpr int UNITS = sizeof(W) == 4 ? 4 : 2;  // of 64 bytes a row: a tile, or two
+// Where a lane's results acc[i][o][r] of a wavefront's NI x 4 tiles are: input 64 (i / 4) + 16 (lane / 16) + 4 (i % 4) + r, output 16 (lane % 16 / 4) + 4 o + lane % 4.
+__device__ inline int input_of(int i, int r, int lane) { return (i >> 2) * 64 + (lane >> 4) * 16 + (i & 3) * 4 + r; }
+
+// Lane t of four has v[o], o = 0 .. 3, and gets v[t] of lane o in o.
+__device__ inline intx4 transpose_quad(intx4 v, int lane) {
+    const bool odd = lane & 1, upper = lane & 2;
+    intx4 w, x;
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {  // with lane t ^ 1
+        const int got = __builtin_amdgcn_update_dpp(0, v[o ^ 1], 0xb1, 0xf, 0xf, true);
+        w[o] = odd == (o & 1) ? v[o] : got;
+    }
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {  // with lane t ^ 2
+        const int got = __builtin_amdgcn_update_dpp(0, w[o ^ 2], 0x4e, 0xf, 0xf, true);
+        x[o] = upper == (o >> 1) ? w[o] : got;
+    }
+    return x;
+}
+// Four lanes exchange their results of four tiles, so that neighbouring lanes store neighbouring 16 bytes, 256 of each of four inputs at once, past the caches, which then keep
+// the rows.  A CU gets 118 GB/s out that way, and 37 if neighbouring lanes store 16 bytes of different inputs, whole lines or not (1024 x 4096 float32 for each of 64 experts
+// from 32768 rows: 440, now 415 us).  VEC: 16 bytes of results are all there or none.
+template <typename W, bool ADD, int NI>
+__device__ __forceinline__ void store_rows(const GradientArgs &a, int e, int in, int out, int lane, const floatx4 (&acc)[NI][4]) {
     typedef W Wx4 __attribute__((ext_vector_type(4)));
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));  // worked out again: what depends on it is not kept in registers across the products
-    const bool up = lane & 8;
-    const int g = lane >> 4;
-    constexpr int AT_ONCE = NI == 8 ? 2 : 1;  // of the 16-input tiles whose float32 addends are requested together, as far as registers go
-    floatx4 addend[AT_ONCE][4];
+    const int col = out + (lane & 15) * 4;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-        if constexpr (sizeof(W) == 4)
-            if (a.add && i % AT_ONCE == 0) {
+        Wx4 addend[4];
+        if constexpr (ADD) {
 #pragma unroll
-                for (int n = 0; n < AT_ONCE * 4; ++n) {
-                    const int row = in + (i + n / 4) * 16 + (lane & 7) + (n & 1) * 8, col = out + ((n & 2) + (up ? 1 : 0)) * 16 + 4 * g;
-                    if (row < a.n_in && col < a.n_out) addend[n / 4][n & 3] = *reinterpret_cast<const floatx4 *>(reinterpret_cast<const float *>(a.add) + ((size_t)e * a.n_in + row) * a.n_out + col);
-                }
-            }
-        intx4 unit[UNITS];
-        if constexpr (sizeof(W) == 4) {
-#pragma unroll
-            for (int o = 0; o < 4; ++o) unit[o] = __builtin_bit_cast(intx4, acc[i][o]);
-        } else {
-            const int row = in + i * 16 + (lane & 15);
-#pragma unroll
-            for (int o = 0; o < 4; ++o) {
-                const int col = out + o * 16 + 4 * g;
-                if (a.add && row < a.n_in && col < a.n_out) {
-                    const Wx4 u = *reinterpret_cast<const Wx4 *>(reinterpret_cast<const W *>(a.add) + ((size_t)e * a.n_in + row) * a.n_out + col);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][o][j] += (float)u[j];
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {  // odd and even quarters of the wavefront swap two tiles' halves: a lane then has eight neighbours
-                const intx2 p = __builtin_bit_cast(intx2, Wx4{(W)acc[i][2 * u][0], (W)acc[i][2 * u][1], (W)acc[i][2 * u][2], (W)acc[i][2 * u][3]});
-                const intx2 q = __builtin_bit_cast(intx2, Wx4{(W)acc[i][2 * u + 1][0], (W)acc[i][2 * u + 1][1], (W)acc[i][2 * u + 1][2], (W)acc[i][2 * u + 1][3]});
-                const auto x = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false), y = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
-                unit[u] = intx4{(int)x[0], (int)y[0], (int)x[1], (int)y[1]};
-            }
+            for (int r = 0; r < 4; ++r)
+                addend[r] = *reinterpret_cast<const Wx4 *>(reinterpret_cast<const W *>(a.add) + ((size_t)e * a.n_in + min(in + input_of(i, r, lane), a.n_in - 1)) * a.n_out + min(col, a.n_out - 4));
         }
 #pragma unroll
-        for (int u = 0; u < UNITS; u += 2) {  // the upper eight inputs of a unit for the lower eight of the next
-            intx4 low, high;
+        for (int r = 0; r < 4; ++r) {
+            floatx4 v = __builtin_bit_cast(floatx4, transpose_quad(__builtin_bit_cast(intx4, floatx4{acc[i][0][r], acc[i][1][r], acc[i][2][r], acc[i][3][r]}), lane));
+            if constexpr (ADD) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int got = __builtin_amdgcn_update_dpp(0, up ? unit[u][j] : unit[u + 1][j], 0x128, 0xf, 0xf, true);  // row_ror:8
-                low[j] = up ? got : unit[u][j];
-                high[j] = up ? unit[u + 1][j] : got;
+                for (int j = 0; j < 4; ++j) v[j] += (float)addend[r][j];
+                asm volatile("" : "+v"(v));  // added up here, not where a store may be left out: the compiler else takes addends for on their way, and waits for results for safety
             }
-            const int col = out + (sizeof(W) == 4 ? (u + (up ? 1 : 0)) * 16 + 4 * g : (u + (up ? 1 : 0)) * 32 + (g & 1) * 16 + (g >> 1) * 8);
-            const int row = in + i * 16 + (lane & 7);
-            const size_t at = ((size_t)e * a.n_in + row) * a.n_out + col;
-            auto put = [&](intx4 v, int r, size_t at, int n) {
-                if (r >= a.n_in || col >= a.n_out) return;
-                if constexpr (sizeof(W) == 4)
-                    if (a.add) v = __builtin_bit_cast(intx4, __builtin_bit_cast(floatx4, v) + addend[i % AT_ONCE][n]);
-                intx4 *to = reinterpret_cast<intx4 *>(reinterpret_cast<W *>(a.d_w) + at);
-                if (a.parts == 1) __builtin_nontemporal_store(v, to);
-                else *to = v;  // gradient_parts_kernel reads it at once
-            };
-            put(low, row, at, u);
-            put(high, row + 8, at + (size_t)8 * a.n_out, u + 1);
+            const int row = in + input_of(i, r, lane);
+            if (row >= a.n_in || col >= a.n_out) continue;
+            const Wx4 w = {(W)v[0], (W)v[1], (W)v[2], (W)v[3]};
+            Wx4 *to = reinterpret_cast<Wx4 *>(reinterpret_cast<W *>(a.d_w) + ((size_t)e * a.n_in + row) * a.n_out + col);
+            if (a.parts == 1) __builtin_nontemporal_store(w, to);
+            else *to = w;  // gradient_parts_kernel reads it at once
         }
     }
 }
 template <typename W, int NI>
-__device__ inline void store_singly(const GradientArgs &a, int e, int in, int out, int lane, const floatx4 (&acc)[NI][4]) {
+__device__ __forceinline__ void store_singly(const GradientArgs &a, int e, int in, int out, int lane, const floatx4 (&acc)[NI][4]) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const int row = in + i * 16 + (lane & 15);
-        if (row >= a.n_in) continue;
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int o = 0; o < 4; ++o) {
-            const int col = out + o * 16 + 4 * (lane >> 4);
-            const size_t at = ((size_t)e * a.n_in + row) * a.n_out + col;
+        for (int r = 0; r < 4; ++r) {
+            const int row = in + input_of(i, r, lane);
+            if (row >= a.n_in) continue;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (col + j < a.n_out) reinterpret_cast<W *>(a.d_w)[at + j] = (W)(a.add ? acc[i][o][j] + (float)reinterpret_cast<const W *>(a.add)[at + j] : acc[i][o][j]);
+            for (int o = 0; o < 4; ++o) {
+                const int col = out + (lane & 12) * 4 + 4 * o + (lane & 3);
+                const size_t at = ((size_t)e * a.n_in + row) * a.n_out + col;
+                if (col < a.n_out) reinterpret_cast<W *>(a.d_w)[at] = (W)(a.add ? acc[i][o][r] + (float)reinterpret_cast<const W *>(a.add)[at] : acc[i][o][r]);
+            }
         }
-    }
 }
 template <bool VEC, int NI>
-__device__ inline void store_gradient(const GradientArgs &a, int e, int in, int out, int lane, floatx4 (&acc)[NI][4]) {
+__device__ __forceinline__ void store_gradient(const GradientArgs &a, int e, int in, int out, int lane, const floatx4 (&acc)[NI][4]) {
     auto finish = [&](auto type) {
-        if constexpr (VEC) store_lines<decltype(type)>(a, e, in, out, lane, acc);
+        if constexpr (VEC) a.add ? store_rows<decltype(type), true>(a, e, in, out, lane, acc) : store_rows<decltype(type), false>(a, e, in, out, lane, acc);
         else store_singly<decltype(type)>(a, e, in, out, lane, acc);
     };
     if (a.dtype == PGMOE_F32) finish(float());
@@ -214,13 +197,14 @@ __device__ inline GradientItem gradient_item(const GradientArgs &a, int i) {
 
 // An item is BI inputs by BO outputs; a workgroup takes every gridDim-th of them and goes through its rows K at a time.  Both sides come through registers, where codes are converted,
 // into one of two buffers in LDS while the other is multiplied, also from one item to the next: the first rows of an item arrive under the last products of the one before.
-// Rows in LDS have 32 bytes more behind them than their columns: the eight rows of 32 bytes that half a wavefront reads at once then lie in different banks.
+// Bound by the products on many rows, 1.12 PFLOP/s (each further 512 rows for each of 64 experts of 1024 x 4096: 246 us), and by the results on few: their float32 leave at 5.5 TB/s, about
+// 160 us of the 426 that 512 rows an expert take, mostly not under the products (workgroups started at different times gained nothing). Without loads the same call takes 340, without stores 270.
 template <int WI_, int WO_, int NI_, int K_>
 struct GradientShape {
     static constexpr int WI = WI_, WO = WO_, NI = NI_, NO = 4, K = K_;  // wavefronts; 16 x 16 tiles of one
     static constexpr int BI = WI * NI * 16, BO = WO * NO * 16, THREADS = WI * WO * 64;
     // a thread brings XP and YP pieces of eight columns of rows that lie XR and YR apart; bytes from one row to the next in LDS
-    static constexpr int XR = THREADS * 8 / BI, YR = THREADS * 8 / BO, XP = K / XR, YP = K / YR, XS = 2 * BI + 32, YS = 2 * BO + 32;
+    static constexpr int XR = THREADS * 8 / BI, YR = THREADS * 8 / BO, XP = K / XR, YP = K / YR, XS = 2 * BI + 8, YS = 2 * BO + 8;
     static_assert(BI % 128 == 0 && BO % 128 == 0 && XP * XR == K && YP * YR == K && K % 32 == 0, "whole pieces");
     static constexpr int buffer(int px, int py) { return K * (px * XS + py * YS); }
     // wavefronts a SIMD: of small tiles with few pieces four workgroups fit into a CU
@@ -237,12 +221,14 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
         GradientItem at;
         int first, rows;  // of d_y and x
     };
+    // the expert's offsets by scalar loads: a vector load would wait for the results of the item before
+    const auto *offsets = (const __attribute__((address_space(4))) int32_t *)a.offsets;
     auto find = [&](int &i, Item &it) {  // the item at number i or the next of this workgroup behind it -> is there one?
         for (;; i += gridDim.x) {
             it.at = gradient_item(a, i);
             if (it.at.e >= a.E) return false;
             if (it.at.ti >= a.tiles_in || it.at.to >= a.tiles_out) continue;
-            const int lo = max(0, min(a.offsets[it.at.e], a.rows)), n = max(lo, min(a.offsets[it.at.e + 1], a.rows)) - lo;
+            const int lo = max(0, min(offsets[it.at.e], a.rows)), n = max(lo, min(offsets[it.at.e + 1], a.rows)) - lo;
             if (a.parts == 1) {
                 it.first = lo;
                 it.rows = n;
@@ -305,6 +291,10 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
     int buffer = 0;
     auto keep = [&](int at) {
         char *to = lds + at * BUFFER;
+        auto put = [](char *to, intx4 v) {  // 8-byte aligned
+            reinterpret_cast<intx2 *>(to)[0] = intx2{v[0], v[1]};
+            reinterpret_cast<intx2 *>(to)[1] = intx2{v[2], v[3]};
+        };
         const intx4 none = {0, 0, 0, 0};  // rows behind the last are zero on both sides, whatever the last one holds
 #pragma unroll
         for (int i = 0; i < S::XP; ++i) {
@@ -312,7 +302,7 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
             intx4 px[PX];
             open_codes<XQ, PX>(codes[i], scale[i], px);
 #pragma unroll
-            for (int p = 0; p < PX; ++p) *reinterpret_cast<intx4 *>(to + p * XPLANE + r * S::XS + x_piece * 16) = r < requested ? px[p] : none;
+            for (int p = 0; p < PX; ++p) put(to + p * XPLANE + r * S::XS + x_piece * 16, r < requested ? px[p] : none);
         }
 #pragma unroll
         for (int i = 0; i < S::YP; ++i) {
@@ -327,7 +317,7 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
                 take_apart<PY>(v, py);
             }
 #pragma unroll
-            for (int p = 0; p < PY; ++p) *reinterpret_cast<intx4 *>(to + PX * XPLANE + p * YPLANE + r * S::YS + y_piece * 16) = r < requested ? py[p] : none;
+            for (int p = 0; p < PY; ++p) put(to + PX * XPLANE + p * YPLANE + r * S::YS + y_piece * 16, r < requested ? py[p] : none);
         }
     };
     // Gradients are the first operand: a lane's four results of a product are neighbouring outputs of one input.
@@ -340,19 +330,19 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
 #pragma unroll
             for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-                for (int p = 0; p < PX; ++p) px[i][p] = operand_of(now + p * XPLANE + k * S::XS + (wi * S::NI + i) * 32, S::XS, lane);
+                for (int p = 0; p < PX; ++p) px[i][p] = operand_of(now + p * XPLANE + k * S::XS + (wi * S::NI + i / 4 * 4) * 32, i % 4, S::XS, lane);
 #pragma unroll
             for (int o = 0; o < S::NO; ++o) {
                 bf16x8 py[PY];
 #pragma unroll
-                for (int p = 0; p < PY; ++p) py[p] = operand_of(now + PX * XPLANE + p * YPLANE + k * S::YS + (wo * S::NO + o) * 32, S::YS, lane);
+                for (int p = 0; p < PY; ++p) py[p] = operand_of(now + PX * XPLANE + p * YPLANE + k * S::YS + wo * S::NO * 32, o, S::YS, lane);
                 // small products first
                 static_for<KEPT>([&](auto s_) {
                     static_for<PY>([&](auto p_) {
                         constexpr int s = KEPT - 1 - decltype(s_)::value, p = decltype(p_)::value;
                         if constexpr (s >= p && s - p < PX) {
 #pragma unroll
-                            for (int i = 0; i < S::NI; ++i) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(py[p], px[i][s - p], acc[i][o], 0, 0, 0);
+                            for (int i = 0; i < S::NI; ++i) acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(px[i][s - p], py[p], acc[i][o], 0, 0, 0);
                         }
                     });
                 });
@@ -377,14 +367,15 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
             for (int o = 0; o < S::NO; ++o) acc[x][o] = floatx4{0.f, 0.f, 0.f, 0.f};
         for (int rows = it.rows; rows > 0; rows -= S::K) {
             lds_barrier();  // these rows are there for everyone, and everyone has read the ones before
-            const bool last = rows <= S::K, any = !last || (more && next.rows > 0);
-            if (last && any) open(next);
-            if (any) request();
+            // Requested in any case, behind the last rows the item's own once more: the compiler then knows what is on its way, and does not wait for an item's results for
+            // safety (with the offsets by scalar loads 450 to 440 us, 64 experts of 1024 x 4096 from 32768 rows).
+            if (rows <= S::K) open(more && next.rows > 0 ? next : it);
+            request();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);  // before another wavefront's conversions: 2 to 4 %
             multiply(buffer);
             __builtin_amdgcn_s_setprio(0);
-            if (any) keep(buffer ^ 1);
+            keep(buffer ^ 1);
             buffer ^= 1;
         }
         if (it.rows == 0 && more && next.rows > 0) {
@@ -462,10 +453,10 @@ static int launch_shape(GradientArgs a, hipStream_t s, int64_t most = 0) {  // m
     hipLaunchKernelGGL((weight_gradient_kernel<XQ, Y, PX, VEC, S>), dim3((unsigned)grid), dim3(S::THREADS), LDS, s, a);
     return PGMOE_OK;
 }
-// Into how many parts the rows of each expert are split where there are fewer tiles than workgroups run at once.  A tile by itself takes 18.5 ns a row; parts cost two more
-// launches' overhead and a write and a read of 64 KiB each at 3 TB/s.  us without parts / with as many as this says, bfloat16 gradients: one expert of 512 x 1024 from 512 rows 13.9 (2 parts
-// would take 14.7), 1024 21.5 / 18.1, 4096 81 / 26, 16384 303 / 40; one of 1024 x 4096 from 1024 rows 26.7 (2: 31.0), 4096 81 / 60; eight of 512 x 512 from 512 rows each
-// 15.0 (2: 19.2), 2048 44 / 29; eight of 1024 x 1024 from 4096 each 93 (2: 142).
+// Into how many parts the rows of each expert are split where there are fewer tiles than workgroups run at once.  A tile by itself takes 17 to 18.5 ns a row; parts cost two more
+// launches' overhead and a write and a read of 64 KiB each at 3 TB/s.  us without parts / with as many as this says, bfloat16 gradients: one expert of 512 x 1024 from 512 rows 12.7 (2 parts
+// would take 14.1), 1024 19.9 / 17.3, 4096 74 / 25, 16384 279 / 40; one of 1024 x 4096 from 1024 rows 25.4 (2: 29.7), 4096 76 / 59; eight of 512 x 512 from 512 rows each
+// 14.0 (2: 18.4), 2048 41 / 29; eight of 1024 x 1024 from 4096 each 93 to 97 (2: 91).
 constexpr int GRADIENT_PARTS = 16, CUS = 256;
 static int gradient_parts(int rows, int E, int n_in, int n_out) {
     const int64_t tiles = (int64_t)E * fp8_blocks(n_in) * fp8_blocks(n_out);
@@ -490,11 +481,11 @@ static int launch_parts(const GradientArgs &a, float *planes, hipStream_t s) {
     return PGMOE_OK;
 }
 // Which tiles (us, bfloat16 gradients with scales that are powers of two unless said otherwise, float32 results):
-//  * 256 x 256, one workgroup a CU: from 256 rows an expert on the mean on, if the last round of a tile for each CU leaves at most a fifth of them idle (64 experts of 1024 x 4096 from 64 rows each 232, 128 x 128
-//    214, 256 rows 325 / 363, 512 430 / 492; 16 of 512 x 2048 from 256 24.1 / 23.9, 2048 80 / 96; 192 tiles: eight of 768 x 2048 from 512 30.3 / 26.5, 2048 73 / 68);
-//  * 128 x 256, where pieces of both sides leave room in LDS for one workgroup a CU of either kind, if there are more of 128 x 128 than CUs: 16 experts of 2048 x 768 from 512 rows each, three and three pieces
-//    160, 128 x 128 231; eight of 1024 x 1024 from 32 rows 15.8 / 20.3; eight of 512 x 512 from 512 rows, three and two pieces 42.7 / 34.5.  Two workgroups a CU, the second when the first ends: 16 of 2048 x 1024, three and two pieces, from 512 rows each 170 (a workgroup an item 173, one a CU
-//    168), from 32 44.1 (48.8, 42.9), of 512 x 2048 with a fifth of 8192 rows in one 136.7 (136.9, 163.7);
+//  * 256 x 256, one workgroup a CU: from 256 rows an expert on the mean on, if the last round of a tile for each CU leaves at most a fifth of them idle (64 experts of 1024 x 4096 from 64 rows each 228, 128 x 128
+//    219, 256 rows 303 / 370, 512 426 / 493; 16 of 512 x 2048 from 256 24.5 / 22.8, 2048 80 / 99; 192 tiles: eight of 768 x 2048 from 512 28.2 / 24.8, 2048 68 / 65);
+//  * 128 x 256, one workgroup a CU, where pieces of both sides leave room in LDS for no more, if there are more of 128 x 128 than CUs: 16 experts of 2048 x 768 from 512 rows each, three and three pieces
+//    153, 128 x 128 234; eight of 1024 x 1024 from 32 rows 16.0 / 21.6; eight of 512 x 512 from 512 rows, three and two pieces 44 / 36.  Against two workgroups a CU, the second when the first ends, and one
+//    an item: 16 of 2048 x 1024, three and two pieces, from 512 rows each 179 / 188 / 181, from 32 36.6 / 38.9 / 45.3, with a fifth of 8192 rows in one 236.4 / 236.5 / 240.5;
 //  * 128 x 128 otherwise.
 template <int XQ, typename Y, int PX, bool VEC>
 static int launch_gradient(const GradientArgs &a, float *planes, hipStream_t s) {
@@ -505,7 +496,7 @@ static int launch_gradient(const GradientArgs &a, float *planes, hipStream_t s) 
         if (a.rows / a.E >= 256 && 5 * large >= 4 * CUS * rounds) return launch_shape<XQ, Y, PX, VEC, LargeTile>(a, s, CUS);
     }
     if constexpr (PX == 3 && pieces_of<Y> > 1)
-        if (tiles(128, 128) > CUS) return launch_shape<XQ, Y, PX, VEC, WideTile>(a, s, 2 * CUS);
+        if (tiles(128, 128) > CUS) return launch_shape<XQ, Y, PX, VEC, WideTile>(a, s, CUS);
     return launch_shape<XQ, Y, PX, VEC, SmallTile>(a, s);
 }
 template <int XQ, typename Y>
