@@ -27,6 +27,7 @@ struct GradientArgs {
     int dtype;  // of d_w and add
     int parts;  // an expert's rows are split into: each writes a float32 plane of its own to d_w, [parts][E][n_in][n_out]
     int tiles_in, tiles_out, group_in, group_out;
+    bool sorted;  // items of experts with many rows first, one a workgroup
 };
 
 // The steps of part `part` of an expert's `steps`: none for some parts if there are few.
@@ -205,7 +206,7 @@ struct GradientShape {
     static constexpr int BI = WI * NI * 16, BO = WO * NO * 16, THREADS = WI * WO * 64;
     // a thread brings XP and YP pieces of eight columns of rows that lie XR and YR apart; bytes from one row to the next in LDS
     static constexpr int XR = THREADS * 8 / BI, YR = THREADS * 8 / BO, XP = K / XR, YP = K / YR, XS = 2 * BI + 8, YS = 2 * BO + 8;
-    static_assert(BI % 128 == 0 && BO % 128 == 0 && XP * XR == K && YP * YR == K && K % 32 == 0, "whole pieces");
+    static_assert(THREADS >= PGMOE_MAX_EXPERTS && BI % 128 == 0 && BO % 128 == 0 && XP * XR == K && YP * YR == K && K % 32 == 0, "whole pieces");
     static constexpr int buffer(int px, int py) { return K * (px * XS + py * YS); }
     // wavefronts a SIMD: of small tiles with few pieces four workgroups fit into a CU
     static constexpr int waves(int px, int py) { return THREADS == 256 && px * py == 1 ? 4 : THREADS == 256 && px * py < 4 ? 3 : 2; }
@@ -223,11 +224,27 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
     };
     // the expert's offsets by scalar loads: a vector load would wait for the results of the item before
     const auto *offsets = (const __attribute__((address_space(4))) int32_t *)a.offsets;
+    int expert = 0;
+    if (a.sorted) {  // which expert has as many rows that the item's number says?  (uniform)
+        const int place = gradient_item(a, blockIdx.x).e;
+        int *rows = reinterpret_cast<int *>(lds), t = threadIdx.x;
+        if (t < a.E) rows[t] = offsets[t + 1] - offsets[t];
+        lds_barrier();
+        if (t < a.E) {
+            int before = 0;
+            for (int j = 0; j < a.E; ++j) before += rows[j] > rows[t] || (rows[j] == rows[t] && j < t);
+            if (before == place) rows[a.E] = t;
+        }
+        lds_barrier();
+        expert = __builtin_amdgcn_readfirstlane(place < a.E ? rows[a.E] : 0);
+        lds_barrier();
+    }
     auto find = [&](int &i, Item &it) {  // the item at number i or the next of this workgroup behind it -> is there one?
         for (;; i += gridDim.x) {
             it.at = gradient_item(a, i);
             if (it.at.e >= a.E) return false;
             if (it.at.ti >= a.tiles_in || it.at.to >= a.tiles_out) continue;
+            if (a.sorted) it.at.e = expert;
             const int lo = max(0, min(offsets[it.at.e], a.rows)), n = max(lo, min(offsets[it.at.e + 1], a.rows)) - lo;
             if (a.parts == 1) {
                 it.first = lo;
@@ -430,21 +447,26 @@ static int raise_lds(const void *kernel, int bytes, std::atomic<uint64_t> &raise
     }
     return PGMOE_OK;
 }
-// Tiles in groups of up to 1024 x 1024, as long as there are two for each die -> item numbers.
-static int64_t gradient_items(GradientArgs &a, int tile_in, int tile_out) {
+// Tiles in groups of up to 1024 x 1024, as long as there are two for each die -> item numbers.  With many products for what is read (`spread`) groups are up to 512 x 512 and all alike,
+// so that an expert of many rows is all dies'.
+static int64_t gradient_items(GradientArgs &a, int tile_in, int tile_out, bool spread) {
     a.tiles_in = (a.n_in + tile_in - 1) / tile_in;
     a.tiles_out = (a.n_out + tile_out - 1) / tile_out;
-    a.group_in = std::min(a.tiles_in, 1024 / tile_in);
-    a.group_out = std::min(a.tiles_out, 1024 / tile_out);
+    a.group_in = std::min(a.tiles_in, (spread ? 512 : 1024) / tile_in);
+    a.group_out = std::min(a.tiles_out, (spread ? 512 : 1024) / tile_out);
+    if (spread) {
+        while (a.tiles_in % a.group_in) --a.group_in;
+        while (a.tiles_out % a.group_out) --a.group_out;
+    }
     const auto groups = [&] { return (int64_t)a.E * a.parts * ((a.tiles_in + a.group_in - 1) / a.group_in) * ((a.tiles_out + a.group_out - 1) / a.group_out); };
     while (groups() < 16 && a.group_in * a.group_out > 1) (a.group_in > a.group_out ? a.group_in : a.group_out) = (std::max(a.group_in, a.group_out) + 1) / 2;
     return (groups() + 7) / 8 * 8 * a.group_in * a.group_out;
 }
 template <int XQ, typename Y, int PX, bool VEC, typename S>
-static int launch_shape(GradientArgs a, hipStream_t s, int64_t most = 0) {  // most: workgroups (0: one an item)
+static int launch_shape(GradientArgs a, hipStream_t s, int64_t most, bool spread) {  // most: workgroups (0: one an item)
     constexpr int LDS = 2 * S::buffer(PX, pieces_of<Y>);
     static std::atomic<uint64_t> raised{0};
-    int64_t grid = gradient_items(a, S::BI, S::BO);
+    int64_t grid = gradient_items(a, S::BI, S::BO, spread);
     if (grid * S::THREADS > GRID_THREADS_MAX)
         return fail(nullptr, PGMOE_EINVAL, "pgmoe_expert_weight_gradient: %d matrices of %d x %d are more than one launch holds", a.E, a.n_in, a.n_out);
     if (most) grid = std::min(grid, most);
@@ -471,7 +493,7 @@ static int launch_parts(const GradientArgs &a, float *planes, hipStream_t s) {
     p.d_w = planes;
     p.add = nullptr;
     p.dtype = PGMOE_F32;
-    const int rc = launch_shape<XQ, Y, PX, VEC, SmallTile>(p, s);
+    const int rc = launch_shape<XQ, Y, PX, VEC, SmallTile>(p, s, 0, false);
     if (rc) return rc;
     const int64_t size = (int64_t)a.n_in * a.n_out;
     const dim3 grid((unsigned)((size / (VEC ? 4 : 1) + 255) / 256), a.E);
@@ -487,17 +509,22 @@ static int launch_parts(const GradientArgs &a, float *planes, hipStream_t s) {
 //    153, 128 x 128 234; eight of 1024 x 1024 from 32 rows 16.0 / 21.6; eight of 512 x 512 from 512 rows, three and two pieces 44 / 36.  Against two workgroups a CU, the second when the first ends, and one
 //    an item: 16 of 2048 x 1024, three and two pieces, from 512 rows each 179 / 188 / 181, from 32 36.6 / 38.9 / 45.3, with a fifth of 8192 rows in one 236.4 / 236.5 / 240.5;
 //  * 128 x 128 otherwise.
+// And in which order, of the two smaller ones: from 256 rows an expert on the mean on, and if not all items run at once, those of experts with many rows first, one a workgroup, of which the next goes where one has ended
+// (`sorted`; in order / sorted, rows dealt out evenly, and with nearly a quarter in one of 16: 8192 rows for 16 experts of 2048 x 1024, three and two pieces, 167 / 173 and 257 / 190; for 32 of 1024 x 1024 95 / 107 and 157 / 115;
+// 4096 for 16 of 768 x 2048, one piece, 28.6 / 30.4 and 44 / 33).
 template <int XQ, typename Y, int PX, bool VEC>
-static int launch_gradient(const GradientArgs &a, float *planes, hipStream_t s) {
+static int launch_gradient(GradientArgs a, float *planes, hipStream_t s) {
     if (a.parts > 1) return launch_parts<XQ, Y, PX, VEC>(a, planes, s);
     const auto tiles = [&](int in, int out) { return (int64_t)a.E * ((a.n_in + in - 1) / in) * ((a.n_out + out - 1) / out); };
     if constexpr (PX * pieces_of<Y> == 1 && VEC) {
         const int64_t large = tiles(256, 256), rounds = (large + CUS - 1) / CUS;
-        if (a.rows / a.E >= 256 && 5 * large >= 4 * CUS * rounds) return launch_shape<XQ, Y, PX, VEC, LargeTile>(a, s, CUS);
+        if (a.rows / a.E >= 256 && 5 * large >= 4 * CUS * rounds) return launch_shape<XQ, Y, PX, VEC, LargeTile>(a, s, CUS, false);
     }
+    const int64_t small = tiles(128, 128);
+    a.sorted = a.rows / a.E >= 256 && (PX == 3 && pieces_of<Y> > 1 ? small > CUS : small > 4 * CUS);
     if constexpr (PX == 3 && pieces_of<Y> > 1)
-        if (tiles(128, 128) > CUS) return launch_shape<XQ, Y, PX, VEC, WideTile>(a, s, CUS);
-    return launch_shape<XQ, Y, PX, VEC, SmallTile>(a, s);
+        if (small > CUS) return launch_shape<XQ, Y, PX, VEC, WideTile>(a, s, a.sorted ? 0 : CUS, a.sorted);
+    return launch_shape<XQ, Y, PX, VEC, SmallTile>(a, s, 0, a.sorted && PX * pieces_of<Y> > 1);
 }
 template <int XQ, typename Y>
 static int launch_gradient(const GradientArgs &a, bool pow2, float *planes, hipStream_t s) {

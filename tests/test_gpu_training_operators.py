@@ -370,6 +370,18 @@ def test_expert_weight_gradient_of_ordinary_sizes(B, counts, n_in, n_out, y_kind
         p.check("f32", workspace=False)
 
 
+@pytest.mark.parametrize("counts,n_in,n_out,y_kind,pow2", [([0, 900, 900, 40, 0, 300], 1000, 1300, "f32", False), ([0, 900, 900, 40, 0, 300], 1000, 1304, "f16", False),
+                                                           ([5, 1500, 0, 1500, 64] + [100] * 7, 1040, 1304, "bf16", True), ([5, 1500, 0, 1500, 64] + [100] * 7, 1040, 1304, "bf16", False),
+                                                           ([2100] + [1] * 7, 1152, 1288, "f16", False)])
+def test_expert_weight_gradient_of_experts_of_very_different_size(B, counts, n_in, n_out, y_kind, pow2):
+    """Items go by how many rows an expert has: two have as many, some none; each matrix is its own expert's."""
+    say("gradient", counts[:6], n_in, n_out, y_kind, pow2)
+    p = Gradient(B, counts, n_in, n_out, "e4m3", y_kind, pow2)
+    got = p.check("f32")
+    assert torch.equal(got, p.run("f32"))
+    assert all(got[e].any() == (c > 0) for e, c in enumerate(counts))
+
+
 @pytest.mark.parametrize("out", DTYPES)
 @pytest.mark.parametrize("n_in,n_out", [(200, 136), (130, 77)])
 def test_expert_weight_gradient_is_added(B, out, n_in, n_out):
