@@ -398,10 +398,11 @@ def expert_matmul_kernel_name(rows, n_experts, n_in, n_out, y_dtype=BF16, q_stri
 
 
 # ---- training a block: rows there and back with weights, and the gradients
-def _entries(row_of, T, weight):
+def _entries(row_of, T, weight, d_weight=None):
     """row_of [T * copies] or [T, copies], weight [T, copies] -> (address of row_of, copies, address of weight)."""
     n = row_of.numel()
-    copies = n // T if T else 1
+    # of no tokens the entries do not say how many copies each has: the matrices do, or any number fits
+    copies = n // T if T else next((t.shape[1] for t in (weight, d_weight) if t is not None and t.dim() == 2), 1)
     if copies * T != n or (T and n == 0):
         raise ValueError(f"row_of has {n} entries for {T} tokens")
     return _expect(row_of, "row_of", row_of.shape, _i32), copies, None if weight is None else _expect(weight, "weight", (T, copies), _f32)
@@ -459,7 +460,7 @@ def combine_rows_backward(d_y, rows, row_of, weight=None, d_rows=None, d_weight=
     """Gradients of combine_rows(): d_rows[row_of[t, j]] = weight[t, j] * d_y[t], as values in the type of `rows`, as codes q, or both;
     d_weight[t, j] = <d_y[t], rows[row_of[t, j]]>, for which alone `rows` is needed (else it may be None)."""
     T, d = d_y.shape
-    of, copies, w = _entries(row_of, T, weight)
+    of, copies, w = _entries(row_of, T, weight, d_weight)
     given = [t for t in (rows, d_rows, q) if t is not None]
     if not given:
         raise ValueError("rows, d_rows and q are None")

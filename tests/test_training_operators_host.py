@@ -199,6 +199,30 @@ def test_binding_refuses_tensors_that_do_not_fit(monkeypatch, which, change, err
         go(**dict(tensors, **{k: v if v is None else v.as_subclass(OnGpu) for k, v in change.items()}), stream=0)
 
 
+@pytest.mark.parametrize("flat", [True, False])
+@pytest.mark.parametrize("k", [1, 2, 8])
+def test_binding_takes_a_batch_without_tokens(monkeypatch, k, flat):
+    """Weights and their gradients [0, k], as a batch of that router has them; matrices that do not fit each other are refused for it too."""
+    launched = []
+    for name in ("pgmoe_dispatch_rows", "pgmoe_combine_rows", "pgmoe_combine_rows_backward"):       # the library's own answer: it has nothing to launch
+        monkeypatch.setattr(B.lib, name, lambda *a, call=getattr(B.lib, name): launched.append(1) or call(*a))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    new = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype).as_subclass(OnGpu)  # noqa: E731
+    of = new(0, dtype=torch.int32) if flat else new(0, k, dtype=torch.int32)
+    x, w = new(0, 100), new(0, k)
+    for rows in (new(0, 100), new(6, 100)):
+        B.dispatch_rows(x, of, rows, weight=w, stream=0)
+        B.dispatch_rows(x, of, rows, stream=0)
+        B.combine_rows(rows, of, x, weight=w, stream=0)
+        B.combine_rows_backward(x, rows, of, w, torch.zeros_like(rows), new(0, k), stream=0)
+        B.combine_rows_backward(x, rows, of, None, None, new(0, k), stream=0)
+    assert len(launched) == 10
+    with pytest.raises(ValueError, match="d_weight"):
+        B.combine_rows_backward(x, rows, of, w, None, new(0, k + 1), stream=0)
+    with pytest.raises(ValueError, match="row_of"):
+        B.dispatch_rows(x, new(3, dtype=torch.int32), rows, weight=w, stream=0)
+
+
 # ------------------------------------------------------------------------------------ the plain forms
 @pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
 def test_plain_powers_of_two(kind):
