@@ -67,7 +67,7 @@ class Block:
         return self.y
 
     def backward(self, logits, d_y, stream=None, d_w=None):
-        """d_y [T, d] float32, after forward() on the same logits -> (d_x through the experts [T, d] bf16, d_logits [T, E]), on `stream` or
+        """d_y [T, d] float32, its elements wherever they lie, after forward() on the same logits -> (d_x through the experts [T, d] bf16, d_logits [T, E]), on `stream` or
         torch's current one, like forward(): torch's operations and the library's one behind the other.  d_w: (d_w1 [E, d, f], d_w2 [E, f, d]), to which the
         gradients of the matrices are added."""
         stream = stream or torch.cuda.current_stream()
@@ -82,6 +82,7 @@ class Block:
     def _backward(self, logits, d_y, d_w):
         R = self.T * self.k
         new = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
+        d_y = d_y.contiguous()  # the gradient of a sum over tokens is one row for all of them, which the library's calls do not take
         # y[t] = sum over j of weight[t, j] * y_rows[row_of[t, j]]
         d_weight, g, values = new(self.T, self.k, dtype=torch.float32), _codes(R, self.d, torch.float8_e5m2), new(R, self.d) if d_w else None
         B.combine_rows_backward(d_y, self.y_rows, self.row_of, self.weight, values, d_weight, *g)

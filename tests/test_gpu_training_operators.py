@@ -640,6 +640,25 @@ def test_gradients_of_the_matrices_of_a_block(example, T, d, f, E, k, train):
     block.close()
 
 
+def test_gradients_of_a_block_take_a_gradient_that_lies_in_any_way(example):
+    """One row for all tokens (what the sum over tokens has for a gradient), one number for all, columns that do not lie side by side: the bits of a copy."""
+    say("block gradients, layouts")
+    T, d, f, E, k = 50, 128, 200, 8, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    block = example.Block(0.05 * normal(E, d, f), 0.05 * normal(E, f, d), None, k, T, train=True, renormalize=True)
+    x, z = normal(T, d).bfloat16(), normal(T, E)
+    block.forward(x, z)
+    for d_y in (normal(1, d).expand(T, d), normal(1, 1).expand(T, d), normal(d, T).t(), normal(T, 2 * d)[:, ::2]):
+        both = []
+        for t in (d_y, d_y.clone(memory_format=torch.contiguous_format)):
+            d_w = torch.zeros(E, d, f, device="cuda"), torch.zeros(E, f, d, device="cuda")
+            both.append([*block.backward(z, t, d_w=d_w), *d_w])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(*both))
+    block.close()
+
+
 def test_step_of_training_replays_from_a_captured_graph(example):
     """Forward, backward and gradients of the matrices of a block, captured; replays with the eager work of other inputs between them give the eager bits."""
     say("training captured")
