@@ -531,8 +531,9 @@ int pgmoe_relu_backward(const void *d_h, int64_t d_h_stride, int d_h_dtype, int 
 /* Gradient of the experts' matrices, y = x . W, from rows kept in 8 bits: for every expert e and its rows [expert_offsets[e],
  * expert_offsets[e+1]) of x and d_y
  *   d_w[e] = add[e] + sum over the rows of (code * scale of x)^T . d_y         add[e], or 0, for an expert without rows
- * on the matrix cores, sums in float32, rounded once.  Operands are bfloat16 pieces that add up to the values (but for a part in 2^32): one for codes whose scales are
- * powers of two (x->dtype | PGMOE_SCALE_POW2: their exponents are taken, whatever else a scale holds), else three; one for gradients in PGMOE_BF16, two in
+ * on the matrix cores, sums in float32, rounded once.  Operands are bfloat16 pieces that add up to the values, but for 2^-131 (gradients in F16: a part in 2^32); none is zero if its value is not,
+ * so that an infinity beside any other value counts as one.  One piece for codes whose scales are powers of two (x->dtype | PGMOE_SCALE_POW2: their exponents are taken, whatever else
+ * a scale holds), else three of code times scale in float32; one for gradients in PGMOE_BF16, two in
  * F16, three in F32.  Products of pieces i and j are taken while i + j is below the larger count: 1 to 6 for each row, input and output.
  *   x rows of n_in = x->cols columns, at most 2^24    d_y dev [x->rows, n_out], rows d_y_stride >= n_out elements apart
  *   expert_offsets dev [n_experts+1]    d_w dev [n_experts, n_in, n_out] out    add: in d_w's type and layout | NULL; may be d_w itself

@@ -39,24 +39,36 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
-// PIECES bfloat16 whose sum is v but for a part in 2^32 (of two: 16 bits, of three: 24).  All have v's sign and none is zero if v is not, so
-// that an infinity times each of them is the infinity that it times v is: pieces are cut off, not rounded, and what is left of v is
-// raised by that part.  (Products of pieces that are left out are below 2^-20 of the first, on the mean 2^-23.)
+// PIECES bfloat16 that add up to v's leading 8 * PIECES bits, but for bfloat16's least step, 2^-133, each.  All have v's sign and none is zero if v is not, however small it is, so
+// that an infinity times each of them is the infinity that it times v is: pieces are cut off, not rounded, and v and what is left of it each time are first raised by a
+// step towards v's side.  v: raised already; of(left, j): raises what is left of v[j].  (Products of pieces that are left out are below 2^-20 of the first, on the mean 2^-23.)
 __device__ inline int high_halves(float a, float b) { return (int)__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
-template <int PIECES>
-__device__ inline void take_apart(const float (&v)[8], intx4 (&to)[PIECES]) {
-    float rest[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) rest[j] = __builtin_canonicalizef(v[j]);  // NaN: with a bit that is not cut off
+__device__ inline float between(float v, float limit) { return __builtin_amdgcn_fmed3f(v, -limit, limit); }
+__device__ inline float least_step(float v) { return between(v, 0x1p-133f); }  // 0 of 0; v itself if that is less
+template <int PIECES, typename Raised>
+__device__ inline void take_apart(float (&v)[8], intx4 (&to)[PIECES], Raised &&raised) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-        to[p] = intx4{high_halves(rest[0], rest[1]), high_halves(rest[2], rest[3]), high_halves(rest[4], rest[5]), high_halves(rest[6], rest[7])};
+        to[p] = intx4{high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]), high_halves(v[6], v[7])};
+        if (p + 1 < PIECES) {  // of an infinity the largest bfloat16 is taken off: the infinity is left
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float left = fmaf(v[j], 0x1p-32f, rest[j] - __uint_as_float(__float_as_uint(rest[j]) & 0xffff0000u));
-            rest[j] = fabsf(v[j]) < INFINITY ? left : rest[j];
+            for (int j = 0; j < 8; ++j) v[j] = raised(v[j] - between(__uint_as_float(__float_as_uint(v[j]) & 0xffff0000u), 0x1.fep127f), j);
         }
     }
+}
+// Gradients: of 16-bit floating point, whose least value is 2^-24, a part in 2^32 is far above a step and does as well.
+__device__ inline void take_apart(float (&v)[8], intx4 (&to)[2]) {
+    const float whole[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+    take_apart<2>(v, to, [&](float left, int j) { return fmaf(whole[j], 0x1p-32f, left); });
+}
+__device__ inline void take_apart(float (&v)[8], intx4 (&to)[3]) {
+    float step[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        step[j] = least_step(v[j] * 0x1p16f);  // the least float32, 2^-149, has a whole one too
+        v[j] += step[j];                       // NaN: with a bit that is not cut off
+    }
+    take_apart<3>(v, to, [&](float left, int j) { return left + step[j]; });
 }
 
 // Eight codes times their scale.
@@ -74,16 +86,19 @@ __device__ inline void open_codes(intx2 codes, float scale, intx4 (&to)[PIECES])
         }
         to[0] = intx4{pairs[0], pairs[1], pairs[2], pairs[3]};
     } else {
-        float v[8];
+        float v[8], step[8];  // a code is 2^-16 or more, or 0
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             floatx2 pair;
             if constexpr (Q == PGMOE_E4M3) pair = j & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(codes[j >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(codes[j >> 1], false);
             else pair = j & 1 ? __builtin_amdgcn_cvt_pk_f32_bf8(codes[j >> 1], true) : __builtin_amdgcn_cvt_pk_f32_bf8(codes[j >> 1], false);
-            v[2 * j] = pair[0] * scale;
-            v[2 * j + 1] = pair[1] * scale;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                step[2 * j + i] = least_step(pair[i]);
+                v[2 * j + i] = fmaf(pair[i], scale, step[2 * j + i]);
+            }
         }
-        take_apart<PIECES>(v, to);
+        take_apart<PIECES>(v, to, [&](float left, int j) { return left + step[j]; });
     }
 }
 
@@ -331,7 +346,7 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = (float)grad[i].v[j];
-                take_apart<PY>(v, py);
+                take_apart(v, py);
             }
 #pragma unroll
             for (int p = 0; p < PY; ++p) put(to + PX * XPLANE + p * YPLANE + r * S::YS + y_piece * 16, r < requested ? py[p] : none);

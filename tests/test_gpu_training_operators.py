@@ -463,6 +463,62 @@ def test_expert_weight_gradient_passes_on_what_is_not_finite(B, pow2, y_kind):
     assert torch.equal(got[2][130] == -float("inf"), last > 0) and torch.equal(got[2][130] == float("inf"), last < 0)
 
 
+def tiny(g, shape, lowest):
+    """Float32 of 24 bits and of eight, magnitudes from 2^lowest to 2^(lowest + 60), each sign."""
+    v = (1 + g.random(shape)) * np.exp2(g.integers(lowest, lowest + 60, shape))
+    v = np.where(g.random(shape) < 0.5, v, np.exp2(np.floor(np.log2(v))))
+    return (v * g.choice([-1, 1], shape)).astype(np.float32)
+
+
+def keep_rows(p, x, x_kind, scale):
+    """Rows x of codes' values, [R, n_in], with scales [blocks, R], in place of the ones p has."""
+    p.x[:, :p.n_in], p.x_s = x, scale.astype(np.float32)
+    p.x_q, p.x_scale = dev(p.x, x_kind), dev(p.x_s)
+    p.x = f64(p.x_q)
+
+
+@pytest.mark.parametrize("y_kind,x_kind,pow2", [("f32", "e5m2", True), ("f32", "e5m2", False), ("f32", "e4m3", False), ("bf16", "e4m3", False), ("f16", "e5m2", False)])
+def test_expert_weight_gradient_of_tiny_values(B, y_kind, x_kind, pow2):
+    """Next to infinities they count with their sign, however small they are, and among finite values they are off by a few of bfloat16's least steps, 2^-133: a
+    value's three pieces are each a step from it at most, so an operand is below 2^-131 off."""
+    say("gradient tiny", y_kind, x_kind, pow2)
+    counts, n_in, n_out = [9, 0, 34], 136, 144
+    p = Gradient(B, counts, n_in, n_out, x_kind, y_kind, pow2)
+    g = np.random.default_rng(n_in)
+    if y_kind == "f32":
+        p.d_y = dev(tiny(g, (p.R, n_out), -149))
+        assert (f64(p.d_y) != 0).all()
+    if not pow2:
+        small = (1 + g.random((2, p.R))) * np.exp2(g.integers(-126, -90, (2, p.R)))
+        if y_kind == "f32":
+            small = np.where(g.random((2, p.R)) < 0.5, small, 1 + g.random((2, p.R)))
+        small[:, 3], small[:, 20] = 2.0 ** -126, 1.5 * 2.0 ** -115      # rows that meet an infinity below
+        keep_rows(p, p.x[:, :n_in], x_kind, small)
+    for finite in (True, False):
+        if not finite:
+            d_y, x = f64(p.d_y), p.x.copy()
+            d_y[3, 5], d_y[20, 100] = np.inf, -np.inf
+            p.d_y = dev(d_y, y_kind)
+            if x_kind == "e5m2":
+                x[7, 11], x[30, 130] = -np.inf, np.inf
+                keep_rows(p, x[:, :n_in], x_kind, p.x_s)
+        got = f64(p.run("f32"))
+        with np.errstate(invalid="ignore"):
+            want, mag = O.expert_weight_gradient(p.x[:, :n_in], p.x_s, f64(p.d_y), p.offs)
+        there = np.isfinite(want)
+        assert there.all() == finite
+        same = np.array_equal(got[~there], want[~there], equal_nan=True)
+        assert same, finite
+        xs = np.abs(p.x[:, :n_in] * np.repeat(p.x_s.astype(np.float64).T, 128, axis=1)[:, :n_in])
+        for e in range(3):
+            lo, hi = p.offs[e], p.offs[e + 1]
+            # relative as for other values; an operand off by 2^-131 beside the other's magnitude, twice as much for the products that are left out; sums below 2^-126 are multiples
+            # of 2^-149 after each of their terms; code times scale is one in float32
+            with np.errstate(invalid="ignore"):
+                err = (p.terms * 34 + 34) * H * mag[e] + 2.0 ** -130 * (xs[lo:hi].sum(0)[:, None] + np.abs(f64(p.d_y)[lo:hi]).sum(0)[None]) + p.terms * 34 * 2.0 ** -149
+                assert np.all(np.abs(got[e] - want[e])[there[e]] <= err[there[e]]), (e, finite)
+
+
 def test_expert_weight_gradient_is_that_of_differences_of_the_product(B):
     """The loss <x . W, c> of expert_matmul is linear in W: for a W of one code the product is that entry's column of x times it."""
     say("gradient differences")
