@@ -457,8 +457,9 @@ typedef struct {
     int32_t dtype;        /* PGMOE_E4M3 or PGMOE_E5M2, possibly | PGMOE_SCALE_POW2 */
 } pgmoe_fp8_rows;
 /* In the dtype of rows that are written: a block's scale is the least power of two, at least 2^-126, by which its largest finite
- * magnitude is within the type (so that code times scale is a bfloat16 as it stands: pgmoe_expert_weight_gradient() needs a
- * third of the products); codes are as exact as with any scale.  (A block's value from 2^128 (1 - 2^-5) on, e5m2 2^128 (1 - 2^-4), becomes 2^128, which
+ * magnitude is within the type (so that code times scale is a bfloat16 as it stands, but for the smallest scales: pgmoe_expert_weight_gradient() needs a
+ * third of the products).  The scale is up to twice the one it would be otherwise: codes in the type's normal range are as exact, values that are small beside their block's largest
+ * have steps up to twice as wide.  (A block's value from 2^128 (1 - 2^-5) on, e5m2 2^128 (1 - 2^-4), becomes 2^128, which
  * float32 takes for an infinity.)  In the dtype of rows that are read: the scales are powers of two, which only that call looks at. */
 #define PGMOE_SCALE_POW2 0x100
 /* Weights, e4m3: the matrices of n_experts experts, y = x . W with W [n_in, n_out] as everywhere in this header, one
@@ -533,8 +534,8 @@ int pgmoe_relu_backward(const void *d_h, int64_t d_h_stride, int d_h_dtype, int 
  *   d_w[e] = add[e] + sum over the rows of (code * scale of x)^T . d_y         add[e], or 0, for an expert without rows
  * on the matrix cores, sums in float32, rounded once.  Operands are bfloat16 pieces that add up to the values, but for 2^-131 (gradients in F16: a part in 2^32); none is zero if its value is not,
  * so that an infinity beside any other value counts as one.  One piece for codes whose scales are powers of two (x->dtype | PGMOE_SCALE_POW2: their exponents are taken, whatever else
- * a scale holds), else three of code times scale in float32; one for gradients in PGMOE_BF16, two in
- * F16, three in F32.  Products of pieces i and j are taken while i + j is below the larger count: 1 to 6 for each row, input and output.
+ * a scale holds; with scales below 2^-124, e5m2 2^-117, small codes times them are between bfloat16's values, multiples of 2^-133, and become the nearest, zero among them), else three of
+ * code times scale in float32; one for gradients in PGMOE_BF16, two in F16, three in F32.  Products of pieces i and j are taken while i + j is below the larger count: 1 to 6 for each row, input and output.
  *   x rows of n_in = x->cols columns, at most 2^24    d_y dev [x->rows, n_out], rows d_y_stride >= n_out elements apart
  *   expert_offsets dev [n_experts+1]    d_w dev [n_experts, n_in, n_out] out    add: in d_w's type and layout | NULL; may be d_w itself
  *   workspace dev, 16-byte aligned | NULL, workspace_bytes: where there are few matrices and many rows, these are split over workgroups that leave

@@ -519,6 +519,34 @@ def test_expert_weight_gradient_of_tiny_values(B, y_kind, x_kind, pow2):
                 assert np.all(np.abs(got[e] - want[e])[there[e]] <= err[there[e]]), (e, finite)
 
 
+@pytest.mark.parametrize("y_kind", DTYPES)
+@pytest.mark.parametrize("x_kind,pow2,scale,least", [("e4m3", True, 2.0 ** -126, 2.0 ** -134), ("e4m3", True, 2.0 ** -124, 0), ("e4m3", True, 2.0 ** 120, 0), ("e5m2", True, 2.0 ** -126, 2.0 ** -134),
+                                                     ("e5m2", True, 2.0 ** -117, 0), ("e5m2", True, 2.0 ** 112, 0), ("e4m3", False, 1.25 * 2.0 ** -126, 2.0 ** -131), ("e5m2", False, 2.0 ** -126, 2.0 ** -131),
+                                                     ("e4m3", False, 1.9 * 2.0 ** 119, 2.0 ** -131), ("e5m2", False, 1.9 * 2.0 ** 111, 2.0 ** -131)])
+def test_expert_weight_gradient_at_both_ends_of_the_scales(B, x_kind, pow2, scale, least, y_kind):
+    """Every finite code but those that the scale takes past float32.  `least`: how far an operand may be off besides roundings: half of bfloat16's least step where a scale that is a power
+    of two leaves less than that, and 2^-131 for three pieces."""
+    say("gradient scales", x_kind, pow2, scale, y_kind)
+    counts, n_in, n_out = [300], 136, 144
+    p = Gradient(B, counts, n_in, n_out, x_kind, y_kind, pow2)
+    codes = torch.arange(256, dtype=torch.uint8).view(TORCH[x_kind]).float().double().numpy()
+    codes = codes[np.isfinite(codes) & (np.abs(codes * scale) < 2.0 ** 127)]
+    g = np.random.default_rng(int(n_in + abs(np.log2(scale))))
+    keep_rows(p, g.choice(codes, (p.R, n_in)), x_kind, np.full((2, p.R), scale))
+    p.d_y = dev(g.standard_normal((p.R, n_out)) * (2.0 ** -14 if scale > 1 else 1), y_kind)
+    want, mag = O.expert_weight_gradient(p.x[:, :n_in], p.x_s, f64(p.d_y), p.offs)
+    y = np.abs(f64(p.d_y)).sum(0)
+    # gradients of three pieces are 2^-131 off beside a code times its scale; sums below 2^-126 are multiples of 2^-149 after each of their terms; (-0 and 0 in `codes` make zeros)
+    x = np.abs(p.x[:, :n_in]).sum(0)[:, None] * scale
+    err = (p.terms * p.R + 34) * H * mag + least * y[None] + (2.0 ** -130 * x if y_kind == "f32" else 0) + p.terms * p.R * 2.0 ** -149
+    got = f64(p.run("f32"))
+    assert np.isfinite(got).all() and np.abs(want).max() < 2.0 ** 126
+    worst = (np.abs(got - want) - err).max()
+    assert worst <= 0
+    if scale < 1:
+        assert got.any()
+
+
 def test_expert_weight_gradient_is_that_of_differences_of_the_product(B):
     """The loss <x . W, c> of expert_matmul is linear in W: for a W of one code the product is that entry's column of x times it."""
     say("gradient differences")
