@@ -509,7 +509,7 @@ int pgmoe_dispatch_rows(const void *x, int64_t x_stride, int x_dtype, int T, int
                         const float *weight, void *rows, int64_t rows_stride, int rows_dtype, int n_rows,
                         const pgmoe_fp8_rows *rows_q, void *stream);
 /* y[t] = add[t] + sum over j of weight[t, j] * rows[row_of[t, j]], in ascending j; without weights the gradient of
- * pgmoe_dispatch_rows().
+ * pgmoe_dispatch_rows().  (pgmoe_combine() is the stack's form of it, for the sizes and the type of its context, and gives the same bits there.)
  *   rows dev [n_rows, d]    add dev [T, d] in y's type | NULL; may be y itself    y dev [T, d] out */
 int pgmoe_combine_rows(const void *rows, int64_t rows_stride, int rows_dtype, int n_rows, const int32_t *row_of, int copies,
                        const float *weight, const void *add, int64_t add_stride, int T, int d, void *y, int64_t y_stride,

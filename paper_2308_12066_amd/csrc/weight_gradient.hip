@@ -2,9 +2,10 @@
 //
 //   d_w[e, i, o] = add[e, i, o] + sum over the rows r of expert e of  x[r, i] d_y[r, o],   x[r, i] = code[r, i] * scale[r, i / 128]
 //
-// The scales of x vary along the sum, so they cannot be taken out of it: the matrix cores' operand is code times scale.  Where scales are
-// powers of two that is a bfloat16 as it stands (four bits), and one product a row, input and output is exact.  Otherwise code times scale in 32
-// bits is taken apart into three bfloat16 whose sum it is, and so are gradients of 32 bits; those of 16-bit floating point are the sum of two.
+// The scales of x vary along the sum, so they are in one of its operands; here it is that of the codes, code times scale.  Where scales are
+// powers of two that is a bfloat16 as it stands (four bits; scales below 2^-124, e5m2 2^-117, leave some codes less), and one product a row, input and output is exact.  Otherwise code times scale in 32
+// bits is taken apart into three bfloat16 whose sum it is, and so are gradients of 32 bits; those of 16-bit floating point are the sum of two.  (A tile of 128 inputs has one scale a row: its mantissa could go
+// to the gradients instead, which would take three products whatever their type, where five and six are taken now.  Not built.)
 #include <algorithm>
 #include <atomic>
 
@@ -214,7 +215,7 @@ __device__ inline GradientItem gradient_item(const GradientArgs &a, int i) {
 // An item is BI inputs by BO outputs; a workgroup takes every gridDim-th of them and goes through its rows K at a time.  Both sides come through registers, where codes are converted,
 // into one of two buffers in LDS while the other is multiplied, also from one item to the next: the first rows of an item arrive under the last products of the one before.
 // Bound by the products on many rows, 1.12 PFLOP/s (each further 512 rows for each of 64 experts of 1024 x 4096: 246 us), and by the results on few: their float32 leave at 5.5 TB/s, about
-// 160 us of the 426 that 512 rows an expert take, mostly not under the products (workgroups started at different times gained nothing). Without loads the same call takes 340, without stores 270.
+// 160 us of the 411 that 512 rows an expert take, mostly not under the products (workgroups started at different times gained nothing). Without loads the same call takes 340, without stores 270.
 template <int WI_, int WO_, int NI_, int K_>
 struct GradientShape {
     static constexpr int WI = WI_, WO = WO_, NI = NI_, NO = 4, K = K_;  // wavefronts; 16 x 16 tiles of one
@@ -352,7 +353,7 @@ __global__ __launch_bounds__(S::THREADS, S::waves(PX, pieces_of<Y>)) void weight
             for (int p = 0; p < PY; ++p) put(to + PX * XPLANE + p * YPLANE + r * S::YS + y_piece * 16, r < requested ? py[p] : none);
         }
     };
-    // Gradients are the first operand: a lane's four results of a product are neighbouring outputs of one input.
+    // Rows are the first operand: a lane's four results of a product are neighbouring inputs of one output (input_of), until store_rows exchanges them.
     floatx4 acc[S::NI][S::NO];
     auto multiply = [&](int at) {
 #pragma unroll
@@ -490,10 +491,10 @@ static int launch_shape(GradientArgs a, hipStream_t s, int64_t most, bool spread
     hipLaunchKernelGGL((weight_gradient_kernel<XQ, Y, PX, VEC, S>), dim3((unsigned)grid), dim3(S::THREADS), LDS, s, a);
     return PGMOE_OK;
 }
-// Into how many parts the rows of each expert are split where there are fewer tiles than workgroups run at once.  A tile by itself takes 17 to 18.5 ns a row; parts cost two more
-// launches' overhead and a write and a read of 64 KiB each at 3 TB/s.  us without parts / with as many as this says, bfloat16 gradients: one expert of 512 x 1024 from 512 rows 12.7 (2 parts
-// would take 14.1), 1024 19.9 / 17.3, 4096 74 / 25, 16384 279 / 40; one of 1024 x 4096 from 1024 rows 25.4 (2: 29.7), 4096 76 / 59; eight of 512 x 512 from 512 rows each
-// 14.0 (2: 18.4), 2048 41 / 29; eight of 1024 x 1024 from 4096 each 93 to 97 (2: 91).
+// Into how many parts the rows of each expert are split where there are fewer tiles than workgroups run at once.  A tile by itself takes 17 to 18.5 ns a row; the rule, fitted to the
+// times below, takes the cost of parts, a launch and planes of 64 KiB a tile that are written and read, for 4 us and 0.021 us for each part of each tile.  us without parts / with as many as this says, bfloat16 gradients: one expert of 512 x 1024 from 512 rows 12.7 (2 parts
+// would take 14.0), 1024 20.3 / 16.7, 4096 73 / 30, 16384 279 / 42; one of 1024 x 4096 from 1024 rows 25.0 (2: 32.6), 4096 76 / 60; eight of 512 x 512 from 512 rows each
+// 13.7 (2: 26.6), 2048 40 / 31; eight of 1024 x 1024 from 4096 each 89 (2: 107).
 constexpr int GRADIENT_PARTS = 16, CUS = 256;
 static int gradient_parts(int rows, int E, int n_in, int n_out) {
     const int64_t tiles = (int64_t)E * fp8_blocks(n_in) * fp8_blocks(n_out);
@@ -517,16 +518,17 @@ static int launch_parts(const GradientArgs &a, float *planes, hipStream_t s) {
     else hipLaunchKernelGGL((gradient_parts_kernel<_Float16, VEC>), grid, dim3(256), 0, s, planes, a, SmallTile::K);
     return PGMOE_OK;
 }
-// Which tiles (us, bfloat16 gradients with scales that are powers of two unless said otherwise, float32 results):
-//  * 256 x 256, one workgroup a CU: from 256 rows an expert on the mean on, if the last round of a tile for each CU leaves at most a fifth of them idle (64 experts of 1024 x 4096 from 64 rows each 228, 128 x 128
-//    219, 256 rows 303 / 370, 512 426 / 493; 16 of 512 x 2048 from 256 24.5 / 22.8, 2048 80 / 99; 192 tiles: eight of 768 x 2048 from 512 28.2 / 24.8, 2048 68 / 65);
+// Which tiles (us, bfloat16 gradients with scales that are powers of two unless said otherwise, float32 results, rows dealt out evenly):
+//  * 256 x 256, one workgroup a CU: from 256 rows an expert on the mean on, if the last round of a tile for each CU leaves at most a fifth of them idle (64 experts of 1024 x 4096 from 64 rows each 222, 128 x 128
+//    193, 256 rows 282 / 344, 512 399 / 475; 16 of 512 x 2048 from 256 21.3 / 20.1, 2048 76 / 92; 192 tiles: eight of 768 x 2048 from 512 24.8 / 22.7, 2048 64 / 62);
 //  * 128 x 256, one workgroup a CU, where pieces of both sides leave room in LDS for no more, if there are more of 128 x 128 than CUs: 16 experts of 2048 x 768 from 512 rows each, three and three pieces
-//    153, 128 x 128 234; eight of 1024 x 1024 from 32 rows 16.0 / 21.6; eight of 512 x 512 from 512 rows, three and two pieces 44 / 36.  Against two workgroups a CU, the second when the first ends, and one
-//    an item: 16 of 2048 x 1024, three and two pieces, from 512 rows each 179 / 188 / 181, from 32 36.6 / 38.9 / 45.3, with a fifth of 8192 rows in one 236.4 / 236.5 / 240.5;
-//  * 128 x 128 otherwise.
+//    149, 128 x 128 217; eight of 1024 x 1024 from 32 rows 13.0 / 17.2; eight of 512 x 512 from 512 rows, three and two pieces 41 / 32.  Against two workgroups a CU, the second when the first ends, and one
+//    an item: 16 of 2048 x 1024, three and two pieces, from 512 rows each 156 / 160 / 163, from 32 29.5 / 32.5 / 38.2, with a fifth of 8192 rows in one 218.6 / 218.5 / 223.2;
+//  * 128 x 128 otherwise.  (Two or three products with scales that are powers of two have no other: the larger tiles were not built for them.  16 experts
+//    of 2048 x 1024 from 512 rows each: 16-bit floating point 84, float32 128; 64 of 1024 x 4096 685 and 1031.)
 // And in which order, of the two smaller ones: from 256 rows an expert on the mean on, and if not all items run at once, those of experts with many rows first, one a workgroup, of which the next goes where one has ended
-// (`sorted`; in order / sorted, rows dealt out evenly, and with nearly a quarter in one of 16: 8192 rows for 16 experts of 2048 x 1024, three and two pieces, 167 / 173 and 257 / 190; for 32 of 1024 x 1024 95 / 107 and 157 / 115;
-// 4096 for 16 of 768 x 2048, one piece, 28.6 / 30.4 and 44 / 33).
+// (`sorted`; in order / sorted, rows dealt out evenly, and with nearly a quarter in one: 8192 rows for 16 experts of 2048 x 1024, three and two pieces, 156 / 167 and 233 / 178; for 32 of 1024 x 1024 86 / 103 and 192 / 143;
+// 4096 for 16 of 768 x 2048, one piece, 28.2 / 29.6 and 37 / 33).
 template <int XQ, typename Y, int PX, bool VEC>
 static int launch_gradient(GradientArgs a, float *planes, hipStream_t s) {
     if (a.parts > 1) return launch_parts<XQ, Y, PX, VEC>(a, planes, s);

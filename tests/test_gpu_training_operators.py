@@ -204,6 +204,23 @@ def test_combine_skips_dropped_copies_whatever_their_weights(B):
     assert torch.all(y == 1)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("T,k,d", [(1, 1, 512), (1, 2, 1024), (64, 2, 768), (1100, 8, 2048), (1500, 2, 512)])
+def test_both_combines_give_the_same_bits(B, T, k, d, kind):
+    """The context's and the one without, of the same rows."""
+    say("both combines", T, k, d, kind)
+    g = np.random.default_rng(T)
+    row_of, R = entries(g, T, k)
+    rows, of, w = dev(g.standard_normal((R, d)), kind), ints(row_of), dev(g.random((T, k)))
+    ctx = B.Context(B.make_config(d, 64, 16, k, 1, T, B.BF16 if kind == "bf16" else B.F32))
+    y, z = (torch.full((T, d), 7.0, device="cuda").to(TORCH[kind]) for _ in range(2))
+    ctx.combine(rows, of, w, T, y, stream=torch.cuda.current_stream())
+    B.combine_rows(rows, of, z, w)
+    torch.cuda.synchronize()
+    assert torch.equal(y, z)
+    ctx.close()
+
+
 # ------------------------------------------------------------------------------------ combine's gradient
 @pytest.mark.parametrize("T,k,d", SHAPES)
 @pytest.mark.parametrize("weighed", [False, True])
