@@ -45,7 +45,7 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 // step towards v's side.  v: raised already; of(left, j): raises what is left of v[j].  (Products of pieces that are left out are below 2^-20 of the first, on the mean 2^-23.)
 __device__ inline int high_halves(float a, float b) { return (int)__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
 __device__ inline float between(float v, float limit) { return __builtin_amdgcn_fmed3f(v, -limit, limit); }
-__device__ inline float least_step(float v) { return between(v, 0x1p-133f); }  // 0 of 0; v itself if that is less
+constexpr float LEAST_STEP = 0x1p-133f;
 template <int PIECES, typename Raised>
 __device__ inline void take_apart(float (&v)[8], intx4 (&to)[PIECES], Raised &&raised) {
 #pragma unroll
@@ -66,7 +66,7 @@ __device__ inline void take_apart(float (&v)[8], intx4 (&to)[3]) {
     float step[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        step[j] = least_step(v[j] * 0x1p16f);  // the least float32, 2^-149, has a whole one too
+        step[j] = between(v[j] * 0x1p16f, LEAST_STEP);  // the least float32, 2^-149, has a whole one too, 0 none
         v[j] += step[j];                       // NaN: with a bit that is not cut off
     }
     take_apart<3>(v, to, [&](float left, int j) { return left + step[j]; });
@@ -87,7 +87,8 @@ __device__ inline void open_codes(intx2 codes, float scale, intx4 (&to)[PIECES])
         }
         to[0] = intx4{pairs[0], pairs[1], pairs[2], pairs[3]};
     } else {
-        float v[8], step[8];  // a code is 2^-16 or more, or 0
+        float v[8], step[8];
+        const float least = between(scale, LEAST_STEP);  // the step of a code, which is 2^-16 or more, or 0; rows with a scale of 0 add nothing
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             floatx2 pair;
@@ -95,7 +96,7 @@ __device__ inline void open_codes(intx2 codes, float scale, intx4 (&to)[PIECES])
             else pair = j & 1 ? __builtin_amdgcn_cvt_pk_f32_bf8(codes[j >> 1], true) : __builtin_amdgcn_cvt_pk_f32_bf8(codes[j >> 1], false);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                step[2 * j + i] = least_step(pair[i]);
+                step[2 * j + i] = between(pair[i], least);
                 v[2 * j + i] = fmaf(pair[i], scale, step[2 * j + i]);
             }
         }

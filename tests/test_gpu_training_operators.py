@@ -564,6 +564,20 @@ def test_expert_weight_gradient_at_both_ends_of_the_scales(B, x_kind, pow2, scal
         assert got.any()
 
 
+@pytest.mark.parametrize("y_kind", DTYPES)
+def test_expert_weight_gradient_of_rows_with_a_scale_of_zero(B, y_kind):
+    """Codes that are left over in rows whose scales are 0, which a plan's spare rows are cleared to, add nothing: the bits of zero codes."""
+    say("gradient scales of zero", y_kind)
+    p = Gradient(B, [60, 7], 136, 144, "e4m3", y_kind, False)
+    p.x_scale[:, 10:20] = 0
+    p.x_scale[1, 60:] = 0
+    got = p.run("f32")
+    codes = p.x_q.view(torch.uint8)
+    codes[10:20] = 0
+    codes[60:, 128:] = 0
+    assert torch.equal(got, p.run("f32")) and not got[1][128:].any() and got[1][:128].any()
+
+
 def test_expert_weight_gradient_is_that_of_differences_of_the_product(B):
     """The loss <x . W, c> of expert_matmul is linear in W: for a W of one code the product is that entry's column of x times it."""
     say("gradient differences")
